@@ -637,6 +637,128 @@ enum {
 TAPOUT_API tapout_status tapout_profile_enable(tapout_ctx *ctx, uint32_t kind_mask, int32_t max_records);
 TAPOUT_API tapout_status tapout_profile_read(tapout_ctx *ctx, int32_t kind, double *total_ms, int32_t *launches, void *stream);
 
+/*
+ * The draft model's output head: the product that writes the draft logits, and
+ * the loss that trains it.
+ *
+ * Speculative sampling is exact whatever the draft distribution is, so the draft
+ * head is where low precision costs accepted tokens only, never correctness:
+ * its weights can be held in 4 bits (tapout_mx4_quantize), and
+ * tapout_head_logits_mx4 writes the [B,K,V] rows that tapout_draft_stats and
+ * tapout_verify read.  Its weights (and the draft model below, through the
+ * gradient by the hidden states) are trained on the tokens that rounds emitted
+ * with tapout_head_loss and tapout_head_loss_grad, which never hold the logits
+ * of more than one piece of the vocabulary.
+ *
+ * Everything under "General rules" holds, with a tapout_head in the place of the
+ * context: it owns the scratch memory of its calls, which must be issued in
+ * stream order on one stream at a time (two captured graphs of one head must not
+ * run at the same time; take a head each), and allocates only in
+ * tapout_head_create.
+ *
+ * Layout.  Hidden states are [B,K,dim] with the last axis contiguous, weights
+ * [V,dim] with contiguous rows; strides are in elements.  Unlike logits, they must be
+ * 16-byte aligned, strides included (TAPOUT_EINVAL otherwise), and dim must be a
+ * multiple of 32.  Row strides of weights are at most 8 MiB.
+ */
+typedef struct tapout_head tapout_head;
+
+typedef struct {
+    int32_t device;                       /* HIP device ordinal                                 */
+    int32_t max_rows;                     /* largest B * K of any call, at most 2^20            */
+    int32_t dim;                          /* length of a hidden state: a multiple of 32, at most 65536 */
+    int32_t vocab;                        /* largest V of any call, at most 2^24                */
+    int32_t dtype;                        /* tapout_dtype of hidden states and weights          */
+    int32_t training;                     /* 1: tapout_head_loss_grad may be called; adds       */
+                                          /* scratch: up to 1 GiB for a piece of the vocabulary */
+                                          /* (more where 256 vocabulary rows need more), and 4  */
+                                          /* bytes an element of the hidden states, at least 64 MiB */
+} tapout_head_config;
+
+typedef struct {
+    const void *ptr;                      /* device pointer to element [0,0]                    */
+    int32_t dtype;                        /* tapout_dtype                                       */
+    int64_t stride;                       /* elements from row to row; columns are contiguous   */
+} tapout_matrix;
+
+TAPOUT_API tapout_status tapout_head_create(tapout_head **out, const tapout_head_config *cfg);
+TAPOUT_API tapout_status tapout_head_destroy(tapout_head *head);
+/* Text of the last error on head; with NULL the text of the last failed
+ * tapout_head_create or tapout_mx4_* call on this thread.                     */
+TAPOUT_API const char *tapout_head_last_error(const tapout_head *head);
+
+/*
+ * Microscaled 4-bit floating point (OCP MX, E2M1 elements, E8M0 scales).  32
+ * neighbours of a row share a scale 2^e held as the byte e + 127:
+ *   e = max(floor(log2 max|x|) - 2, -127)
+ * and an element is x / 2^e rounded to {0, 0.5, 1, 1.5, 2, 3, 4, 6} (codes 0..7,
+ * bit 3 the sign) to nearest, ties to the even code, magnitudes from 5 on to 6.
+ * A block that holds a NaN or an infinity gets the scale byte 255: all its
+ * elements stand for NaN.  No context, on the CURRENT HIP device.
+ *   codes   [rows, P / 2] u8, P = cols rounded up to a multiple of 128; element
+ *           2n in the low half of byte n; 16-byte aligned
+ *   scales  [rows, P / 32] u8, 4-byte aligned
+ * tapout_mx4_quantize writes the columns behind cols as zeros (scale byte 0).
+ * cols: a multiple of 32; x and out 16-byte aligned, strides included.
+ * tapout_mx4_dequantize writes the values that codes stand for, which are exact
+ * in either type (magnitudes beyond its range: infinite).
+ */
+TAPOUT_API tapout_status tapout_mx4_quantize(const tapout_matrix *x, int32_t rows, int32_t cols,
+                                  uint8_t *codes, uint8_t *scales, void *stream);
+TAPOUT_API tapout_status tapout_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int32_t rows, int32_t cols,
+                                  const tapout_matrix *out, void *stream);
+
+/*
+ * Draft logits of hidden states under a head held in 4 bits:
+ *   out[b,k,v] = sum_d h[b,k,d] w[v,d],  w the values of codes / scales [V, dim]
+ * summed in binary32 and rounded once.  For bfloat16 heads.
+ *   act_bits 16: h as it is;  4: h is quantised like the weights first (two to
+ *            three times the rate where rows are many; scores get noise of the
+ *            order of a tenth of their spread)
+ *   k_len    [B] i32 or NULL: rows k >= k_len[b] of out are left untouched (and
+ *            the hidden states there may hold anything, but must be addressable)
+ *   out      [B,K,V] logits, binary32 or bfloat16, any element-aligned address
+ *            and strides, as the calls above take them
+ */
+TAPOUT_API tapout_status tapout_head_logits_mx4(tapout_head *head, const tapout_logits *hidden,
+                                  const uint8_t *codes, const uint8_t *scales,
+                                  int32_t B, int32_t K, int32_t V, const int32_t *k_len, int32_t act_bits,
+                                  const tapout_logits *out, void *stream);
+
+/*
+ * Cross entropy of softmax(h W^T) at one target token a row:
+ *   z = h W^T,  lse = ln sum_v exp(z_v),  loss = lse - z[target]
+ *   hidden  [B,K,dim], weight [V,dim]: the head's type
+ *   target  [B,K] i32; negative: the row is left out (loss 0)
+ *   loss, lse [B,K] f32
+ *   flags   [B] u32 or NULL (overwritten): BAD_TOKEN, a target >= V (loss NaN);
+ *           BAD_ROW, a row that counts whose logits hold a NaN or have no finite
+ *           lse (loss and lse NaN)
+ */
+TAPOUT_API tapout_status tapout_head_loss(tapout_head *head, const tapout_logits *hidden, const tapout_matrix *weight,
+                                  int32_t B, int32_t K, int32_t V, const int32_t *target,
+                                  float *loss, float *lse, uint32_t *flags, void *stream);
+
+/*
+ * Gradient of  scale * sum over rows of row_weight * loss  by both factors:
+ *   g = row_weight (exp(z - lse) - [v = target]),
+ *   grad_hidden = scale g W,  grad_weight = scale g^T h
+ * The logits are formed again, a piece of the vocabulary at a time; g is rounded
+ * to the head's type before the products (which is why a factor that all rows
+ * share belongs into scale: it meets the sums, in binary32), the results once.
+ * Rows that are left out (a target outside [0, V), an lse that is not finite, a
+ * row_weight of 0) contribute nothing, whatever their hidden states hold, and
+ * get zeros.
+ *   lse         [B,K] f32 of tapout_head_loss on the same inputs
+ *   row_weight  [B,K] f32 or NULL (1)
+ *   scale       [1] f32 on the device, or NULL (1): for a mean, 1 / rows
+ *   grad_hidden [B,K,dim], grad_weight [V,dim]: the head's type, overwritten
+ */
+TAPOUT_API tapout_status tapout_head_loss_grad(tapout_head *head, const tapout_logits *hidden, const tapout_matrix *weight,
+                                  int32_t B, int32_t K, int32_t V, const int32_t *target, const float *lse,
+                                  const float *row_weight, const float *scale,
+                                  const tapout_logits *grad_hidden, const tapout_matrix *grad_weight, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

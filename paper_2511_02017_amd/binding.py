@@ -36,7 +36,9 @@ EXPORTS = ("tapout_default_config", "tapout_create", "tapout_destroy", "tapout_l
            "tapout_shard_stats", "tapout_draft_stats_sharded", "tapout_verify_accept_sharded",
            "tapout_shard_final_sums", "tapout_shard_final_token",
            "tapout_set_option",
-           "tapout_profile_enable", "tapout_profile_read")
+           "tapout_profile_enable", "tapout_profile_read",
+           "tapout_head_create", "tapout_head_destroy", "tapout_head_last_error", "tapout_mx4_quantize", "tapout_mx4_dequantize",
+           "tapout_head_logits_mx4", "tapout_head_loss", "tapout_head_loss_grad")
 
 PROFILE_KINDS = ("select", "draft_pass", "draft_finalize", "target_pass", "verify_head", "verify_slices", "verify_locate", "update",
                  "sample_head", "sample_slices", "sample_locate", "stream_pair")
@@ -63,6 +65,15 @@ class TapoutRoundArgs(C.Structure):
                                           "active", "lse", "entropy", "p_top1", "p_top2", "margin", "top1_id", "logq_tok", "n_stop",
                                           "stop_fired", "draft_flags", "accept_len", "out_tok", "n_out", "target_lse", "logp_tok",
                                           "target_top1", "verify_flags", "select_flags")]
+
+
+class TapoutHeadConfig(C.Structure):
+    _fields_ = [("device", C.c_int32), ("max_rows", C.c_int32), ("dim", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32),
+                ("training", C.c_int32)]
+
+
+class TapoutMatrix(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32), ("stride", C.c_int64)]
 
 
 class TapoutError(RuntimeError):
@@ -129,6 +140,16 @@ def load_library(path: str = None):
         lib.tapout_set_option.argtypes = [vp, C.c_char_p, i32]
         lib.tapout_profile_enable.argtypes = [vp, C.c_uint32, i32]
         lib.tapout_profile_read.argtypes = [vp, i32, C.POINTER(C.c_double), C.POINTER(i32), vp]
+        lg, mx = C.POINTER(TapoutLogits), C.POINTER(TapoutMatrix)
+        lib.tapout_head_create.argtypes = [C.POINTER(vp), C.POINTER(TapoutHeadConfig)]
+        lib.tapout_head_destroy.argtypes = [vp]
+        lib.tapout_head_last_error.restype = C.c_char_p
+        lib.tapout_head_last_error.argtypes = [vp]
+        lib.tapout_mx4_quantize.argtypes = [mx, i32, i32, vp, vp, vp]
+        lib.tapout_mx4_dequantize.argtypes = [vp, vp, i32, i32, mx, vp]
+        lib.tapout_head_logits_mx4.argtypes = [vp, lg, vp, vp, i32, i32, i32, vp, i32, lg, vp]
+        lib.tapout_head_loss.argtypes = [vp, lg, mx, i32, i32, i32] + [vp] * 5
+        lib.tapout_head_loss_grad.argtypes = [vp, lg, mx, i32, i32, i32, vp, vp, vp, vp, lg, mx, vp]
         _lib = lib
     return _lib
 
@@ -618,3 +639,176 @@ class Tapout:
         lm = None if lam is None else np.ascontiguousarray(lam, np.float64).reshape(nb, A)
         d = lambda x: None if x is None else x.ctypes.data
         self._check(self._lib.tapout_rule_state_set(self._ctx, d(pe), d(ar), d(lm), _stream(stream)))
+
+
+# ---- the draft model's output head ------------------------------------------------------------------------
+_DT = {torch.float32: F32, torch.bfloat16: BF16}
+MX4_BLOCK, MX4_PAD = 32, 128
+
+
+def _matrix(t, name) -> TapoutMatrix:
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-d GPU tensor")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    if t.dtype not in _DT:
+        raise ValueError(f"{name}: dtype {t.dtype} is not supported (float32 / bfloat16)")
+    return TapoutMatrix(t.data_ptr(), _DT[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _on(t, dev, name):
+    if t is not None and t.device != dev:
+        raise ValueError(f"{name} lives on {t.device}, expected {dev}")
+
+
+class _allocating_on:
+    """Outputs made inside belong to `stream`, so that their memory is not handed on while it still works on them."""
+
+    def __init__(self, stream):
+        self.ctx = torch.cuda.stream(stream) if stream is not None else None
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *e):
+        if self.ctx is not None:
+            self.ctx.__exit__(*e)
+
+
+def mx4_quantize(x, out=None, stream=None):
+    """tapout_mx4_quantize: x [rows, cols] to (codes uint8 [rows, P / 2], scales uint8 [rows, P / 32]), P = cols rounded up to 128.
+    `out`: such a pair to write into."""
+    lib = load_library()
+    m = _matrix(x, "x")
+    rows, cols = x.shape
+    P = -(-cols // MX4_PAD) * MX4_PAD
+    with torch.cuda.device(x.device):
+        if out is None:
+            with _allocating_on(stream):
+                out = (torch.empty((rows, P // 2), dtype=torch.uint8, device=x.device), torch.empty((rows, P // 32), dtype=torch.uint8, device=x.device))
+        codes, scales = out
+        _on(codes, x.device, "codes"), _on(scales, x.device, "scales")
+        st = lib.tapout_mx4_quantize(C.byref(m), rows, cols, _ptr(codes, torch.uint8, (rows, P // 2), "codes"),
+                                     _ptr(scales, torch.uint8, (rows, P // 32), "scales"), _stream(stream))
+    if st != 0:
+        raise TapoutError(st, lib.tapout_head_last_error(None).decode())
+    return out
+
+
+def mx4_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, stream=None):
+    """tapout_mx4_dequantize: the values [rows, cols] that codes and scales stand for."""
+    lib = load_library()
+    rows, P = codes.shape[0], -(-cols // MX4_PAD) * MX4_PAD
+    with torch.cuda.device(codes.device):
+        if out is None:
+            with _allocating_on(stream):
+                out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+        m = _matrix(out, "out")
+        if tuple(out.shape) != (rows, cols):
+            raise ValueError(f"out: expected shape {(rows, cols)}, got {tuple(out.shape)}")
+        _on(scales, codes.device, "scales"), _on(out, codes.device, "out")
+        st = lib.tapout_mx4_dequantize(_ptr(codes, torch.uint8, (rows, P // 2), "codes"), _ptr(scales, torch.uint8, (rows, P // 32), "scales"),
+                                       rows, cols, C.byref(m), _stream(stream))
+    if st != 0:
+        raise TapoutError(st, lib.tapout_head_last_error(None).decode())
+    return out
+
+
+class DraftHead:
+    """One tapout_head on one GPU: the scratch memory of a draft model's output head [V, dim] with V <= vocab, for calls of up to
+    max_rows hidden states.  training: loss_grad may be called."""
+
+    def __init__(self, max_rows: int, dim: int, vocab: int, *, dtype=torch.bfloat16, device: int = 0, training: bool = False):
+        self._lib = load_library()
+        if dtype not in _DT:
+            raise ValueError(f"dtype {dtype} is not supported (float32 / bfloat16)")
+        self.cfg = TapoutHeadConfig(device, max_rows, dim, vocab, _DT[dtype], 1 if training else 0)
+        self.dim, self.dtype, self.device = dim, dtype, torch.device("cuda", device)
+        self._head = C.c_void_p()
+        st = self._lib.tapout_head_create(C.byref(self._head), C.byref(self.cfg))
+        if st != 0:
+            raise TapoutError(st, self._lib.tapout_head_last_error(None).decode())
+
+    def close(self):
+        head = getattr(self, "_head", None)
+        if head is not None and head.value:
+            self._lib.tapout_head_destroy(head)
+            self._head = None
+
+    __del__ = close
+
+    def _check(self, st):
+        if st != 0:
+            raise TapoutError(st, self._lib.tapout_head_last_error(self._head).decode())
+
+    def _hidden(self, t, name) -> TapoutLogits:
+        if t.dim() != 3 or t.shape[2] != self.dim:
+            raise ValueError(f"{name} must be [B, K, {self.dim}], got {tuple(t.shape)}")
+        _on(t, self.device, name)
+        if t.stride(2) != 1:
+            raise ValueError(f"{name}: the last axis must be contiguous")
+        if t.dtype != self.dtype:
+            raise ValueError(f"{name}: expected {self.dtype}, got {t.dtype}")
+        # the stride of an axis of one entry says nothing
+        return TapoutLogits(t.data_ptr(), _DT[t.dtype], t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+    def _weight(self, t, name) -> TapoutMatrix:
+        m = _matrix(t, name)
+        _on(t, self.device, name)
+        if t.shape[1] != self.dim or t.dtype != self.dtype:
+            raise ValueError(f"{name} must be [V, {self.dim}] of {self.dtype}, got {tuple(t.shape)} of {t.dtype}")
+        return m
+
+    def logits(self, hidden, codes, scales, k_len=None, act_bits: int = 16, dtype=torch.bfloat16, out=None, stream=None):
+        """tapout_head_logits_mx4: the draft logits [B, K, V] of hidden states [B, K, dim] under the head codes, scales
+        (mx4_quantize).  With k_len, rows behind it are left as they are in `out` (and undefined without)."""
+        hd = self._hidden(hidden, "hidden")
+        (B, K, _), V, P = hidden.shape, codes.shape[0], -(-self.dim // MX4_PAD) * MX4_PAD
+        if out is None:
+            with _allocating_on(stream):
+                out = torch.empty((B, K, V), dtype=dtype, device=self.device)
+        lg = _logits(out, "out")
+        if tuple(out.shape) != (B, K, V):
+            raise ValueError(f"out: expected shape {(B, K, V)}, got {tuple(out.shape)}")
+        for t, n in ((codes, "codes"), (scales, "scales"), (k_len, "k_len"), (out, "out")):
+            _on(t, self.device, n)
+        self._check(self._lib.tapout_head_logits_mx4(
+            self._head, C.byref(hd), _ptr(codes, torch.uint8, (V, P // 2), "codes"), _ptr(scales, torch.uint8, (V, P // 32), "scales"),
+            B, K, V, _ptr(k_len, torch.int32, (B,), "k_len"), int(act_bits), C.byref(lg), _stream(stream)))
+        return out
+
+    def loss(self, hidden, weight, target, out=None, stream=None):
+        """tapout_head_loss.  Returns / fills a dict: loss, lse [B, K] float32, flags [B] int32."""
+        hd, w = self._hidden(hidden, "hidden"), self._weight(weight, "weight")
+        B, K, _ = hidden.shape
+        if out is None:
+            with _allocating_on(stream):
+                out = dict(loss=torch.empty((B, K), dtype=torch.float32, device=self.device), lse=torch.empty((B, K), dtype=torch.float32, device=self.device),
+                           flags=torch.empty(B, dtype=torch.int32, device=self.device))
+        _on(target, self.device, "target")
+        self._check(self._lib.tapout_head_loss(
+            self._head, C.byref(hd), C.byref(w), B, K, weight.shape[0], _ptr(target, torch.int32, (B, K), "target"),
+            _ptr(out["loss"], torch.float32, (B, K), "loss"), _ptr(out["lse"], torch.float32, (B, K), "lse"),
+            _ptr(out.get("flags"), torch.int32, (B,), "flags"), _stream(stream)))
+        return out
+
+    def loss_grad(self, hidden, weight, target, lse, row_weight=None, scale=None, out=None, stream=None):
+        """tapout_head_loss_grad.  Returns / fills a dict: grad_hidden [B, K, dim], grad_weight [V, dim], of the head's type."""
+        hd, w = self._hidden(hidden, "hidden"), self._weight(weight, "weight")
+        B, K, _ = hidden.shape
+        if out is None:
+            with _allocating_on(stream):
+                out = dict(grad_hidden=torch.empty((B, K, self.dim), dtype=self.dtype, device=self.device),
+                           grad_weight=torch.empty((weight.shape[0], self.dim), dtype=self.dtype, device=self.device))
+        gh, gw = self._hidden(out["grad_hidden"], "grad_hidden"), self._weight(out["grad_weight"], "grad_weight")
+        if tuple(out["grad_hidden"].shape) != tuple(hidden.shape) or out["grad_weight"].shape[0] != weight.shape[0]:
+            raise ValueError("grad_hidden and grad_weight must have the shapes of hidden and weight")
+        for t, n in ((target, "target"), (lse, "lse"), (row_weight, "row_weight"), (scale, "scale")):
+            _on(t, self.device, n)
+        f32 = torch.float32
+        self._check(self._lib.tapout_head_loss_grad(
+            self._head, C.byref(hd), C.byref(w), B, K, weight.shape[0], _ptr(target, torch.int32, (B, K), "target"),
+            _ptr(lse, f32, (B, K), "lse"), _ptr(row_weight, f32, (B, K), "row_weight"), _ptr(scale, f32, (1,), "scale"),
+            C.byref(gh), C.byref(gw), _stream(stream)))
+        return out

@@ -19,7 +19,7 @@ OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(PKG, "libtapout.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 LIB_STAMPS = os.path.join(PKG, "libtapout_stamps.so")
-SOURCES = ["row_reduce.hip", "finalize.hip", "verify.hip", "bandit.hip", "api.hip"]
+SOURCES = ["row_reduce.hip", "finalize.hip", "verify.hip", "bandit.hip", "api.hip", "head_loss.hip", "head_mx4.hip", "head_api.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
