@@ -48,13 +48,14 @@ struct Operand {
     int32_t scale_stride;   // bytes, a multiple of 4
 };
 
-// Exchange of a row's 16-byte chunks.  Both for 8 and for 16 lanes at a time the chunks of neighbouring rows fall into
-// different banks.
+// Exchange of a row's 16-byte chunks.  A 16-byte LDS read serves its 64 lanes sixteen at a time, lanes 0-3, 12-15 and 20-27, then
+// 4-11, 16-19 and 28-31, then the same of the upper half; with lane l at row l % 16 and chunk l / 16 of its row these sixteen meet
+// 64 different banks.  (With chunk ^ (row & 7), which suits sixteen lanes in a row, half of the LDS cycles were conflicts.)
 template <int R> __device__ __forceinline__ int chunk_swap(int row)
 {
-    if constexpr (R == 64) return ((row >> 2) & 1) | ((((row >> 1) ^ (row >> 3)) & 1) << 1);
-    else if constexpr (R == 128) return (row & 7) ^ ((row >> 3) & 1);
-    else return row & 15;
+    if constexpr (R == 64) return -(row >> 2) & 3;                            // four rows to 64 banks, lane's chunk l / 16
+    else if constexpr (R == 128) return (row >> 1) & 7;                       // two rows
+    else return (row & 3) | (row & 8) | (row & 8) >> 1;                       // one row; lane's chunk 4 (l / 16) + t
 }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, int64_t bytes)
@@ -63,7 +64,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, int64
     return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)n, 0x00020000);
 }
 
-// T rows of R bytes of a stage, in pieces of 1 KB (a wavefront's load), dealt out to NW wavefronts.
+// T rows of R bytes of a stage, in pieces of 1 KB (a wavefront's load), dealt out to NW wavefronts.  Every wavefront makes the same
+// number of loads, since it waits for them by their number: where the pieces do not come out even, some are loaded twice.
 template <int T, int R, int NW> struct Stager {
     static constexpr int pieces = T * R / 1024, per = (pieces + NW - 1) / NW;
     uint32_t off[per];
@@ -71,19 +73,14 @@ template <int T, int R, int NW> struct Stager {
     {
 #pragma unroll
         for (int n = 0; n < per; ++n) {
-            const int row = (wave + n * NW) * (1024 / R) + lane / (R / 16);
+            const int row = (wave + n * NW) % pieces * (1024 / R) + lane / (R / 16);
             const int chunk = (lane % (R / 16)) ^ chunk_swap<R>(row);
             off[n] = (uint32_t)(min(row, rows_left - 1) * stride) + chunk * 16;      // rows behind the last one: the last one again
         }
     }
-    __device__ void issue(__amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t k_byte, int wave) const
+    __device__ __forceinline__ void issue_one(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t k_byte, int wave) const
     {
-#pragma unroll
-        for (int n = 0; n < per; ++n) {
-            const int q = wave + n * NW;
-            if (pieces % NW == 0 || q < pieces)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + q * 1024), 16, off[n], k_byte, 0, 0);
-        }
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (wave + n * NW) % pieces * 1024), 16, off[n], k_byte, 0, 0);
     }
 };
 
@@ -95,23 +92,19 @@ template <int T, int S, int NW> struct ScaleStager {
     {
 #pragma unroll
         for (int n = 0; n < per; ++n) {
-            const int word = (wave + n * NW) * 64 + lane, row = word / (S / 4);
+            const int word = (wave + n * NW) % pieces * 64 + lane, row = word / (S / 4);
             off[n] = (uint32_t)min(row, rows_left - 1) * (uint32_t)stride + (word % (S / 4)) * 4;
         }
     }
-    __device__ void issue(__amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t k_byte, int wave) const
+    __device__ __forceinline__ void issue_one(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t k_byte, int wave) const
     {
-#pragma unroll
-        for (int n = 0; n < per; ++n) {
-            const int q = wave + n * NW;
-            if (pieces % NW == 0 || q < pieces)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + q * 256), 4, off[n], k_byte, 0, 0);
-        }
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (wave + n * NW) % pieces * 256), 4, off[n], k_byte, 0, 0);
     }
 };
 template <int T, int NW> struct ScaleStager<T, 0, NW> {
+    static constexpr int per = 0;
     __device__ void init(int, int, int, int) {}
-    __device__ void issue(__amdgpu_buffer_rsrc_t, char *, uint32_t, int) const {}
+    __device__ void issue_one(int, __amdgpu_buffer_rsrc_t, char *, uint32_t, int) const {}
 };
 
 __device__ __forceinline__ f32x4 mma_f32(u32x4 a, u32x4 b, f32x4 c)
@@ -145,75 +138,82 @@ __device__ __forceinline__ u32x4 codes_to_bf16(uint32_t w, float scale)
     return r;
 }
 
+template <int N> __device__ __forceinline__ void wait_loads_and_barrier()
+{
+    // the LDS reads of this wavefront are done, all of its loads but the last N have landed, and those of the others
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // TI x TJ results by WI x WJ wavefronts; a wavefront holds MI x NJ blocks of 16 x 16.  acc[mi][nj][r] of lane l is
 //   i = (wave's i) + 16 mi + 4 (l / 16) + r,   j = (wave's j) + 16 nj + l % 16.
+// I's part of a stage has three places in LDS, J's two: that is what 160 KB hold of 256 x 256 (128 x 128: twice a compute unit).
 template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
     using K = Kind<KIND>;
     static constexpr int kind = KIND, TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, NW = WI * WJ, threads = NW * 64;
     static constexpr int MI = TI / WI / 16, NJ = TJ / WJ / 16;
-    static constexpr int oJ = TI * K::row_i, oSI = oJ + TJ * K::row_j, oSJ = oSI + ((TI * K::scale_i + 255) & ~255);
-    static constexpr int stage_bytes = oSJ + ((TJ * K::scale_j + 255) & ~255), lds_bytes = 2 * stage_bytes;
+    static constexpr int up256(int n) { return (n + 255) & ~255; }
+    static constexpr int oSI = TI * K::row_i, bytes_i = oSI + up256(TI * K::scale_i);
+    static constexpr int oSJ = TJ * K::row_j, bytes_j = oSJ + up256(TJ * K::scale_j);
+    static constexpr int ring_i = KIND == kTileMx4 ? 2 : 3, ring_j = 2, lds_bytes = ring_i * bytes_i + ring_j * bytes_j;
     using Acc = f32x4[MI][NJ];
 
-    static __device__ __forceinline__ void compute(const char *st, int steps, int wi, int wj, int lane, Acc &acc)
+    // What a wavefront multiplies in one step.
+    struct Frags {
+        u32x4 a[MI], b[NJ];
+        uint32_t sa[K::scale_i ? MI : 1], sb[K::scale_j ? NJ : 1];
+    };
+    // Read n of the NJ + MI of a step, J's first: the next step begins with all of J and the first of I.
+    static constexpr int reads = NJ + MI;
+    static __device__ __forceinline__ void load_one(int n, const char *pi, const char *pj, int s, int wi, int wj, int lane, Frags &f)
     {
         const int r16 = lane & 15, g = lane >> 4;
-        const char *si = st + (wi * MI * 16 + r16) * K::row_i, *sj = st + oJ + (wj * NJ * 16 + r16) * K::row_j;
+        if (n < NJ) {
+            const int row = wj * NJ * 16 + r16;
+            f.b[n] = *(const u32x4 *)(pj + row * K::row_j + (((s * 4 + g) ^ chunk_swap<K::row_j>(r16)) * 16) + n * 16 * K::row_j);
+            // four scales, of the four lanes that share a row; the matrix instruction takes the low byte
+            if constexpr (K::scale_j > 0) f.sb[n] = *(const uint32_t *)(pj + oSJ + row * K::scale_j + s * 4 + n * 16 * K::scale_j);
+        } else {
+            const int m = n - NJ, row = wi * MI * 16 + r16;
+            f.a[m] = *(const u32x4 *)(pi + row * K::row_i + (((s * 4 + g) ^ chunk_swap<K::row_i>(r16)) * 16) + m * 16 * K::row_i);
+            if constexpr (K::scale_i > 0) f.sa[m] = *(const uint32_t *)(pi + oSI + row * K::scale_i + s * 4 + m * 16 * K::scale_i);
+        }
+    }
+    static __device__ __forceinline__ void multiply_row(int mi, const Frags &f, int lane, Acc &acc)
+    {
+        const int g8 = (lane >> 4) * 8;
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj)
+            acc[mi][nj] = KIND == kTileF32 ? mma_f32(f.a[mi], f.b[nj], acc[mi][nj])
+                        : KIND == kTileBf16 ? mma_bf16(f.a[mi], f.b[nj], acc[mi][nj])
+                                            : mma_mx4(f.a[mi], f.sa[K::scale_i ? mi : 0] >> g8, f.b[nj], f.sb[K::scale_j ? nj : 0] >> g8, acc[mi][nj]);
+    }
+    // kTileMx4W: a lane holds the 32 codes of block g of its row: four matrix instructions of 8 codes a lane, whose k are
+    // 32 g + 8 t .. + 7 on both sides.
+    static __device__ __forceinline__ void compute_w(const char *pi, const char *pj, int wi, int wj, int lane, Acc &acc)
+    {
+        const int r16 = lane & 15, g = lane >> 4;
+        const char *si = pi + (wi * MI * 16 + r16) * K::row_i, *sj = pj + (wj * NJ * 16 + r16) * K::row_j;
         const int xi = chunk_swap<K::row_i>(r16), xj = chunk_swap<K::row_j>(r16);
+        u32x4 a[MI];
+        float sa[MI];
+        const char *ssi = pi + oSI + (wi * MI * 16 + r16) * K::scale_i;
 #pragma unroll
-        for (int s = 0; s < K::steps; ++s) {
-            if (s > 0 && s >= steps) break;
-            if constexpr (KIND == kTileF32 || KIND == kTileBf16) {
-                u32x4 a[MI], b[NJ];
+        for (int mi = 0; mi < MI; ++mi) {
+            a[mi] = *(const u32x4 *)(si + mi * 16 * K::row_i + ((g ^ xi) * 16));
+            sa[mi] = scale_value((*(const uint32_t *)(ssi + mi * 16 * K::scale_i) >> (8 * g)) & 255u);
+        }
 #pragma unroll
-                for (int nj = 0; nj < NJ; ++nj) b[nj] = *(const u32x4 *)(sj + nj * 16 * K::row_j + (((s * 4 + g) ^ xj) * 16));
+        for (int t = 0; t < 4; ++t) {
+            u32x4 b[NJ];
 #pragma unroll
-                for (int mi = 0; mi < MI; ++mi) a[mi] = *(const u32x4 *)(si + mi * 16 * K::row_i + (((s * 4 + g) ^ xi) * 16));
+            for (int nj = 0; nj < NJ; ++nj) b[nj] = *(const u32x4 *)(sj + nj * 16 * K::row_j + (((g * 4 + t) ^ xj) * 16));
 #pragma unroll
-                for (int mi = 0; mi < MI; ++mi)
+            for (int mi = 0; mi < MI; ++mi) {
+                const u32x4 w = codes_to_bf16(a[mi][t], sa[mi]);
 #pragma unroll
-                    for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = KIND == kTileF32 ? mma_f32(a[mi], b[nj], acc[mi][nj]) : mma_bf16(a[mi], b[nj], acc[mi][nj]);
-            } else if constexpr (KIND == kTileMx4) {
-                u32x4 a[MI], b[NJ];
-                uint32_t sa[MI], sb[NJ];
-                const char *ssi = st + oSI + (wi * MI * 16 + r16) * K::scale_i + s * 4, *ssj = st + oSJ + (wj * NJ * 16 + r16) * K::scale_j + s * 4;
-#pragma unroll
-                for (int nj = 0; nj < NJ; ++nj) {
-                    b[nj] = *(const u32x4 *)(sj + nj * 16 * K::row_j + (((s * 4 + g) ^ xj) * 16));
-                    sb[nj] = *(const uint32_t *)(ssj + nj * 16 * K::scale_j) >> (8 * g);       // the low byte counts
-                }
-#pragma unroll
-                for (int mi = 0; mi < MI; ++mi) {
-                    a[mi] = *(const u32x4 *)(si + mi * 16 * K::row_i + (((s * 4 + g) ^ xi) * 16));
-                    sa[mi] = *(const uint32_t *)(ssi + mi * 16 * K::scale_i) >> (8 * g);
-                }
-#pragma unroll
-                for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                    for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = mma_mx4(a[mi], sa[mi], b[nj], sb[nj], acc[mi][nj]);
-            } else {
-                // A lane holds the 32 codes of block g of its row: four matrix instructions of 8 codes a lane, whose k are
-                // 32 g + 8 t .. + 7 on both sides.
-                u32x4 a[MI];
-                float sa[MI];
-                const char *ssi = st + oSI + (wi * MI * 16 + r16) * K::scale_i;
-#pragma unroll
-                for (int mi = 0; mi < MI; ++mi) {
-                    a[mi] = *(const u32x4 *)(si + mi * 16 * K::row_i + ((g ^ xi) * 16));
-                    sa[mi] = scale_value((*(const uint32_t *)(ssi + mi * 16 * K::scale_i) >> (8 * g)) & 255u);
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    u32x4 b[NJ];
-#pragma unroll
-                    for (int nj = 0; nj < NJ; ++nj) b[nj] = *(const u32x4 *)(sj + nj * 16 * K::row_j + (((g * 4 + t) ^ xj) * 16));
-#pragma unroll
-                    for (int mi = 0; mi < MI; ++mi) {
-                        const u32x4 w = codes_to_bf16(a[mi][t], sa[mi]);
-#pragma unroll
-                        for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = mma_bf16(w, b[nj], acc[mi][nj]);
-                    }
-                }
+                for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = mma_bf16(w, b[nj], acc[mi][nj]);
             }
         }
     }
@@ -246,20 +246,91 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
             rsj = buffer_of(J.scales + (int64_t)j0 * J.scale_stride, left_j * J.scale_stride);
             hj.init((int)min(left_j, (int64_t)TJ), J.scale_stride, wave, lane);
         }
-        auto issue = [&](int s, char *st) {
-            gi.issue(ri, st, (uint32_t)s * K::row_i, wave);
-            gj.issue(rj, st + oJ, (uint32_t)s * K::row_j, wave);
-            hi.issue(rsi, st + oSI, (uint32_t)s * K::scale_i, wave);
-            hj.issue(rsj, st + oSJ, (uint32_t)s * K::scale_j, wave);
+        // Load n of a stage's loads of either operand.  Behind the last stage: the last one again, into memory that nobody reads.
+        constexpr int loads_i = gi.per + hi.per, loads_j = gj.per + hj.per;
+        auto load_i = [&](int x, int s, char *to) {
+            const uint32_t at = (uint32_t)(first + min(s, n - 1));
+            if (x < gi.per) gi.issue_one(x, ri, to, at * K::row_i, wave);
+            else hi.issue_one(x - gi.per, rsi, to + oSI, at * K::scale_i, wave);
         };
-        if (n > 0) issue(first, lds);
-        __syncthreads();
-        for (int s = 0; s < n; ++s) {
-            char *now = lds + (s & 1) * stage_bytes;
-            if (s + 1 < n) issue(first + s + 1, lds + ((s + 1) & 1) * stage_bytes);
-            compute(now, first + s == n_all - 1 ? last_steps : K::steps, wi, wj, lane, acc);
-            __syncthreads();
+        auto load_j = [&](int x, int s, char *to) {
+            const uint32_t at = (uint32_t)(first + min(s, n - 1));
+            if (x < gj.per) gj.issue_one(x, rj, to, at * K::row_j, wave);
+            else hj.issue_one(x - gj.per, rsj, to + oSJ, at * K::scale_j, wave);
+        };
+        char *const lj = lds + ring_i * bytes_i;
+        if (n > 0) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int x = 0; x < loads_i; ++x) load_i(x, s, lds + s * bytes_i);
+#pragma unroll
+                for (int x = 0; x < loads_j; ++x) load_j(x, s, lj + s * bytes_j);
+            }
+            wait_loads_and_barrier<loads_i + loads_j>();
         }
+        // places of I's stages s, s + 1, s + 2
+        char *i0p = lds, *i1p = lds + bytes_i, *i2p = ring_i == 3 ? lds + 2 * bytes_i : i0p;
+        if constexpr (K::steps == 1) {
+            for (int s = 0; s < n; ++s) {
+                char *now = lj + (s & 1) * bytes_j;
+#pragma unroll
+                for (int x = 0; x < loads_i; ++x) load_i(x, s + 2, i2p);
+                compute_w(i0p, now, wi, wj, lane, acc);
+                wait_loads_and_barrier<loads_i>();
+#pragma unroll
+                for (int x = 0; x < loads_j; ++x) load_j(x, s + 2, now);
+                char *t = i0p; i0p = i1p; i1p = i2p; i2p = t;
+            }
+        } else if (n > 0) {
+            // The operands of a step are read while the step before multiplies; the barrier that hands J's place on lies between the
+            // last reads of the stage and its last products.  Reads and loads are dealt out between the products: a wavefront that
+            // issues all its loads at once waits for the others' loads to be taken, with no product under way.
+            Frags f0, f1;
+#pragma unroll
+            for (int x = 0; x < reads; ++x) load_one(x, i0p, lj, 0, wi, wj, lane, f0);
+            for (int s = 0; s + 1 < n; ++s) {
+                char *now = lj + (s & 1) * bytes_j, *next = lj + ((s + 1) & 1) * bytes_j;
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) {
+                    constexpr int fast = MI > 1 ? (MI + 1) / 2 : 1;          // all reads in the first half: the barrier waits for them
+#pragma unroll
+                    for (int x = mi * loads_i / MI; x < (mi + 1) * loads_i / MI; ++x)
+                        if (ring_i == 3) load_i(x, s + 2, i2p);
+#pragma unroll
+                    for (int x = mi * reads / fast; x < (mi + 1) * reads / fast && x < reads; ++x) load_one(x, i0p, now, 1, wi, wj, lane, f1);
+                    multiply_row(mi, f0, lane, acc);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                wait_loads_and_barrier<ring_i == 3 ? loads_i : 0>();
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) {
+#pragma unroll
+                    for (int x = mi * loads_i / MI; x < (mi + 1) * loads_i / MI; ++x)
+                        if (ring_i == 2) load_i(x, s + 2, i0p);
+#pragma unroll
+                    for (int x = mi * loads_j / MI; x < (mi + 1) * loads_j / MI; ++x) load_j(x, s + 2, now);
+#pragma unroll
+                    for (int x = mi * reads / MI; x < (mi + 1) * reads / MI; ++x) load_one(x, i1p, next, 0, wi, wj, lane, f0);
+                    multiply_row(mi, f1, lane, acc);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                char *t = i0p; i0p = i1p; i1p = ring_i == 3 ? i2p : t; i2p = t;
+            }
+            const bool two = first + n < n_all || last_steps == 2;
+            if (two) {
+#pragma unroll
+                for (int x = 0; x < reads; ++x) load_one(x, i0p, lj + ((n - 1) & 1) * bytes_j, 1, wi, wj, lane, f1);
+            }
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) multiply_row(mi, f0, lane, acc);
+            if (two) {
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) multiply_row(mi, f1, lane, acc);
+            }
+        }
+        wait_loads_and_barrier<0>();
+        __syncthreads();
     }
 };
 

@@ -314,7 +314,10 @@ template <class T, class E> hipError_t product_with(const ProductArgs &a, hipStr
 
 template <int KIND> using Small = Tile<KIND, 128, 32, 4, 1>;
 template <int KIND> using Mid = Tile<KIND, 128, 128, 2, 2>;
-template <int KIND> using Large = Tile<KIND, 256, 256, 2, 4>;
+#ifndef LARGE
+#define LARGE 256, 256, 2, 4
+#endif
+template <int KIND> using Large = Tile<KIND, LARGE>;
 
 }  // namespace
 

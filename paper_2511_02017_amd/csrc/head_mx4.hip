@@ -154,7 +154,7 @@ template <class E> hipError_t logits_of(const LogitsArgs &a, int kind, hipStream
 {
     if (kind == kTileMx4)
         return a.N <= 32 ? logits_with<Tile<kTileMx4, 128, 32, 4, 1>, E>(a, st)
-             : a.N <= 256 ? logits_with<Tile<kTileMx4, 128, 128, 2, 2>, E>(a, st) : logits_with<Tile<kTileMx4, 256, 256, 2, 4>, E>(a, st);
+             : logits_with<Tile<kTileMx4, 128, 128, 2, 2>, E>(a, st);
     return a.N <= 32 ? logits_with<Tile<kTileMx4W, 128, 32, 4, 1>, E>(a, st)
          : a.N <= 64 ? logits_with<Tile<kTileMx4W, 128, 64, 4, 1>, E>(a, st) : logits_with<Tile<kTileMx4W, 128, 128, 2, 2>, E>(a, st);
 }
