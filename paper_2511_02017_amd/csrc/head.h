@@ -17,7 +17,7 @@ struct LossArgs {
     Operand weight, hidden;      // I: vocabulary rows, J: tokens
     int32_t N, V, D, rows_per_seq, B;
     const int32_t *target;       // [N]
-    float2 *part;                // [N, tiles]: maximum and sum of exp(z - maximum) over a tile's vocabulary rows
+    float2 *part;                // [N, blocks]: maximum and sum of exp(z - maximum) over a wavefront's vocabulary rows
     float *target_logit;         // [N]
     float *loss, *lse;           // [N]
     uint32_t *flags;             // [B] or NULL
@@ -50,7 +50,7 @@ hipError_t launch_head_transpose(const TransposeArgs &a, int dtype, hipStream_t 
 // unless `first`; else out, scaled and rounded.
 struct ProductArgs {
     Operand I, J;
-    int32_t ni, nj, k;           // results and length of k in elements (a multiple of a matrix step)
+    int32_t ni, nj, k;           // results and length of k in elements (not 0)
     int32_t splits, first;
     float *part;                 // [splits, nj, ni]
     void *out; int64_t out_stride;             // elements
@@ -68,11 +68,11 @@ struct GradHiddenArgs {
 };
 hipError_t launch_head_grad_hidden(const GradHiddenArgs &a, int dtype, hipStream_t st);
 
-// dst [B * K, cols_pad] = src [B, K, cols], zeros behind `cols`.
+// dst [B * K, cols] = src [B, K, cols].
 struct PackArgs {
     const void *src; int64_t stride_b, stride_k;
     void *dst;
-    int32_t N, K, cols, cols_pad;
+    int32_t N, K, cols;
 };
 hipError_t launch_head_pack(const PackArgs &a, int dtype, hipStream_t st);
 
@@ -92,7 +92,7 @@ hipError_t launch_mx4_dequantize(const DequantArgs &a, int dtype, hipStream_t st
 
 struct LogitsArgs {
     Operand weight, hidden;
-    int32_t N, K, V, D;          // D as far as the operands reach: padded to whole matrix steps
+    int32_t N, K, V, D;
     const int32_t *k_len;
     void *out; int64_t stride_b, stride_k;
 };

@@ -11,9 +11,9 @@ using namespace tapout;
 
 struct tapout_head {
     tapout_head_config cfg;
-    float2 *part = nullptr;              // [max_rows, tiles of 128 vocabulary rows]
+    float2 *part = nullptr;              // [N, blocks of a wavefront's vocabulary rows]: at least 64 of them, 32 up to N = 32
     float *target_logit = nullptr;       // [max_rows]
-    void *packed = nullptr;              // [max_rows, dim padded to 128]: hidden states whose rows lie unevenly
+    void *packed = nullptr;              // [max_rows, dim]: hidden states whose rows lie unevenly
     uint8_t *act_codes = nullptr, *act_scales = nullptr;      // quantised hidden states (bfloat16 heads)
     // training only
     char *piece = nullptr;  size_t piece_cap = 0;             // a piece's gradient in both orientations and its weights transposed
@@ -95,18 +95,18 @@ bool rows_overlap(const tapout_logits *x, int B, int K, int len)
     return !(k >= len && b >= (K - 1) * k + len) && !(b >= len && k >= (B - 1) * b + len);
 }
 
-// The hidden states as an operand of N rows: as they lie where their rows are evenly spaced (and need no padding), else packed.
-hipError_t hidden_operand(tapout_head *h, const tapout_logits *x, int B, int K, int pad, hipStream_t st, Operand *op)
+// The hidden states as an operand of N rows: as they lie where their rows are evenly spaced, else packed.
+hipError_t hidden_operand(tapout_head *h, const tapout_logits *x, int B, int K, hipStream_t st, Operand *op)
 {
-    const int N = B * K, D = h->cfg.dim, esz = size_of(x->dtype), cols = up_to(D, pad);
+    const int N = B * K, D = h->cfg.dim, esz = size_of(x->dtype);
     const int64_t stride = K == 1 ? x->stride_b : x->stride_k;
     const bool even = B == 1 || K == 1 || x->stride_b == (int64_t)K * x->stride_k;
-    if (even && cols == D && stride * esz <= kMaxRowBytes) {
+    if (even && stride * esz <= kMaxRowBytes) {
         *op = Operand{x->ptr, stride * esz, N, D * esz, nullptr, 0};
         return hipSuccess;
     }
-    const PackArgs a{x->ptr, x->stride_b, x->stride_k, h->packed, N, K, D, cols};
-    *op = Operand{h->packed, (int64_t)cols * esz, N, cols * esz, nullptr, 0};
+    const PackArgs a{x->ptr, x->stride_b, x->stride_k, h->packed, N, K, D};
+    *op = Operand{h->packed, (int64_t)D * esz, N, D * esz, nullptr, 0};
     return launch_head_pack(a, x->dtype, st);
 }
 
@@ -134,9 +134,10 @@ tapout_status tapout_head_create(tapout_head **out, const tapout_head_config *cf
     h->cfg = *cfg;
     DeviceGuard guard(cfg->device);
     const size_t N = cfg->max_rows, D = cfg->dim, esz = size_of(cfg->dtype), P = mx4_cols(cfg->dim);
-    bool ok = hipMalloc(&h->part, N * ((cfg->vocab + 127) / 128) * sizeof(float2)) == hipSuccess
+    const size_t blocks = (cfg->vocab + 127) / 128;
+    bool ok = hipMalloc(&h->part, (N + std::min<size_t>(N, 32)) * 2 * blocks * sizeof(float2)) == hipSuccess
            && hipMalloc(&h->target_logit, N * sizeof(float)) == hipSuccess
-           && hipMalloc(&h->packed, N * P * esz) == hipSuccess;
+           && hipMalloc(&h->packed, N * D * esz) == hipSuccess;
     if (ok && cfg->dtype == TAPOUT_BF16)
         ok = hipMalloc(&h->act_codes, N * P / 2) == hipSuccess && hipMalloc(&h->act_scales, N * P / 32) == hipSuccess;
     if (ok && cfg->training) {
@@ -223,7 +224,7 @@ tapout_status tapout_head_logits_mx4(tapout_head *h, const tapout_logits *hidden
         e = launch_mx4_quantize(q, TAPOUT_BF16, st);
         a.hidden = Operand{h->act_codes, P / 2, N, P / 2, h->act_scales, P / 32};
     } else {
-        e = hidden_operand(h, hidden, B, K, kMx4Pad, st, &a.hidden);
+        e = hidden_operand(h, hidden, B, K, st, &a.hidden);
     }
     if (e != hipSuccess) return hip_fail(h, e, "hidden states");
     e = launch_head_logits(a, act_bits == 4 ? kTileMx4 : kTileMx4W, out->dtype, st);
@@ -242,7 +243,7 @@ tapout_status tapout_head_loss(tapout_head *h, const tapout_logits *hidden, cons
     DeviceGuard guard(h->cfg.device);
     hipStream_t st = (hipStream_t)stream;
     LossArgs a{};
-    hipError_t e = hidden_operand(h, hidden, B, K, 1, st, &a.hidden);
+    hipError_t e = hidden_operand(h, hidden, B, K, st, &a.hidden);
     if (e != hipSuccess) return hip_fail(h, e, "hidden states");
     const int esz = size_of(h->cfg.dtype);
     a.weight = Operand{weight->ptr, weight->stride * esz, V, h->cfg.dim * esz, nullptr, 0};
@@ -270,50 +271,48 @@ tapout_status tapout_head_loss_grad(tapout_head *h, const tapout_logits *hidden,
     if (N > 0 && (!target || !lse)) return fail(h, TAPOUT_EINVAL, "target or lse is NULL");
     DeviceGuard guard(h->cfg.device);
     hipStream_t st = (hipStream_t)stream;
-    const int N_pad = up_to(N, 32);
-    hipError_t e = hipSuccess;
-    Operand x{};
-    if (N > 0) {
-        e = hidden_operand(h, hidden, B, K, 1, st, &x);
-        if (e != hipSuccess) return hip_fail(h, e, "hidden states");
-        const TransposeArgs t{x.p, x.stride / esz, h->hidden_t, N_pad, N, D, N_pad, V, target, lse, row_weight};
-        e = launch_head_transpose(t, dt, st);
-        if (e != hipSuccess) return hip_fail(h, e, "hidden states transposed");
+    if (N == 0) {                                              // a transposition of nothing, padded: zeros
+        const TransposeArgs t{nullptr, 0, (void *)grad_weight->ptr, grad_weight->stride, 0, V, D, V, nullptr, nullptr, nullptr};
+        const hipError_t e = launch_head_transpose(t, dt, st);
+        return e == hipSuccess ? TAPOUT_OK : hip_fail(h, e, "grad_weight");
     }
+    const int N_pad = up_to(N, 32);
+    Operand x{};
+    hipError_t e = hidden_operand(h, hidden, B, K, st, &x);
+    if (e != hipSuccess) return hip_fail(h, e, "hidden states");
+    const TransposeArgs t{x.p, x.stride / esz, h->hidden_t, N_pad, N, D, N_pad, V, target, lse, row_weight};
+    e = launch_head_transpose(t, dt, st);
+    if (e != hipSuccess) return hip_fail(h, e, "hidden states transposed");
     // pieces of the vocabulary of equal length, as long as the scratch allows
     const size_t per = piece_bytes(1, N, D, esz);
     const int most = (int)std::min<size_t>(up_to(V, 256), h->piece_cap / per / 256 * 256);
     const int pieces = (V + most - 1) / most, len = up_to((V + pieces - 1) / pieces, 256);
     // runs of k of the product by the hidden states: as many as it takes to give every compute unit two tiles
-    int splits = 1;
-    if (N > 0) {
-        const int tiles = head_product_tiles(D, N, dt), stages = up_to(std::min(len, V), 64) / (dt == TAPOUT_F32 ? 32 : 64);
-        splits = std::max(1, std::min({512 / tiles, stages / 4, (int)(h->grad_cap / ((size_t)N * D))}));
-    }
+    const int tiles = head_product_tiles(D, N, dt), stages = up_to(std::min(len, V), 64) / (dt == TAPOUT_F32 ? 32 : 64);
+    int splits = std::max(1, std::min({512 / tiles, stages / 4, (int)(h->grad_cap / ((size_t)N * D))}));
+    splits = (stages + (stages + splits - 1) / splits - 1) / ((stages + splits - 1) / splits);        // runs of equal length, none of them empty
     for (int v0 = 0; v0 < V; v0 += len) {
         const int n = std::min(len, V - v0), n_pad = up_to(n, 64);
         const char *rows = (const char *)weight->ptr + v0 * weight->stride * esz;
         char *g = h->piece, *gt = g + (size_t)N * n_pad * esz, *wt = gt + (size_t)N_pad * n_pad * esz;
-        if (N > 0) {
-            GradArgs a{};
-            a.weight = Operand{rows, weight->stride * esz, n, D * esz, nullptr, 0};
-            a.hidden = x;
-            a.N = N; a.V = V; a.D = D; a.v0 = v0; a.n = n;
-            a.target = target; a.lse = lse; a.row_weight = row_weight;
-            a.g = g; a.g_stride = n_pad; a.gt = gt; a.gt_stride = N_pad;
-            e = launch_head_grad(a, dt, st);
-            if (e != hipSuccess) return hip_fail(h, e, "head_grad");
-            const TransposeArgs t{rows, weight->stride, wt, n_pad, n, D, n_pad, V, nullptr, nullptr, nullptr};
-            e = launch_head_transpose(t, dt, st);
-            if (e != hipSuccess) return hip_fail(h, e, "weights transposed");
-            ProductArgs p{};
-            p.I = Operand{wt, (int64_t)n_pad * esz, D, n_pad * esz, nullptr, 0};
-            p.J = Operand{g, (int64_t)n_pad * esz, N, n_pad * esz, nullptr, 0};
-            p.ni = D; p.nj = N; p.k = n_pad; p.splits = splits; p.first = v0 == 0; p.part = h->grad_part;
-            e = launch_head_product(p, dt, st);
-            if (e != hipSuccess) return hip_fail(h, e, "grad_hidden");
-        }
+        GradArgs a{};
+        a.weight = Operand{rows, weight->stride * esz, n, D * esz, nullptr, 0};
+        a.hidden = x;
+        a.N = N; a.V = V; a.D = D; a.v0 = v0; a.n = n;
+        a.target = target; a.lse = lse; a.row_weight = row_weight;
+        a.g = g; a.g_stride = n_pad; a.gt = gt; a.gt_stride = N_pad;
+        e = launch_head_grad(a, dt, st);
+        if (e != hipSuccess) return hip_fail(h, e, "head_grad");
+        const TransposeArgs t{rows, weight->stride, wt, n_pad, n, D, n_pad, V, nullptr, nullptr, nullptr};
+        e = launch_head_transpose(t, dt, st);
+        if (e != hipSuccess) return hip_fail(h, e, "weights transposed");
         ProductArgs p{};
+        p.I = Operand{wt, (int64_t)n_pad * esz, D, n_pad * esz, nullptr, 0};
+        p.J = Operand{g, (int64_t)n_pad * esz, N, n_pad * esz, nullptr, 0};
+        p.ni = D; p.nj = N; p.k = n_pad; p.splits = splits; p.first = v0 == 0; p.part = h->grad_part;
+        e = launch_head_product(p, dt, st);
+        if (e != hipSuccess) return hip_fail(h, e, "grad_hidden");
+        p = ProductArgs{};
         p.I = Operand{h->hidden_t, (int64_t)N_pad * esz, D, N_pad * esz, nullptr, 0};
         p.J = Operand{gt, (int64_t)N_pad * esz, n, N_pad * esz, nullptr, 0};
         p.ni = D; p.nj = n; p.k = N_pad; p.splits = 1;
@@ -321,13 +320,10 @@ tapout_status tapout_head_loss_grad(tapout_head *h, const tapout_logits *hidden,
         e = launch_head_product(p, dt, st);
         if (e != hipSuccess) return hip_fail(h, e, "grad_weight");
     }
-    if (N > 0) {
-        const GradHiddenArgs a{h->grad_part, splits, N, D, K, V, (void *)grad_hidden->ptr, grad_hidden->stride_b, grad_hidden->stride_k,
-                               scale, target, lse, row_weight};
-        e = launch_head_grad_hidden(a, dt, st);
-        if (e != hipSuccess) return hip_fail(h, e, "grad_hidden");
-    }
-    return TAPOUT_OK;
+    const GradHiddenArgs a{h->grad_part, splits, N, D, K, V, (void *)grad_hidden->ptr, grad_hidden->stride_b, grad_hidden->stride_k,
+                           scale, target, lse, row_weight};
+    e = launch_head_grad_hidden(a, dt, st);
+    return e == hipSuccess ? TAPOUT_OK : hip_fail(h, e, "grad_hidden");
 }
 
 }  // extern "C"

@@ -8,6 +8,8 @@
 // bank once.  The exchange is made on the source address, which stays within the row.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace tapout {
@@ -43,9 +45,9 @@ struct Operand {
     const void *p;          // row 0, 16-byte aligned
     int64_t stride;         // bytes from row to row, a multiple of 16; 256 of them within 2^31 (checked on the host)
     int32_t rows;
-    int32_t row_bytes;      // bytes of a row that may be read
+    int32_t row_bytes;      // bytes of a row, a multiple of 16: what lies behind counts as zeros
     const uint8_t *scales;  // kTileMx4, and I of kTileMx4W
-    int32_t scale_stride;   // bytes, a multiple of 4
+    int32_t scale_stride;   // bytes of a row's scales, a multiple of 4
 };
 
 // Exchange of a row's 16-byte chunks.  A 16-byte LDS read serves its 64 lanes sixteen at a time, lanes 0-3, 12-15 and 20-27, then
@@ -58,53 +60,49 @@ template <int R> __device__ __forceinline__ int chunk_swap(int row)
     else return (row & 3) | (row & 8) | (row & 8) >> 1;                       // one row; lane's chunk 4 (l / 16) + t
 }
 
+// The memory of `bytes` bytes from p on, at most 2^31 - 1 of them: loads of what lies behind bring zeros, into LDS too.
+constexpr uint32_t kNoMemory = 0x80000000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, int64_t bytes)
 {
-    const uint32_t n = bytes <= 0 ? 0u : bytes > 0xfffffff0ll ? 0xfffffff0u : (uint32_t)bytes;
-    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)n, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(bytes < 0x7fffffff ? bytes : 0x7fffffff), 0x00020000);
 }
 
-// T rows of R bytes of a stage, in pieces of 1 KB (a wavefront's load), dealt out to NW wavefronts.  Every wavefront makes the same
-// number of loads, since it waits for them by their number: where the pieces do not come out even, some are loaded twice.
-template <int T, int R, int NW> struct Stager {
-    static constexpr int pieces = T * R / 1024, per = (pieces + NW - 1) / NW;
-    uint32_t off[per];
-    __device__ void init(int rows_left, int64_t stride, int wave, int lane)
-    {
-#pragma unroll
-        for (int n = 0; n < per; ++n) {
-            const int row = (wave + n * NW) % pieces * (1024 / R) + lane / (R / 16);
-            const int chunk = (lane % (R / 16)) ^ chunk_swap<R>(row);
-            off[n] = (uint32_t)(min(row, rows_left - 1) * stride) + chunk * 16;      // rows behind the last one: the last one again
-        }
-    }
-    __device__ __forceinline__ void issue_one(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t k_byte, int wave) const
-    {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (wave + n * NW) % pieces * 1024), 16, off[n], k_byte, 0, 0);
-    }
-};
+// Which row of the tile lies at row q of its part of LDS, that is, which row a matrix instruction takes as its q % 16th.  A lane's
+// four results of one instruction are rows 4 (l / 16) .. + 3 of I and one row of J; with this order the results of two
+// instructions that are neighbours in I are eight neighbouring rows of I, and those of NJ neighbours in J are NJ neighbouring
+// rows of J, so that results leave the registers in 16-byte pieces, in either orientation, without passing through LDS.
+__device__ __forceinline__ int row_of_i(int q) { return (q & ~31) | (q & 12) << 1 | (q & 16) >> 2 | (q & 3); }
+template <int NJ> __device__ __forceinline__ int row_of_j(int q) { return q / (16 * NJ) * (16 * NJ) + (q & 15) * NJ + (q >> 4) % NJ; }
+template <int NJ> __device__ __forceinline__ int tile_row(int q) { if constexpr (NJ == 0) return row_of_i(q); else return row_of_j<NJ>(q); }
 
-// The scale bytes of a stage: S (4 or 8) a row, four a lane, 256 bytes a piece.
-template <int T, int S, int NW> struct ScaleStager {
-    static constexpr int pieces = (T * S + 255) / 256, per = (pieces + NW - 1) / NW;
-    uint32_t off[per];
-    __device__ void init(int rows_left, int stride, int wave, int lane)
+// T rows of R bytes of a stage, in pieces of a wavefront's load, W bytes a lane.  Every wavefront makes the same number of loads,
+// since it waits for them by their number: where there are fewer pieces than wavefronts, some are loaded twice.  Rows behind the
+// operand's last one and bytes behind a row's last one come as zeros.
+template <int T, int R, int W, int NW, int NJ> struct Stager {           // NJ = 0: I's rows
+    static constexpr int pieces = T * R / (64 * W) < 1 ? 1 : T * R / (64 * W), per = (pieces + NW - 1) / NW, rows = 64 * W / R, lanes = R / W;
+    static_assert(pieces % NW == 0 || pieces < NW, "");
+    uint32_t off, now, at;           // of this lane: from the tile's first row; the same, or nowhere; its first byte in a row's R
+    __device__ __forceinline__ void init(int64_t stride, int wave, int lane)
     {
-#pragma unroll
-        for (int n = 0; n < per; ++n) {
-            const int word = (wave + n * NW) % pieces * 64 + lane, row = word / (S / 4);
-            off[n] = (uint32_t)min(row, rows_left - 1) * (uint32_t)stride + (word % (S / 4)) * 4;
-        }
+        const int q = wave % pieces * rows + lane / lanes;
+        at = (uint32_t)((lane % lanes) ^ (W == 16 ? chunk_swap<R>(q) : 0)) * W;
+        off = (uint32_t)(tile_row<NJ>(q) * stride) + at;
     }
-    __device__ __forceinline__ void issue_one(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t k_byte, int wave) const
+    __device__ __forceinline__ void stage(int s, int row_bytes) { now = s * R + (int)at < row_bytes ? off : kNoMemory; }
+    // The row orders exchange bits of a row's number, and the wavefronts' pieces of one n differ in bits of their own.
+    __device__ __forceinline__ void issue(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, int s, int64_t stride, int wave) const
     {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (wave + n * NW) % pieces * 256), 4, off[n], k_byte, 0, 0);
+        const auto to = (__attribute__((address_space(3))) void *)(lds + (wave % pieces + n * NW) * (64 * W));
+        const uint32_t from = (uint32_t)(tile_row<NJ>(n * NW * rows) * stride) + (uint32_t)(s * R);
+        if constexpr (W == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, now, from, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 4, now, from, 0, 0);
     }
 };
-template <int T, int NW> struct ScaleStager<T, 0, NW> {
+struct NoStager {
     static constexpr int per = 0;
-    __device__ void init(int, int, int, int) {}
-    __device__ void issue_one(int, __amdgpu_buffer_rsrc_t, char *, uint32_t, int) const {}
+    __device__ __forceinline__ void init(int64_t, int, int) {}
+    __device__ __forceinline__ void stage(int, int) {}
+    __device__ __forceinline__ void issue(int, __amdgpu_buffer_rsrc_t, char *, int, int64_t, int) const {}
 };
 
 __device__ __forceinline__ f32x4 mma_f32(u32x4 a, u32x4 b, f32x4 c)
@@ -146,204 +144,282 @@ template <int N> __device__ __forceinline__ void wait_loads_and_barrier()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// TI x TJ results by WI x WJ wavefronts; a wavefront holds MI x NJ blocks of 16 x 16.  acc[mi][nj][r] of lane l is
-//   i = (wave's i) + 16 mi + 4 (l / 16) + r,   j = (wave's j) + 16 nj + l % 16.
-// I's part of a stage has three places in LDS, J's two: that is what 160 KB hold of 256 x 256 (128 x 128: twice a compute unit).
+// A workgroup's way through ni x nj tiles by `splits` runs of k.  Consecutive workgroups go to the eight dies in turn, each with an
+// L2 of its own: die x gets a run of tiles, of which its workgroups take every S-th, and a run walks bands of eight rows of
+// tiles (at the end four, two, one) by all J tiles, I fastest, so that the workgroups of a die share both operands at any
+// time.  Each step is a few additions: divisions would take longer than a stage of a short product.
+struct Walk {
+    int ni, nj, left, step;          // left: tiles of this workgroup's run from here on
+    int split, base, shift, in;      // band of 1 << shift rows of tiles from `base`, tile `in` of the band
+    __device__ __forceinline__ void band(int b)
+    {
+        base = b;
+        const int rest = ni - b;
+        shift = rest >= 8 ? 3 : rest >= 4 ? 2 : rest >= 2 ? 1 : 0;
+    }
+    __device__ __forceinline__ void settle()
+    {
+        while (in >= nj << shift) {
+            in -= nj << shift;
+            int b = base + (1 << shift);
+            if (b >= ni) { b = 0; ++split; }
+            band(b);
+        }
+    }
+    __device__ __forceinline__ Walk(int ni_, int nj_, int splits) : ni(ni_), nj(nj_)
+    {
+        const int n = ni * nj * splits, x = blockIdx.x & 7, q = n >> 3, r = n & 7, at = blockIdx.x >> 3;
+        left = q + (x < r) - at;
+        step = (gridDim.x + 7) >> 3;               // of a whole number of eights, or a tile for each workgroup
+        const int from = x * q + min(x, r) + at, one = ni * nj, b = (from % one) / (nj * 8);
+        split = from / one;
+        in = from % one - b * nj * 8;
+        band(b * 8);
+        settle();
+    }
+    __device__ __forceinline__ bool more() const { return left > step; }
+    __device__ __forceinline__ void next()
+    {
+        left -= step;
+        in += step;
+        settle();
+    }
+    __device__ __forceinline__ int i() const { return base + (in & ((1 << shift) - 1)); }
+    __device__ __forceinline__ int j() const { return in >> shift; }
+};
+
+// A tile at (i0, j0) over stages [first, first + n) of k.
+struct Work { int i0, j0, first, n; };
+
+// TI x TJ results by WI x WJ wavefronts; a wavefront holds MI x NJ blocks of 16 x 16.  acc[mi][nj][r] of a lane is
+//   i = i_of(mi) + r,   j = j_of(nj).
+// I's part of a stage has ring_i places in LDS, J's two: three and two are what 160 KB hold of 256 x 256 (128 x 128: twice a
+// compute unit).
 template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
     using K = Kind<KIND>;
     static constexpr int kind = KIND, TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, NW = WI * WJ, threads = NW * 64;
     static constexpr int MI = TI / WI / 16, NJ = TJ / WJ / 16;
+    static_assert(MI % 2 == 0, "rows of I are ordered by pairs of blocks");
     static constexpr int up256(int n) { return (n + 255) & ~255; }
     static constexpr int oSI = TI * K::row_i, bytes_i = oSI + up256(TI * K::scale_i);
     static constexpr int oSJ = TJ * K::row_j, bytes_j = oSJ + up256(TJ * K::scale_j);
-    static constexpr int ring_i = KIND == kTileMx4 ? 2 : 3, ring_j = 2, lds_bytes = ring_i * bytes_i + ring_j * bytes_j;
+    static constexpr int ring_i = KIND == kTileMx4 ? 2 : 3, ring_j = 2, ring_bytes = ring_i * bytes_i + ring_j * bytes_j;
+    static constexpr int per_cu = 163840 / ring_bytes < 1 ? 1 : 163840 / ring_bytes > 2048 / threads ? 2048 / threads : 163840 / ring_bytes;
     using Acc = f32x4[MI][NJ];
+    using StagerI = Stager<TI, K::row_i, 16, NW, 0>;
+    using StagerJ = Stager<TJ, K::row_j, 16, NW, NJ>;
+    using ScalesI = std::conditional_t<(K::scale_i > 0), Stager<TI, (K::scale_i > 0 ? K::scale_i : 4), 4, NW, 0>, NoStager>;
+    using ScalesJ = std::conditional_t<(K::scale_j > 0), Stager<TJ, (K::scale_j > 0 ? K::scale_j : 4), 4, NW, NJ>, NoStager>;
+    static constexpr int li = StagerI::per + ScalesI::per, lj = StagerJ::per + ScalesJ::per;       // loads of a wavefront and stage
 
-    // What a wavefront multiplies in one step.
+    static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
+    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    static __device__ __forceinline__ int i_of(int mi) { return wave() / WJ * (MI * 16) + (mi >> 1) * 32 + (lane() >> 4) * 8 + (mi & 1) * 4; }
+    static __device__ __forceinline__ int j_of(int nj) { return wave() % WJ * (NJ * 16) + (lane() & 15) * NJ + nj; }
+
+    // What a wavefront multiplies: blocks of I (those of the next step replace them one by one), and of J for two steps.
     struct Frags {
-        u32x4 a[MI], b[NJ];
-        uint32_t sa[K::scale_i ? MI : 1], sb[K::scale_j ? NJ : 1];
+        u32x4 a[KIND == kTileMx4W ? 2 : 1][MI], b[2][NJ];
+        uint32_t sa[KIND == kTileMx4W ? 2 : 1][K::scale_i ? MI : 1], sb[2][K::scale_j ? NJ : 1];
     };
-    // Read n of the NJ + MI of a step, J's first: the next step begins with all of J and the first of I.
-    static constexpr int reads = NJ + MI;
-    static __device__ __forceinline__ void load_one(int n, const char *pi, const char *pj, int s, int wi, int wj, int lane, Frags &f)
-    {
-        const int r16 = lane & 15, g = lane >> 4;
-        if (n < NJ) {
-            const int row = wj * NJ * 16 + r16;
-            f.b[n] = *(const u32x4 *)(pj + row * K::row_j + (((s * 4 + g) ^ chunk_swap<K::row_j>(r16)) * 16) + n * 16 * K::row_j);
-            // four scales, of the four lanes that share a row; the matrix instruction takes the low byte
-            if constexpr (K::scale_j > 0) f.sb[n] = *(const uint32_t *)(pj + oSJ + row * K::scale_j + s * 4 + n * 16 * K::scale_j);
-        } else {
-            const int m = n - NJ, row = wi * MI * 16 + r16;
-            f.a[m] = *(const u32x4 *)(pi + row * K::row_i + (((s * 4 + g) ^ chunk_swap<K::row_i>(r16)) * 16) + m * 16 * K::row_i);
-            if constexpr (K::scale_i > 0) f.sa[m] = *(const uint32_t *)(pi + oSI + row * K::scale_i + s * 4 + m * 16 * K::scale_i);
+    // Where this lane reads: its row of the first block, and the chunk of step 0; steps exchange bits of the chunk.
+    struct Places {
+        uint32_t a, b, sa, sb;
+        __device__ __forceinline__ Places()
+        {
+            const int r16 = lane() & 15, g = lane() >> 4, ra = wave() / WJ * MI * 16 + r16, rb = wave() % WJ * NJ * 16 + r16;
+            a = ra * K::row_i + (g ^ chunk_swap<K::row_i>(r16)) * 16;
+            b = rb * K::row_j + ((KIND == kTileMx4W ? g * 4 : g) ^ chunk_swap<K::row_j>(r16)) * 16;
+            sa = oSI + ra * K::scale_i + g;
+            sb = oSJ + rb * K::scale_j + g;
         }
-    }
-    static __device__ __forceinline__ void multiply_row(int mi, const Frags &f, int lane, Acc &acc)
+    };
+    static __device__ __forceinline__ void read_a(int set, int m, const char *pi, int s, const Places &at, Frags &f)
     {
-        const int g8 = (lane >> 4) * 8;
-#pragma unroll
-        for (int nj = 0; nj < NJ; ++nj)
-            acc[mi][nj] = KIND == kTileF32 ? mma_f32(f.a[mi], f.b[nj], acc[mi][nj])
-                        : KIND == kTileBf16 ? mma_bf16(f.a[mi], f.b[nj], acc[mi][nj])
-                                            : mma_mx4(f.a[mi], f.sa[K::scale_i ? mi : 0] >> g8, f.b[nj], f.sb[K::scale_j ? nj : 0] >> g8, acc[mi][nj]);
+        f.a[set][m] = *(const u32x4 *)(pi + (at.a ^ (s * 64)) + m * 16 * K::row_i);
+        // a byte of its own for every lane: shifted out of a word that four lanes read, it would hold up the matrix instructions, which
+        // wait for results of the vector ALU (6.6 and 4.1 PFLOP/s of 4-bit products with nothing else in the loop)
+        if constexpr (K::scale_i > 0) f.sa[set][m] = *(const uint8_t *)(pi + at.sa + s * 4 + m * 16 * K::scale_i);
     }
-    // kTileMx4W: a lane holds the 32 codes of block g of its row: four matrix instructions of 8 codes a lane, whose k are
-    // 32 g + 8 t .. + 7 on both sides.
-    static __device__ __forceinline__ void compute_w(const char *pi, const char *pj, int wi, int wj, int lane, Acc &acc)
+    static __device__ __forceinline__ void read_b(int set, int n, const char *pj, int s, const Places &at, Frags &f)
     {
-        const int r16 = lane & 15, g = lane >> 4;
-        const char *si = pi + (wi * MI * 16 + r16) * K::row_i, *sj = pj + (wj * NJ * 16 + r16) * K::row_j;
-        const int xi = chunk_swap<K::row_i>(r16), xj = chunk_swap<K::row_j>(r16);
-        u32x4 a[MI];
-        float sa[MI];
-        const char *ssi = pi + oSI + (wi * MI * 16 + r16) * K::scale_i;
+        f.b[set][n] = *(const u32x4 *)(pj + (at.b ^ (s * (KIND == kTileMx4W ? 16 : 64))) + n * 16 * K::row_j);
+        if constexpr (K::scale_j > 0) f.sb[set][n] = *(const uint8_t *)(pj + at.sb + s * 4 + n * 16 * K::scale_j);
+    }
+    // Row mi of blocks times the J blocks of `set`.  kTileMx4W: a lane holds the 32 codes of block l / 16 of its row; matrix
+    // instruction t of four takes codes 8 t .. + 7 of every lane, and the same k of J.
+    static __device__ __forceinline__ void multiply_row(int mi, int set_a, int set_b, int t, const Frags &f, Acc &acc)
+    {
+        u32x4 a = f.a[set_a][mi];
+        if constexpr (KIND == kTileMx4W) a = codes_to_bf16(a[t], scale_value(f.sa[set_a][mi]));
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-            a[mi] = *(const u32x4 *)(si + mi * 16 * K::row_i + ((g ^ xi) * 16));
-            sa[mi] = scale_value((*(const uint32_t *)(ssi + mi * 16 * K::scale_i) >> (8 * g)) & 255u);
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            u32x4 b[NJ];
-#pragma unroll
-            for (int nj = 0; nj < NJ; ++nj) b[nj] = *(const u32x4 *)(sj + nj * 16 * K::row_j + (((g * 4 + t) ^ xj) * 16));
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi) {
-                const u32x4 w = codes_to_bf16(a[mi][t], sa[mi]);
-#pragma unroll
-                for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = mma_bf16(w, b[nj], acc[mi][nj]);
-            }
+        for (int nj = 0; nj < NJ; ++nj) {
+            if constexpr (KIND == kTileF32) acc[mi][nj] = mma_f32(a, f.b[set_b][nj], acc[mi][nj]);
+            else if constexpr (KIND == kTileMx4) acc[mi][nj] = mma_mx4(a, f.sa[set_a][mi], f.b[set_b][nj], f.sb[set_b][nj], acc[mi][nj]);
+            else acc[mi][nj] = mma_bf16(a, f.b[set_b][nj], acc[mi][nj]);
         }
     }
 
-    // acc = the sums over stages [first, first + n); the last stage of k (index n_all - 1) has last_steps steps.  All
-    // wavefronts of the workgroup come here; LDS is free again when it returns.
-    static __device__ __forceinline__ void run(const Operand &I, const Operand &J, int i0, int j0, int first, int n, int n_all, int last_steps,
-                                               char *lds, Acc &acc)
+    // Works through the tiles of `walk`.  where(walk): its Work, with n >= 1; before(w): fetches what its results need from memory; finish(w, acc): hands the results on, out of the registers, and says
+    // whether it made STORES stores exactly.
+    //
+    // Stages of all tiles form one stream, of which the loads are two stages ahead of the products: a tile is finished while the
+    // first stages of the next one arrive.  Stores count like loads where a wavefront waits for its loads by number: behind a
+    // tile whose stores are known in number, the next stage is not waited for longer on their account.
+    template <int STORES, class Where, class Before, class Finish>
+    static __device__ __forceinline__ void work(const Operand &I, const Operand &J, Walk walk, char *lds, Where where, Before before, Finish finish)
     {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-            for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int64_t left_i = I.rows - i0, left_j = J.rows - j0;
-        const __amdgpu_buffer_rsrc_t ri = buffer_of((const char *)I.p + i0 * I.stride, (left_i - 1) * I.stride + I.row_bytes);
-        const __amdgpu_buffer_rsrc_t rj = buffer_of((const char *)J.p + j0 * J.stride, (left_j - 1) * J.stride + J.row_bytes);
-        Stager<TI, K::row_i, NW> gi;
-        Stager<TJ, K::row_j, NW> gj;
-        gi.init((int)min(left_i, (int64_t)TI), I.stride, wave, lane);
-        gj.init((int)min(left_j, (int64_t)TJ), J.stride, wave, lane);
-        ScaleStager<TI, K::scale_i, NW> hi;
-        ScaleStager<TJ, K::scale_j, NW> hj;
-        __amdgpu_buffer_rsrc_t rsi = ri, rsj = rj;
-        if constexpr (K::scale_i > 0) {
-            rsi = buffer_of(I.scales + (int64_t)i0 * I.scale_stride, left_i * I.scale_stride);
-            hi.init((int)min(left_i, (int64_t)TI), I.scale_stride, wave, lane);
-        }
-        if constexpr (K::scale_j > 0) {
-            rsj = buffer_of(J.scales + (int64_t)j0 * J.scale_stride, left_j * J.scale_stride);
-            hj.init((int)min(left_j, (int64_t)TJ), J.scale_stride, wave, lane);
-        }
-        // Load n of a stage's loads of either operand.  Behind the last stage: the last one again, into memory that nobody reads.
-        constexpr int loads_i = gi.per + hi.per, loads_j = gj.per + hj.per;
-        auto load_i = [&](int x, int s, char *to) {
-            const uint32_t at = (uint32_t)(first + min(s, n - 1));
-            if (x < gi.per) gi.issue_one(x, ri, to, at * K::row_i, wave);
-            else hi.issue_one(x - gi.per, rsi, to + oSI, at * K::scale_i, wave);
+        const int wave = Tile::wave(), lane = Tile::lane();
+        if (walk.left <= 0) return;
+        const Places places;
+        __amdgpu_buffer_rsrc_t ri, rj, rsi, rsj;
+        StagerI gi;
+        StagerJ gj;
+        ScalesI hi;
+        ScalesJ hj;
+        gi.init(I.stride, wave, lane);
+        gj.init(J.stride, wave, lane);
+        hi.init(I.scale_stride, wave, lane);
+        hj.init(J.scale_stride, wave, lane);
+        Work w = where(walk);                                    // the tile that is multiplied
+        Walk ahead_walk = walk;                                  // the tile that is loaded
+        int ahead = 0, ahead_n = 0;                              // the next stage to be loaded, and where its tile's stages end
+        auto stage = [&] {
+            gi.stage(ahead, I.row_bytes);
+            gj.stage(ahead, J.row_bytes);
+            hi.stage(ahead, I.scale_stride);
+            hj.stage(ahead, J.scale_stride);
         };
-        auto load_j = [&](int x, int s, char *to) {
-            const uint32_t at = (uint32_t)(first + min(s, n - 1));
-            if (x < gj.per) gj.issue_one(x, rj, to, at * K::row_j, wave);
-            else hj.issue_one(x - gj.per, rsj, to + oSJ, at * K::scale_j, wave);
+        auto load_from = [&](const Work &v) {
+            const int64_t left_i = I.rows - v.i0, left_j = J.rows - v.j0;
+            ri = buffer_of((const char *)I.p + v.i0 * I.stride, (left_i - 1) * I.stride + I.row_bytes);
+            rj = buffer_of((const char *)J.p + v.j0 * J.stride, (left_j - 1) * J.stride + J.row_bytes);
+            if constexpr (K::scale_i > 0) rsi = buffer_of(I.scales + (int64_t)v.i0 * I.scale_stride, left_i * I.scale_stride);
+            if constexpr (K::scale_j > 0) rsj = buffer_of(J.scales + (int64_t)v.j0 * J.scale_stride, left_j * J.scale_stride);
+            ahead = v.first;
+            ahead_n = v.first + v.n;
+            stage();
         };
-        char *const lj = lds + ring_i * bytes_i;
-        if (n > 0) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-#pragma unroll
-                for (int x = 0; x < loads_i; ++x) load_i(x, s, lds + s * bytes_i);
-#pragma unroll
-                for (int x = 0; x < loads_j; ++x) load_j(x, s, lj + s * bytes_j);
+        // Load x of either operand's part of stage `ahead`.  Behind the last tile: its last stage again, into memory that nobody reads.
+        auto load_i = [&](int x, char *to) {
+            if (x < gi.per) gi.issue(x, ri, to, ahead, I.stride, wave);
+            else hi.issue(x - gi.per, rsi, to + oSI, ahead, I.scale_stride, wave);
+        };
+        auto load_j = [&](int x, char *to) {
+            if (x < gj.per) gj.issue(x, rj, to, ahead, J.stride, wave);
+            else hj.issue(x - gj.per, rsj, to + oSJ, ahead, J.scale_stride, wave);
+        };
+        auto advance = [&] {
+            if (ahead + 1 < ahead_n) {
+                ++ahead;
+                stage();
+            } else if (ahead_walk.more()) {
+                ahead_walk.next();
+                load_from(where(ahead_walk));
             }
-            wait_loads_and_barrier<loads_i + loads_j>();
-        }
-        // places of I's stages s, s + 1, s + 2
-        char *i0p = lds, *i1p = lds + bytes_i, *i2p = ring_i == 3 ? lds + 2 * bytes_i : i0p;
-        if constexpr (K::steps == 1) {
-            for (int s = 0; s < n; ++s) {
-                char *now = lj + (s & 1) * bytes_j;
+        };
+        load_from(w);
+        // places of I's stages s, s + 1, s + 2, and of J's s, s + 1
+        char *i0p = lds, *i1p = lds + bytes_i, *i2p = ring_i == 3 ? lds + 2 * bytes_i : i0p, *j0p = lds + ring_i * bytes_i, *j1p = j0p + bytes_j;
 #pragma unroll
-                for (int x = 0; x < loads_i; ++x) load_i(x, s + 2, i2p);
-                compute_w(i0p, now, wi, wj, lane, acc);
-                wait_loads_and_barrier<loads_i>();
+        for (int x = 0; x < li; ++x) load_i(x, i0p);
 #pragma unroll
-                for (int x = 0; x < loads_j; ++x) load_j(x, s + 2, now);
-                char *t = i0p; i0p = i1p; i1p = i2p; i2p = t;
-            }
-        } else if (n > 0) {
-            // The operands of a step are read while the step before multiplies; the barrier that hands J's place on lies between the
-            // last reads of the stage and its last products.  Reads and loads are dealt out between the products: a wavefront that
-            // issues all its loads at once waits for the others' loads to be taken, with no product under way.
-            Frags f0, f1;
+        for (int x = 0; x < lj; ++x) load_j(x, j0p);
+        advance();
 #pragma unroll
-            for (int x = 0; x < reads; ++x) load_one(x, i0p, lj, 0, wi, wj, lane, f0);
-            for (int s = 0; s + 1 < n; ++s) {
-                char *now = lj + (s & 1) * bytes_j, *next = lj + ((s + 1) & 1) * bytes_j;
+        for (int x = 0; x < li; ++x) load_i(x, i1p);
+#pragma unroll
+        for (int x = 0; x < lj; ++x) load_j(x, j1p);
+        advance();
+        wait_loads_and_barrier<li + lj>();
+        Frags f;
+#pragma unroll
+        for (int x = 0; x < NJ; ++x) read_b(0, x, j0p, 0, places, f);
+#pragma unroll
+        for (int x = 0; x < MI; ++x) read_a(0, x, i0p, 0, places, f);
+        bool stores = false;                                     // STORES stores are younger than the loads that are waited for next
+        constexpr int steps = KIND == kTileMx4W ? 4 : K::steps, last = steps - 1;
+        constexpr int hold = KIND == kTileMx4W || MI < 4 ? 0 : 1;          // the row of blocks behind which a stage is handed on
+        static_assert(steps % 2 == 0, "a stage begins with J's first set of blocks");
+        for (;;) {
+            before(w);
+            Acc acc;
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // The blocks of a step are read while the step before multiplies, each block of I into the place of one that is done
+            // with.  Reads and loads are dealt out between the products: a wavefront that issues all its loads at once waits for the
+            // others' loads to be taken, with no product under way.  The barrier that hands J's place on lies behind the last reads
+            // of the stage, inside its last step.
+            auto early_steps = [&] {
+#pragma unroll
+                for (int t = 0; t < last; ++t) {
+#pragma unroll
+                    for (int mi = 0; mi < MI; ++mi) {
+                        constexpr int rows = last * MI, half = MI > 1 ? MI / 2 : 1;
+#pragma unroll
+                        for (int x = (t * MI + mi) * li / rows; x < (t * MI + mi + 1) * li / rows; ++x)
+                            if (ring_i == 3) load_i(x, i2p);
+                        // J's blocks within the first half: the next step begins with all of them
+#pragma unroll
+                        for (int x = mi * NJ / half; x < (mi + 1) * NJ / half && x < NJ; ++x) read_b((t + 1) & 1, x, j0p, t + 1, places, f);
+                        multiply_row(mi, 0, t & 1, t, f, acc);
+                        if constexpr (KIND != kTileMx4W) read_a(0, mi, i0p, t + 1, places, f);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            };
+            auto hand_on = [&] {
+                constexpr int young = ring_i == 3 ? li : 0;
+                if (STORES > 0 && stores) wait_loads_and_barrier<young + STORES>();
+                else wait_loads_and_barrier<young>();
+                stores = false;
+            };
+            auto last_step = [&] {
+                constexpr bool first = KIND == kTileMx4W;
+                if (first) hand_on();
 #pragma unroll
                 for (int mi = 0; mi < MI; ++mi) {
-                    constexpr int fast = MI > 1 ? (MI + 1) / 2 : 1;          // all reads in the first half: the barrier waits for them
+                    multiply_row(mi, 0, last & 1, last, f, acc);
+                    if (!first && mi == hold) hand_on();
+                    if (mi >= hold) {
+                        constexpr int rest = MI - hold, half = rest > 1 ? rest / 2 : 1;
 #pragma unroll
-                    for (int x = mi * loads_i / MI; x < (mi + 1) * loads_i / MI; ++x)
-                        if (ring_i == 3) load_i(x, s + 2, i2p);
+                        for (int x = (mi - hold) * lj / rest; x < (mi - hold + 1) * lj / rest; ++x) load_j(x, j0p);
 #pragma unroll
-                    for (int x = mi * reads / fast; x < (mi + 1) * reads / fast && x < reads; ++x) load_one(x, i0p, now, 1, wi, wj, lane, f1);
-                    multiply_row(mi, f0, lane, acc);
+                        for (int x = (mi - hold) * li / rest; x < (mi - hold + 1) * li / rest; ++x)
+                            if (ring_i == 2) load_i(x, i0p);
+#pragma unroll
+                        for (int x = (mi - hold) * NJ / half; x < (mi - hold + 1) * NJ / half && x < NJ; ++x) read_b(0, x, j1p, 0, places, f);
+#pragma unroll
+                        for (int x = mi == hold ? 0 : mi; x <= mi; ++x) read_a(first ? 1 : 0, x, i1p, 0, places, f);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                wait_loads_and_barrier<ring_i == 3 ? loads_i : 0>();
+                if constexpr (first) {
 #pragma unroll
-                for (int mi = 0; mi < MI; ++mi) {
-#pragma unroll
-                    for (int x = mi * loads_i / MI; x < (mi + 1) * loads_i / MI; ++x)
-                        if (ring_i == 2) load_i(x, s + 2, i0p);
-#pragma unroll
-                    for (int x = mi * loads_j / MI; x < (mi + 1) * loads_j / MI; ++x) load_j(x, s + 2, now);
-#pragma unroll
-                    for (int x = mi * reads / MI; x < (mi + 1) * reads / MI; ++x) load_one(x, i1p, next, 0, wi, wj, lane, f0);
-                    multiply_row(mi, f1, lane, acc);
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int x = 0; x < MI; ++x) { f.a[0][x] = f.a[1][x]; f.sa[0][x] = f.sa[1][x]; }
                 }
-                char *t = i0p; i0p = i1p; i1p = ring_i == 3 ? i2p : t; i2p = t;
+                advance();
+                char *p = i0p; i0p = i1p; i1p = ring_i == 3 ? i2p : p; i2p = p;
+                p = j0p; j0p = j1p; j1p = p;
+            };
+            for (int s = 0; s < w.n; ++s) {
+                early_steps();
+                last_step();
             }
-            const bool two = first + n < n_all || last_steps == 2;
-            if (two) {
-#pragma unroll
-                for (int x = 0; x < reads; ++x) load_one(x, i0p, lj + ((n - 1) & 1) * bytes_j, 1, wi, wj, lane, f1);
-            }
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi) multiply_row(mi, f0, lane, acc);
-            if (two) {
-#pragma unroll
-                for (int mi = 0; mi < MI; ++mi) multiply_row(mi, f1, lane, acc);
-            }
+            stores = finish(w, acc);
+            if (!walk.more()) break;
+            walk.next();
+            w = where(walk);
         }
-        wait_loads_and_barrier<0>();
-        __syncthreads();
+        wait_loads_and_barrier<0>();                             // no load into LDS outlives the workgroup
     }
 };
 
-// Workgroup -> tile.  Consecutive workgroups go to the eight dies in turn, each with an L2 of its own: die x gets a run of
-// tiles, and a run walks blocks of `band` I tiles by all J tiles, I fastest, so that the workgroups a die has at a time
-// share both operands.
-struct TileAt { int i, j; };
-__device__ __forceinline__ TileAt tile_at(int bid, int ni, int nj, int band)
-{
-    const int n = ni * nj, x = bid & 7, q = n >> 3, r = n & 7;
-    const int at = x * q + min(x, r) + (bid >> 3);
-    const int per = band * nj, b = at / per, in = at - b * per, h = min(band, ni - b * band);
-    return TileAt{b * band + in % h, in / h};
-}
+constexpr int kCUs = 256;
+// Workgroups of a launch: as many as are resident at once.
+template <class T> inline int grid_of(int64_t tiles) { return (int)(tiles < (int64_t)kCUs * T::per_cu ? tiles : (int64_t)kCUs * T::per_cu); }
 
 }  // namespace tapout

@@ -14,6 +14,13 @@ namespace {
 template <int DT> struct ElemOf { using T = float; };
 template <> struct ElemOf<TAPOUT_BF16> { using T = __bf16; };
 
+// Eight neighbouring results.
+__device__ __forceinline__ void store8(float *to, f32x4 a, f32x4 b) { ((f32x4 *)to)[0] = a; ((f32x4 *)to)[1] = b; }
+__device__ __forceinline__ void store8(__bf16 *to, f32x4 a, f32x4 b)
+{
+    *(bf16x8 *)to = bf16x8{(__bf16)a[0], (__bf16)a[1], (__bf16)a[2], (__bf16)a[3], (__bf16)b[0], (__bf16)b[1], (__bf16)b[2], (__bf16)b[3]};
+}
+
 __device__ __forceinline__ bool row_counts(int t, int V, const float *lse, const float *row_weight, int n)
 {
     if (counted_target(t, V) < 0) return false;
@@ -22,65 +29,63 @@ __device__ __forceinline__ bool row_counts(int t, int V, const float *lse, const
 }
 
 // ---- forward -----------------------------------------------------------------------------------------
+// Every wavefront leaves the maximum and sum of its own MI * 16 vocabulary rows for each of its tokens.
 template <class T>
-__global__ __launch_bounds__(T::threads) void head_loss_kernel(LossArgs a, int ni, int nj, int stages, int last_steps)
+__global__ __launch_bounds__(T::threads) void head_loss_kernel(LossArgs a, int ni, int nj, int stages)
 {
     extern __shared__ __align__(16) char lds[];
-    const TileAt at = tile_at(blockIdx.x, ni, nj, 8);
-    const int i0 = at.i * T::TI, j0 = at.j * T::TJ;
     if (blockIdx.x == 0 && a.flags)
         for (int b = threadIdx.x; b < a.B; b += T::threads) a.flags[b] = 0;
-    typename T::Acc acc;
-    T::run(a.weight, a.hidden, i0, j0, 0, stages, stages, last_steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / T::WJ, wj = wave % T::WJ;
-    const int r16 = lane & 15, g = lane >> 4;
-    const int iw = i0 + wi * T::MI * 16 + 4 * g, jw = wj * T::NJ * 16 + r16;
-    float2 *red = (float2 *)lds;                       // [WI][TJ]
+    int target[T::NJ];
+    T::template work<0>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
+        [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, 0, stages}; },
+        [&](const Work &w) {
 #pragma unroll
-    for (int nj = 0; nj < T::NJ; ++nj) {
-        const int j = j0 + jw + nj * 16;
-        float m = -INFINITY;
+            for (int n = 0; n < T::NJ; ++n) {
+                const int j = w.j0 + T::j_of(n);
+                target[n] = j < a.N ? a.target[j] : -1;
+            }
+        },
+        [&](const Work &w, typename T::Acc &acc) {
+            const int left = a.V - w.i0;
 #pragma unroll
-        for (int mi = 0; mi < T::MI; ++mi)
+            for (int n = 0; n < T::NJ; ++n) {
+                const int j = w.j0 + T::j_of(n);
+                if (left < T::TI) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (iw + mi * 16 + r < a.V) m = fmaxf(m, acc[mi][nj][r]);
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        const float ref = m == -INFINITY ? 0.f : m;
-        float s = 0.f;
+                    for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
-        for (int mi = 0; mi < T::MI; ++mi)
+                        for (int r = 0; r < 4; ++r)
+                            if (T::i_of(mi) + r >= left) acc[mi][n][r] = -INFINITY;
+                }
+                float m = -INFINITY;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (iw + mi * 16 + r < a.V) s += __builtin_amdgcn_exp2f((acc[mi][nj][r] - ref) * kLog2e);
-        s += __shfl_xor(s, 16);
-        s += __shfl_xor(s, 32);
-        if (g == 0) red[wi * T::TJ + jw + nj * 16] = float2{m, s};
-        const int t = j < a.N ? a.target[j] : -1;
-        if (t >= 0 && t < a.V) {
-            const int d = t - iw;
+                for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
-            for (int mi = 0; mi < T::MI; ++mi)
+                    for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[mi][n][r]);
+                m = fmaxf(m, __shfl_xor(m, 16));
+                m = fmaxf(m, __shfl_xor(m, 32));
+                const float ref = m == -INFINITY ? 0.f : m;
+                float s = 0.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (d == mi * 16 + r) a.target_logit[j] = acc[mi][nj][r];
-        }
-    }
-    __syncthreads();
-    for (int x = threadIdx.x; x < T::TJ; x += T::threads) {
-        if (j0 + x >= a.N) continue;
-        float m = -INFINITY, s = 0.f;
+                for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
-        for (int w = 0; w < T::WI; ++w) m = fmaxf(m, red[w * T::TJ + x].x);
-        const float ref = m == -INFINITY ? 0.f : m;
+                    for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f((acc[mi][n][r] - ref) * kLog2e);
+                s += __shfl_xor(s, 16);
+                s += __shfl_xor(s, 32);
+                if (j >= a.N) continue;
+                if (T::lane() < 16) a.part[((int64_t)j * ni + w.i0 / T::TI) * T::WI + T::wave() / T::WJ] = float2{m, s};
+                const int d = target[n] - w.i0;
+                if (d >= 0 && d < min(left, T::TI)) {
 #pragma unroll
-        for (int w = 0; w < T::WI; ++w) {
-            const float2 p = red[w * T::TJ + x];
-            s += p.y * __builtin_amdgcn_exp2f(((p.x == -INFINITY ? 0.f : p.x) - ref) * kLog2e);
-        }
-        a.part[(int64_t)(j0 + x) * ni + at.i] = float2{m, s};
-    }
+                    for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (d == T::i_of(mi) + r) a.target_logit[j] = acc[mi][n][r];
+                }
+            }
+            return false;
+        });
 }
 
 // A wavefront a row: the tiles' maxima and sums to lse, in double.
@@ -114,58 +119,54 @@ __global__ __launch_bounds__(256) void head_loss_join_kernel(LossArgs a, int ni)
 
 // ---- gradient by the logits of one piece ---------------------------------------------------------------
 template <class T, class E>
-__global__ __launch_bounds__(T::threads) void head_grad_kernel(GradArgs a, int ni, int nj, int stages, int last_steps, int n_pad, int N_pad)
+__global__ __launch_bounds__(T::threads) void head_grad_kernel(GradArgs a, int ni, int nj, int stages, int n_pad, int N_pad)
 {
     extern __shared__ __align__(16) char lds[];
-    constexpr int V16 = 16 / sizeof(E), LI = T::TI + V16, LJ = T::TJ + V16;      // row lengths of the two tiles in LDS
-    const TileAt at = tile_at(blockIdx.x, ni, nj, 8);
-    const int i0 = at.i * T::TI, j0 = at.j * T::TJ;
-    typename T::Acc acc;
-    T::run(a.weight, a.hidden, i0, j0, 0, stages, stages, last_steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / T::WJ, wj = wave % T::WJ;
-    const int r16 = lane & 15, g = lane >> 4;
-    const int il = wi * T::MI * 16 + 4 * g, jl = wj * T::NJ * 16 + r16;
-    E *tile = (E *)lds;
+    int target[T::NJ];                                        // -1: the row does not count
+    float lse[T::NJ], weight[T::NJ];
+    T::template work<0>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
+        [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, 0, stages}; },
+        [&](const Work &w) {
 #pragma unroll
-    for (int nj = 0; nj < T::NJ; ++nj) {
-        const int j = j0 + jl + nj * 16;
-        const int t = j < a.N ? a.target[j] : -1;
-        const bool live = j < a.N && row_counts(t, a.V, a.lse, a.row_weight, j);
-        const float lse = live ? a.lse[j] : 0.f, w = live && a.row_weight ? a.row_weight[j] : 1.f;
-        const int d = t - a.v0 - i0 - il;
-#pragma unroll
-        for (int mi = 0; mi < T::MI; ++mi) {
-            E v[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float p = __builtin_amdgcn_exp2f((acc[mi][nj][r] - lse) * kLog2e);
-                p = (p - (d == mi * 16 + r ? 1.f : 0.f)) * w;
-                p = live && i0 + il + mi * 16 + r < a.n ? p : 0.f;
-                v[r] = (E)p;                              // to nearest: the matrix instructions take operands of one type
-                acc[mi][nj][r] = p;
+            for (int n = 0; n < T::NJ; ++n) {
+                const int j = w.j0 + T::j_of(n);
+                target[n] = j < a.N ? a.target[j] : -1;
+                lse[n] = j < a.N ? a.lse[j] : 0.f;
+                weight[n] = j < a.N && a.row_weight ? a.row_weight[j] : 1.f;
             }
-            E *to = tile + (jl + nj * 16) * LI + il + mi * 16;
-            to[0] = v[0]; to[1] = v[1]; to[2] = v[2]; to[3] = v[3];
-        }
-    }
-    __syncthreads();
-    constexpr int CI = T::TI / V16, CJ = T::TJ / V16;
-    for (int x = threadIdx.x; x < T::TJ * CI; x += T::threads) {
-        const int jr = x / CI, c = x % CI * V16;
-        if (j0 + jr < a.N && i0 + c < n_pad) *(u32x4 *)((E *)a.g + (int64_t)(j0 + jr) * a.g_stride + i0 + c) = *(const u32x4 *)(tile + jr * LI + c);
-    }
-    __syncthreads();
+        },
+        [&](const Work &w, typename T::Acc &acc) {
 #pragma unroll
-    for (int nj = 0; nj < T::NJ; ++nj)
+            for (int n = 0; n < T::NJ; ++n) {
+                const int j = w.j0 + T::j_of(n);
+                const bool live = counted_target(target[n], a.V) >= 0 && fabsf(lse[n]) < INFINITY && weight[n] != 0.f;
+                const int hot = target[n] - a.v0 - w.i0, end = live ? a.n - w.i0 : 0;
 #pragma unroll
-        for (int mi = 0; mi < T::MI; ++mi)
+                for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) tile[(il + mi * 16 + r) * LJ + jl + nj * 16] = (E)acc[mi][nj][r];
-    __syncthreads();
-    for (int x = threadIdx.x; x < T::TI * CJ; x += T::threads) {
-        const int ir = x / CJ, c = x % CJ * V16;
-        if (i0 + ir < a.n && j0 + c < N_pad) *(u32x4 *)((E *)a.gt + (int64_t)(i0 + ir) * a.gt_stride + j0 + c) = *(const u32x4 *)(tile + ir * LJ + c);
-    }
+                    for (int r = 0; r < 4; ++r) {
+                        const int i = T::i_of(mi) + r;
+                        const float p = __builtin_amdgcn_exp2f((acc[mi][n][r] - lse[n]) * kLog2e) - (i == hot ? 1.f : 0.f);
+                        acc[mi][n][r] = i < end ? p * weight[n] : 0.f;
+                    }
+                // to nearest in the operands' type: the matrix instructions take both factors in one type
+#pragma unroll
+                for (int mi = 0; mi < T::MI; mi += 2)
+                    if (j < a.N && w.i0 + T::i_of(mi) < n_pad) store8((E *)a.g + (int64_t)j * a.g_stride + w.i0 + T::i_of(mi), acc[mi][n], acc[mi + 1][n]);
+            }
+#pragma unroll
+            for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = w.i0 + T::i_of(mi) + r, j = w.j0 + T::j_of(0);
+                    if (i >= a.n || j >= N_pad) continue;
+                    struct __align__(T::NJ * sizeof(E)) { E v[T::NJ]; } q;
+#pragma unroll
+                    for (int n = 0; n < T::NJ; ++n) q.v[n] = (E)acc[mi][n][r];
+                    *(decltype(q) *)((E *)a.gt + (int64_t)i * a.gt_stride + j) = q;
+                }
+            return false;
+        });
 }
 
 template <class E>
@@ -198,38 +199,33 @@ __global__ __launch_bounds__(256) void head_transpose_kernel(TransposeArgs a)
 
 // ---- products of the gradient ---------------------------------------------------------------------------
 template <class T, class E>
-__global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int last_steps, int per_split)
+__global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int per_split, int splits)
 {
     extern __shared__ __align__(16) char lds[];
-    const TileAt at = tile_at(blockIdx.x, ni, nj, 8);
-    const int i0 = at.i * T::TI, j0 = at.j * T::TJ, split = blockIdx.y;
-    const int first = split * per_split, n = max(0, min(per_split, stages - first));
-    typename T::Acc acc;
-    T::run(a.I, a.J, i0, j0, first, n, stages, last_steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / T::WJ, wj = wave % T::WJ;
-    const int iw = i0 + wi * T::MI * 16 + 4 * (lane >> 4), jw = j0 + wj * T::NJ * 16 + (lane & 15);
     const float scale = a.part || !a.scale ? 1.f : *a.scale;
+    T::template work<0>(a.I, a.J, Walk(ni, nj, splits), lds,
+        [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, t.split * per_split, min(per_split, stages - t.split * per_split)}; },
+        [&](const Work &) {},
+        [&](const Work &w, typename T::Acc &acc) {
 #pragma unroll
-    for (int nj = 0; nj < T::NJ; ++nj) {
-        const int j = jw + nj * 16;
-        if (j >= a.nj) continue;
+            for (int n = 0; n < T::NJ; ++n) {
+                const int j = w.j0 + T::j_of(n);
+                if (j >= a.nj) continue;
 #pragma unroll
-        for (int mi = 0; mi < T::MI; ++mi) {
-            const int i = iw + mi * 16;
-            if (i >= a.ni) continue;
-            if (a.part) {
-                f32x4 *to = (f32x4 *)(a.part + ((int64_t)split * a.nj + j) * a.ni + i);
-                *to = a.first ? acc[mi][nj] : *to + acc[mi][nj];
-            } else {
-                E v[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = (E)(acc[mi][nj][r] * scale);
-                E *to = (E *)a.out + (int64_t)j * a.out_stride + i;
-                if constexpr (sizeof(E) == 4) *(u32x4 *)to = *(const u32x4 *)v;
-                else *(uint2 *)to = *(const uint2 *)v;
+                for (int mi = 0; mi < T::MI; mi += 2) {
+                    const int i = w.i0 + T::i_of(mi);
+                    if (i >= a.ni) continue;
+                    if (a.part) {
+                        f32x4 *to = (f32x4 *)(a.part + ((int64_t)(w.first / per_split) * a.nj + j) * a.ni + i);
+                        to[0] = a.first ? acc[mi][n] : to[0] + acc[mi][n];
+                        to[1] = a.first ? acc[mi + 1][n] : to[1] + acc[mi + 1][n];
+                    } else {
+                        store8((E *)a.out + (int64_t)j * a.out_stride + i, acc[mi][n] * scale, acc[mi + 1][n] * scale);
+                    }
+                }
             }
-        }
-    }
+            return false;
+        });
 }
 
 template <class E>
@@ -257,12 +253,9 @@ __global__ __launch_bounds__(256) void head_pack_kernel(PackArgs a)
 {
     constexpr int V16 = 16 / sizeof(E);
     const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int per = a.cols_pad / V16;
+    const int per = a.cols / V16;
     const int n = (int)(x / per), c = (int)(x % per) * V16;
-    if (n >= a.N) return;
-    u32x4 v = {0, 0, 0, 0};
-    if (c < a.cols) v = *(const u32x4 *)((const E *)a.src + (n / a.K) * a.stride_b + (n % a.K) * a.stride_k + c);
-    *(u32x4 *)((E *)a.dst + (int64_t)n * a.cols_pad + c) = v;
+    if (n < a.N) *(u32x4 *)((E *)a.dst + (int64_t)n * a.cols + c) = *(const u32x4 *)((const E *)a.src + (n / a.K) * a.stride_b + (n % a.K) * a.stride_k + c);
 }
 
 template <class T, class F> hipError_t with_lds(const void *kernel, int bytes, F launch)
@@ -280,44 +273,40 @@ inline int up(int a, int b) { return (a + b - 1) / b; }
 template <class T> hipError_t loss_with(const LossArgs &a, hipStream_t st)
 {
     using K = Kind<T::kind>;
-    const int ni = up(a.V, T::TI), nj = up(a.N, T::TJ), steps = a.D / K::step_elems, stages = up(steps, K::steps);
-    hipError_t e = with_lds<T>((const void *)head_loss_kernel<T>, T::lds_bytes, [&] {
-        head_loss_kernel<T><<<ni * nj, T::threads, T::lds_bytes, st>>>(a, ni, nj, stages, steps - (stages - 1) * K::steps);
+    static_assert(T::TI / T::WI >= (T::TJ > 32 ? 64 : 32), "part has room for as many blocks");
+    const int ni = up(a.V, T::TI), nj = up(a.N, T::TJ), stages = up(a.D, K::elems);
+    hipError_t e = with_lds<T>((const void *)head_loss_kernel<T>, T::ring_bytes, [&] {
+        head_loss_kernel<T><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
     });
     if (e != hipSuccess) return e;
-    head_loss_join_kernel<<<up(a.N, 4), 256, 0, st>>>(a, ni);
+    head_loss_join_kernel<<<up(a.N, 4), 256, 0, st>>>(a, ni * T::WI);
     return hipGetLastError();
 }
 
 template <class T, class E> hipError_t grad_with(const GradArgs &a, hipStream_t st)
 {
     using K = Kind<T::kind>;
-    constexpr int V16 = 16 / sizeof(E);
-    constexpr int t1 = T::TJ * (T::TI + V16) * (int)sizeof(E), t2 = T::TI * (T::TJ + V16) * (int)sizeof(E), tiles = t1 > t2 ? t1 : t2;
-    constexpr int lds = T::lds_bytes > tiles ? T::lds_bytes : tiles;
     const int n_pad = up(a.n, 64) * 64, N_pad = up(a.N, 32) * 32;
-    const int ni = up(n_pad, T::TI), nj = up(N_pad, T::TJ), steps = a.D / K::step_elems, stages = up(steps, K::steps);
-    return with_lds<T>((const void *)head_grad_kernel<T, E>, lds, [&] {
-        head_grad_kernel<T, E><<<ni * nj, T::threads, lds, st>>>(a, ni, nj, stages, steps - (stages - 1) * K::steps, n_pad, N_pad);
+    const int ni = up(n_pad, T::TI), nj = up(N_pad, T::TJ), stages = up(a.D, K::elems);
+    return with_lds<T>((const void *)head_grad_kernel<T, E>, T::ring_bytes, [&] {
+        head_grad_kernel<T, E><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages, n_pad, N_pad);
     });
 }
 
 template <class T, class E> hipError_t product_with(const ProductArgs &a, hipStream_t st)
 {
     using K = Kind<T::kind>;
-    const int ni = up(a.ni, T::TI), nj = up(a.nj, T::TJ), steps = a.k / K::step_elems, stages = up(steps, K::steps);
-    return with_lds<T>((const void *)head_product_kernel<T, E>, T::lds_bytes, [&] {
-        head_product_kernel<T, E><<<dim3(ni * nj, a.splits), T::threads, T::lds_bytes, st>>>(a, ni, nj, stages, steps - (stages - 1) * K::steps,
-                                                                                             up(stages, a.splits));
+    const int ni = up(a.ni, T::TI), nj = up(a.nj, T::TJ), stages = up(a.k, K::elems);
+    const int per_split = up(stages, a.splits), splits = up(stages, per_split);
+    return with_lds<T>((const void *)head_product_kernel<T, E>, T::ring_bytes, [&] {
+        head_product_kernel<T, E><<<grid_of<T>((int64_t)ni * nj * splits), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages,
+                                                                                             per_split, splits);
     });
 }
 
 template <int KIND> using Small = Tile<KIND, 128, 32, 4, 1>;
 template <int KIND> using Mid = Tile<KIND, 128, 128, 2, 2>;
-#ifndef LARGE
-#define LARGE 256, 256, 2, 4
-#endif
-template <int KIND> using Large = Tile<KIND, LARGE>;
+template <int KIND> using Large = Tile<KIND, 256, 256, 2, 4>;
 
 }  // namespace
 
@@ -366,7 +355,7 @@ hipError_t launch_head_grad_hidden(const GradHiddenArgs &a, int dtype, hipStream
 
 hipError_t launch_head_pack(const PackArgs &a, int dtype, hipStream_t st)
 {
-    const int64_t grid = ((int64_t)a.N * (a.cols_pad / (dtype == TAPOUT_F32 ? 4 : 8)) + 255) / 256;
+    const int64_t grid = ((int64_t)a.N * (a.cols / (dtype == TAPOUT_F32 ? 4 : 8)) + 255) / 256;
     if (dtype == TAPOUT_F32) head_pack_kernel<float><<<grid, 256, 0, st>>>(a);
     else head_pack_kernel<__bf16><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();

@@ -65,88 +65,61 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(DequantArgs a, int 
 }
 
 // ---- logits -----------------------------------------------------------------------------------------------
+// Eight neighbouring logits at any element-aligned address: the memory unit takes 16-byte stores there.
+__device__ __forceinline__ void store8(float *to, f32x4 a, f32x4 b)
+{
+    struct __attribute__((packed, aligned(4))) Any { f32x4 v; };
+    ((Any *)to)[0].v = a;
+    ((Any *)to)[1].v = b;
+}
+__device__ __forceinline__ void store8(__bf16 *to, f32x4 a, f32x4 b)
+{
+    struct __attribute__((packed, aligned(2))) Any { bf16x8 v; };
+    ((Any *)to)->v = bf16x8{(__bf16)a[0], (__bf16)a[1], (__bf16)a[2], (__bf16)a[3], (__bf16)b[0], (__bf16)b[1], (__bf16)b[2], (__bf16)b[3]};
+}
+
 template <class T, class E>
-__global__ __launch_bounds__(T::threads) void head_logits_kernel(LogitsArgs a, int ni, int nj, int stages, int last_steps)
+__global__ __launch_bounds__(T::threads) void head_logits_kernel(LogitsArgs a, int ni, int nj, int stages)
 {
     extern __shared__ __align__(16) char lds[];
-    const TileAt at = tile_at(blockIdx.x, ni, nj, 8);
-    const int i0 = at.i * T::TI, j0 = at.j * T::TJ;
-    typename T::Acc acc;
-    T::run(a.weight, a.hidden, i0, j0, 0, stages, stages, last_steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / T::WJ, wj = wave % T::WJ;
-    const int il = wi * T::MI * 16 + 4 * (lane >> 4), jl = wj * T::NJ * 16 + (lane & 15);
-    auto row_of = [&](int j) -> E * {                  // NULL: not written
-        if (j >= a.N) return nullptr;
-        const int b = j / a.K, k = j % a.K;
-        if (a.k_len && k >= a.k_len[b]) return nullptr;
-        return (E *)a.out + b * a.stride_b + k * a.stride_k;
-    };
-    if constexpr (sizeof(E) == 4) {
-        // four neighbours a lane
+    E *row[T::NJ];                                            // NULL: not written
+    T::template work<T::MI * T::NJ * (int)sizeof(E) / 4>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
+        [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, 0, stages}; },
+        [&](const Work &) {},
+        [&](const Work &w, typename T::Acc &acc) {
 #pragma unroll
-        for (int nj = 0; nj < T::NJ; ++nj) {
-            E *row = row_of(j0 + jl + nj * 16);
-            if (!row) continue;
+            for (int n = 0; n < T::NJ; ++n) {
+                const int j = w.j0 + T::j_of(n), b = j / a.K, k = j - b * a.K;
+                row[n] = j < a.N && (!a.k_len || k < a.k_len[b]) ? (E *)a.out + b * a.stride_b + k * a.stride_k + w.i0 : nullptr;
+            }
+            const int left = a.V - w.i0;
 #pragma unroll
-            for (int mi = 0; mi < T::MI; ++mi) {
-                const int i = i0 + il + mi * 16;
-                if (i + 4 <= a.V && ((uintptr_t)(row + i) & 15) == 0) *(f32x4 *)(row + i) = acc[mi][nj];
-                else {
+            for (int n = 0; n < T::NJ; ++n) {
+                if (!row[n]) continue;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (i + r < a.V) row[i + r] = acc[mi][nj][r];
+                for (int mi = 0; mi < T::MI; mi += 2) {
+                    const int i = T::i_of(mi);
+                    if (i + 8 <= left) store8(row[n] + i, acc[mi][n], acc[mi + 1][n]);
+                    else {
+#pragma unroll
+                        for (int r = 0; r < 8; ++r)
+                            if (i + r < left) row[n][i + r] = (E)acc[mi + r / 4][n][r % 4];
+                    }
                 }
             }
-        }
-    } else {
-        // through LDS, so that a row of the tile leaves in whole 16-byte pieces; where the row starts between them, the pieces
-        // are taken from LDS element by element
-        constexpr int L = T::TI + 8, C = T::TI / 8 + 1;
-        E *tile = (E *)lds;
-#pragma unroll
-        for (int nj = 0; nj < T::NJ; ++nj)
-#pragma unroll
-            for (int mi = 0; mi < T::MI; ++mi) {
-                const bf16x4 v = {(__bf16)acc[mi][nj][0], (__bf16)acc[mi][nj][1], (__bf16)acc[mi][nj][2], (__bf16)acc[mi][nj][3]};
-                *(uint2 *)(tile + (jl + nj * 16) * L + il + mi * 16) = __builtin_bit_cast(uint2, v);
-            }
-        __syncthreads();
-        const int n = min(T::TI, a.V - i0);
-        for (int x = threadIdx.x; x < T::TJ * C; x += T::threads) {
-            const int jr = x / C;
-            E *row = row_of(j0 + jr);
-            if (!row) continue;
-            E *to = row + i0;
-            const int mis = (int)(((uintptr_t)to >> 1) & 7), e = (x % C) * 8 - mis;
-            const E *from = tile + jr * L;
-            if (e >= 0 && e + 8 <= n) {
-                u32x4 v;
-                if (mis == 0) v = *(const u32x4 *)(from + e);
-                else {
-                    const uint16_t *h = (const uint16_t *)from + e;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] = (uint32_t)h[2 * q] | (uint32_t)h[2 * q + 1] << 16;
-                }
-                *(u32x4 *)(to + e) = v;
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (e + q >= 0 && e + q < n) to[e + q] = from[e + q];
-            }
-        }
-    }
+            return left >= T::TI && w.j0 + T::TJ <= a.N && !a.k_len;
+        });
 }
 
 template <class T, class E> hipError_t logits_with(const LogitsArgs &a, hipStream_t st)
 {
     using K = Kind<T::kind>;
-    constexpr int tile = sizeof(E) == 2 ? T::TJ * (T::TI + 8) * 2 : 0, lds = T::lds_bytes > tile ? T::lds_bytes : tile;
-    const int ni = up(a.V, T::TI), nj = up(a.N, T::TJ), steps = a.D / K::step_elems, stages = up(steps, K::steps);
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute((const void *)head_logits_kernel<T, E>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const int ni = up(a.V, T::TI), nj = up(a.N, T::TJ), stages = up(a.D, K::elems);
+    if (T::ring_bytes > 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void *)head_logits_kernel<T, E>, hipFuncAttributeMaxDynamicSharedMemorySize, T::ring_bytes);
         if (e != hipSuccess) return e;
     }
-    head_logits_kernel<T, E><<<ni * nj, T::threads, lds, st>>>(a, ni, nj, stages, steps - (stages - 1) * K::steps);
+    head_logits_kernel<T, E><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
     return hipGetLastError();
 }
 
@@ -154,7 +127,7 @@ template <class E> hipError_t logits_of(const LogitsArgs &a, int kind, hipStream
 {
     if (kind == kTileMx4)
         return a.N <= 32 ? logits_with<Tile<kTileMx4, 128, 32, 4, 1>, E>(a, st)
-             : logits_with<Tile<kTileMx4, 128, 128, 2, 2>, E>(a, st);
+             : a.N <= 256 ? logits_with<Tile<kTileMx4, 128, 128, 2, 2>, E>(a, st) : logits_with<Tile<kTileMx4, 256, 128, 4, 2>, E>(a, st);
     return a.N <= 32 ? logits_with<Tile<kTileMx4W, 128, 32, 4, 1>, E>(a, st)
          : a.N <= 64 ? logits_with<Tile<kTileMx4W, 128, 64, 4, 1>, E>(a, st) : logits_with<Tile<kTileMx4W, 128, 128, 2, 2>, E>(a, st);
 }
