@@ -144,6 +144,15 @@ template <int N> __device__ __forceinline__ void wait_loads_and_barrier()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// The same with one of two numbers.  The branch is inside, where the compiler does not see it: it would move the products behind it.
+template <int N0, int N1> __device__ __forceinline__ void wait_loads_and_barrier(int which)
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_cmp_eq_u32 %0, 0\n\ts_cbranch_scc1 .Lfirst%=\n\ts_waitcnt vmcnt(%2) lgkmcnt(0)\n\ts_branch .Lboth%=\n.Lfirst%=:\n\t"
+                 "s_waitcnt vmcnt(%1) lgkmcnt(0)\n.Lboth%=:\n\ts_barrier" ::"s"(which), "n"(N0), "n"(N1) : "memory", "scc");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // A workgroup's way through ni x nj tiles by `splits` runs of k.  Consecutive workgroups go to the eight dies in turn, each with an
 // L2 of its own: die x gets a run of tiles, of which its workgroups take every S-th, and a run walks bands of eight rows of
 // tiles (at the end four, two, one) by all J tiles, I fastest, so that the workgroups of a die share both operands at any
@@ -258,6 +267,11 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
             else if constexpr (KIND == kTileMx4) acc[mi][nj] = mma_mx4(a, f.sa[set_a][mi], f.b[set_b][nj], f.sb[set_b][nj], acc[mi][nj]);
             else acc[mi][nj] = mma_bf16(a, f.b[set_b][nj], acc[mi][nj]);
         }
+        // here and not where the sums are next used, to which the compiler would move the scaled products, past the loads and the barrier
+        if constexpr (KIND == kTileMx4) {
+#pragma unroll
+            for (int nj = 0; nj < NJ; ++nj) asm volatile("" : "+v"(acc[mi][nj]));
+        }
     }
 
     // Works through the tiles of `walk`.  where(walk): its Work, with n >= 1; before(w): fetches what its results need from memory; finish(w, acc): hands the results on, out of the registers, and says
@@ -337,7 +351,7 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
         for (int x = 0; x < NJ; ++x) read_b(0, x, j0p, 0, places, f);
 #pragma unroll
         for (int x = 0; x < MI; ++x) read_a(0, x, i0p, 0, places, f);
-        bool stores = false;                                     // STORES stores are younger than the loads that are waited for next
+        int stores = 0;                                          // 1: STORES stores are younger than the loads that are waited for next
         constexpr int steps = KIND == kTileMx4W ? 4 : K::steps, last = steps - 1;
         constexpr int hold = KIND == kTileMx4W || MI < 4 ? 0 : 1;          // the row of blocks behind which a stage is handed on
         static_assert(steps % 2 == 0, "a stage begins with J's first set of blocks");
@@ -372,9 +386,12 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
             };
             auto hand_on = [&] {
                 constexpr int young = ring_i == 3 ? li : 0;
-                if (STORES > 0 && stores) wait_loads_and_barrier<young + STORES>();
-                else wait_loads_and_barrier<young>();
-                stores = false;
+                if constexpr (STORES > 0) {
+                    wait_loads_and_barrier<young, young + STORES>(__builtin_amdgcn_readfirstlane(stores));
+                    stores = 0;
+                } else {
+                    wait_loads_and_barrier<young>();
+                }
             };
             auto last_step = [&] {
                 constexpr bool first = KIND == kTileMx4W;

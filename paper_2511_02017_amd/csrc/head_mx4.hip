@@ -82,30 +82,33 @@ template <class T, class E>
 __global__ __launch_bounds__(T::threads) void head_logits_kernel(LogitsArgs a, int ni, int nj, int stages)
 {
     extern __shared__ __align__(16) char lds[];
-    E *row[T::NJ];                                            // NULL: not written
+    const float k_inverse = 1.f / (float)a.K;
     T::template work<T::MI * T::NJ * (int)sizeof(E) / 4>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
         [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, 0, stages}; },
         [&](const Work &) {},
         [&](const Work &w, typename T::Acc &acc) {
-#pragma unroll
-            for (int n = 0; n < T::NJ; ++n) {
-                const int j = w.j0 + T::j_of(n), b = j / a.K, k = j - b * a.K;
-                row[n] = j < a.N && (!a.k_len || k < a.k_len[b]) ? (E *)a.out + b * a.stride_b + k * a.stride_k + w.i0 : nullptr;
-            }
             const int left = a.V - w.i0;
 #pragma unroll
             for (int n = 0; n < T::NJ; ++n) {
-                if (!row[n]) continue;
+                // j / K of at most 2^20 rows: the quotient in binary32 is off by less than one
+                const int j = w.j0 + T::j_of(n);
+                int b = (int)((float)j * k_inverse), k = j - b * a.K;
+                if (k < 0) { --b; k += a.K; }
+                if (k >= a.K) { ++b; k -= a.K; }
+                if (j < a.N && (!a.k_len || k < a.k_len[b])) {
+                    E *row = (E *)a.out + b * a.stride_b + k * a.stride_k + w.i0;
 #pragma unroll
-                for (int mi = 0; mi < T::MI; mi += 2) {
-                    const int i = T::i_of(mi);
-                    if (i + 8 <= left) store8(row[n] + i, acc[mi][n], acc[mi + 1][n]);
-                    else {
+                    for (int mi = 0; mi < T::MI; mi += 2) {
+                        const int i = T::i_of(mi);
+                        if (i + 8 <= left) store8(row + i, acc[mi][n], acc[mi + 1][n]);
+                        else {
 #pragma unroll
-                        for (int r = 0; r < 8; ++r)
-                            if (i + r < left) row[n][i + r] = (E)acc[mi + r / 4][n][r % 4];
+                            for (int r = 0; r < 8; ++r)
+                                if (i + r < left) row[i + r] = (E)acc[mi + r / 4][n][r % 4];
+                        }
                     }
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
             return left >= T::TI && w.j0 + T::TJ <= a.N && !a.k_len;
         });
@@ -127,7 +130,7 @@ template <class E> hipError_t logits_of(const LogitsArgs &a, int kind, hipStream
 {
     if (kind == kTileMx4)
         return a.N <= 32 ? logits_with<Tile<kTileMx4, 128, 32, 4, 1>, E>(a, st)
-             : a.N <= 256 ? logits_with<Tile<kTileMx4, 128, 128, 2, 2>, E>(a, st) : logits_with<Tile<kTileMx4, 256, 128, 4, 2>, E>(a, st);
+             : a.N <= 256 ? logits_with<Tile<kTileMx4, 128, 128, 2, 2>, E>(a, st) : logits_with<Tile<kTileMx4, 256, 256, 2, 4>, E>(a, st);
     return a.N <= 32 ? logits_with<Tile<kTileMx4W, 128, 32, 4, 1>, E>(a, st)
          : a.N <= 64 ? logits_with<Tile<kTileMx4W, 128, 64, 4, 1>, E>(a, st) : logits_with<Tile<kTileMx4W, 128, 128, 2, 2>, E>(a, st);
 }
