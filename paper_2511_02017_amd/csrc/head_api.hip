@@ -11,7 +11,7 @@ using namespace tapout;
 
 struct tapout_head {
     tapout_head_config cfg;
-    float2 *part = nullptr;              // [N, blocks of a wavefront's vocabulary rows]: at least 64 of them, 32 up to N = 32
+    float2 *part = nullptr;              // [N, blocks of a wavefront's vocabulary rows]: at least 64 of them, 32 up to N = 64
     float *target_logit = nullptr;       // [max_rows]
     void *packed = nullptr;              // [max_rows, dim]: hidden states whose rows lie unevenly
     uint8_t *act_codes = nullptr, *act_scales = nullptr;      // quantised hidden states (bfloat16 heads)
@@ -135,7 +135,7 @@ tapout_status tapout_head_create(tapout_head **out, const tapout_head_config *cf
     DeviceGuard guard(cfg->device);
     const size_t N = cfg->max_rows, D = cfg->dim, esz = size_of(cfg->dtype), P = mx4_cols(cfg->dim);
     const size_t blocks = (cfg->vocab + 127) / 128;
-    bool ok = hipMalloc(&h->part, (N + std::min<size_t>(N, 32)) * 2 * blocks * sizeof(float2)) == hipSuccess
+    bool ok = hipMalloc(&h->part, (N + std::min<size_t>(N, 64)) * 2 * blocks * sizeof(float2)) == hipSuccess
            && hipMalloc(&h->target_logit, N * sizeof(float)) == hipSuccess
            && hipMalloc(&h->packed, N * D * esz) == hipSuccess;
     if (ok && cfg->dtype == TAPOUT_BF16)

@@ -237,7 +237,17 @@ __global__ __launch_bounds__(256) void head_grad_hidden_kernel(GradHiddenArgs a)
     if (n >= a.N) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (row_counts(a.target[n], a.V, a.lse, a.row_weight, n)) {
-        for (int k = 0; k < a.splits; ++k) s += *(const f32x4 *)(a.part + ((int64_t)k * a.N + n) * a.D + d);
+        const float *p = a.part + (int64_t)n * a.D + d;
+        const int64_t next = (int64_t)a.N * a.D;
+        int k = 0;
+        for (; k + 8 <= a.splits; k += 8) {                  // eight loads under way: with few rows this is a chain of round trips
+            f32x4 v[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x] = *(const f32x4 *)(p + (k + x) * next);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) s += v[x];
+        }
+        for (; k < a.splits; ++k) s += *(const f32x4 *)(p + k * next);
         if (a.scale) s *= *a.scale;
     }
     E v[4];
@@ -308,33 +318,31 @@ template <int KIND> using Small = Tile<KIND, 128, 32, 4, 1>;
 template <int KIND> using Mid = Tile<KIND, 128, 128, 2, 2>;
 template <int KIND> using Large = Tile<KIND, 256, 256, 2, 4>;
 
+// Which tile for how many tokens.  A tile of 32 tokens while more would be empty, of 128 while the vocabulary rows' bytes are what
+// takes the time anyway, else of 256, whose loads serve more products (cross entropy of V = 128256, dim = 2048, bfloat16, us with
+// tiles of 32 / 128 / 256 tokens: 32 rows 113 / 116 / 125, 48 rows 122 / 117 / 125, 128 rows 188 / 117 / 126, 192 rows 244 / 165 / 129,
+// 512 rows 560 / 328 / 220).  binary32 products are so much slower that a tile has to fit, and larger ones gain nothing (V = 32000,
+// dim = 1024: 40 rows 43 / 81 / 243, 128 rows 82 / 84 / 241, 256 rows 159 / 149 / 245).
+template <template <class> class F, class A> hipError_t by_tokens(const A &a, int tokens, int dtype, hipStream_t st)
+{
+    if (dtype == TAPOUT_F32) return tokens <= 64 ? F<Small<kTileF32>>::launch(a, st) : F<Mid<kTileF32>>::launch(a, st);
+    return tokens <= 32 ? F<Small<kTileBf16>>::launch(a, st) : tokens <= 128 ? F<Mid<kTileBf16>>::launch(a, st) : F<Large<kTileBf16>>::launch(a, st);
+}
+
+template <class T> struct Loss { static hipError_t launch(const LossArgs &a, hipStream_t st) { return loss_with<T>(a, st); } };
+template <class T> struct Grad { static hipError_t launch(const GradArgs &a, hipStream_t st) { return grad_with<T, typename ElemOf<T::kind == kTileF32 ? TAPOUT_F32 : TAPOUT_BF16>::T>(a, st); } };
+template <class T> struct Product { static hipError_t launch(const ProductArgs &a, hipStream_t st) { return product_with<T, typename ElemOf<T::kind == kTileF32 ? TAPOUT_F32 : TAPOUT_BF16>::T>(a, st); } };
+
 }  // namespace
 
-hipError_t launch_head_loss(const LossArgs &a, int dtype, hipStream_t st)
-{
-    if (dtype == TAPOUT_F32) return a.N <= 32 ? loss_with<Small<kTileF32>>(a, st) : loss_with<Mid<kTileF32>>(a, st);
-    return a.N <= 32 ? loss_with<Small<kTileBf16>>(a, st) : a.N <= 256 ? loss_with<Mid<kTileBf16>>(a, st) : loss_with<Large<kTileBf16>>(a, st);
-}
-
-hipError_t launch_head_grad(const GradArgs &a, int dtype, hipStream_t st)
-{
-    if (dtype == TAPOUT_F32) return a.N <= 32 ? grad_with<Small<kTileF32>, float>(a, st) : grad_with<Mid<kTileF32>, float>(a, st);
-    return a.N <= 32 ? grad_with<Small<kTileBf16>, __bf16>(a, st)
-         : a.N <= 256 ? grad_with<Mid<kTileBf16>, __bf16>(a, st) : grad_with<Large<kTileBf16>, __bf16>(a, st);
-}
+hipError_t launch_head_loss(const LossArgs &a, int dtype, hipStream_t st) { return by_tokens<Loss>(a, a.N, dtype, st); }
+hipError_t launch_head_grad(const GradArgs &a, int dtype, hipStream_t st) { return by_tokens<Grad>(a, a.N, dtype, st); }
+hipError_t launch_head_product(const ProductArgs &a, int dtype, hipStream_t st) { return by_tokens<Product>(a, a.nj, dtype, st); }
 
 int head_product_tiles(int ni, int nj, int dtype)
 {
-    if (nj <= 32) return up(ni, 128) * up(nj, 32);
-    if (nj <= 256 || dtype == TAPOUT_F32) return up(ni, 128) * up(nj, 128);
-    return up(ni, 256) * up(nj, 256);
-}
-
-hipError_t launch_head_product(const ProductArgs &a, int dtype, hipStream_t st)
-{
-    if (dtype == TAPOUT_F32) return a.nj <= 32 ? product_with<Small<kTileF32>, float>(a, st) : product_with<Mid<kTileF32>, float>(a, st);
-    return a.nj <= 32 ? product_with<Small<kTileBf16>, __bf16>(a, st)
-         : a.nj <= 256 ? product_with<Mid<kTileBf16>, __bf16>(a, st) : product_with<Large<kTileBf16>, __bf16>(a, st);
+    const int tj = nj <= (dtype == TAPOUT_F32 ? 64 : 32) ? 32 : nj <= 128 || dtype == TAPOUT_F32 ? 128 : 256;
+    return up(ni, tj == 256 ? 256 : 128) * up(nj, tj);
 }
 
 hipError_t launch_head_transpose(const TransposeArgs &a, int dtype, hipStream_t st)
