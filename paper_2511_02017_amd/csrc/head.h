@@ -46,8 +46,8 @@ struct TransposeArgs {
 };
 hipError_t launch_head_transpose(const TransposeArgs &a, int dtype, hipStream_t st);
 
-// out[j][i] = sum over k of I[i][k] J[j][k].  part given: binary32 partial sums of `splits` runs of k, added to what is there
-// unless `first`; else out, scaled and rounded.
+// out[j][i] = scale * sum over k of I[i][k] J[j][k], rounded; or, with part given, binary32 partial sums over `splits` runs of k, added to
+// what is there unless `first`.  Then I is given turned: I.p[k][i], I.rows steps of k.
 struct ProductArgs {
     Operand I, J;
     int32_t ni, nj, k;           // results and length of k in elements (not 0)
@@ -57,7 +57,8 @@ struct ProductArgs {
     const float *scale;          // device, or NULL (1)
 };
 hipError_t launch_head_product(const ProductArgs &a, int dtype, hipStream_t st);
-int head_product_tiles(int ni, int nj, int dtype);
+int head_product_tiles(int ni, int nj, int dtype);       // tiles of one run, and workgroups resident at a time
+int head_product_slots(int nj, int dtype);
 
 // grad_hidden = scale * (sum of the partial sums), rows that do not count: zeros.
 struct GradHiddenArgs {

@@ -16,7 +16,7 @@ struct tapout_head {
     void *packed = nullptr;              // [max_rows, dim]: hidden states whose rows lie unevenly
     uint8_t *act_codes = nullptr, *act_scales = nullptr;      // quantised hidden states (bfloat16 heads)
     // training only
-    char *piece = nullptr;  size_t piece_cap = 0;             // a piece's gradient in both orientations and its weights transposed
+    char *piece = nullptr;  size_t piece_cap = 0;             // a piece's gradient in both orientations
     void *hidden_t = nullptr;                                 // [dim, max_rows padded to 32]
     float *grad_part = nullptr;  size_t grad_cap = 0;         // partial sums of grad_hidden (floats)
     char err[256] = {0};
@@ -110,7 +110,7 @@ hipError_t hidden_operand(tapout_head *h, const tapout_logits *x, int B, int K, 
     return launch_head_pack(a, x->dtype, st);
 }
 
-size_t piece_bytes(int n_pad, int N, int D, int esz) { return (size_t)n_pad * ((size_t)N + up_to(N, 32) + D) * esz; }
+size_t piece_bytes(int n_pad, int N, int esz) { return (size_t)n_pad * ((size_t)N + up_to(N, 32)) * esz; }
 
 }  // namespace
 
@@ -141,7 +141,7 @@ tapout_status tapout_head_create(tapout_head **out, const tapout_head_config *cf
     if (ok && cfg->dtype == TAPOUT_BF16)
         ok = hipMalloc(&h->act_codes, N * P / 2) == hipSuccess && hipMalloc(&h->act_scales, N * P / 32) == hipSuccess;
     if (ok && cfg->training) {
-        h->piece_cap = std::min(piece_bytes(up_to(cfg->vocab, 256), (int)N, (int)D, (int)esz), std::max(kPieceBytes, piece_bytes(256, (int)N, (int)D, (int)esz)));
+        h->piece_cap = std::min(piece_bytes(up_to(cfg->vocab, 256), (int)N, (int)esz), std::max(kPieceBytes, piece_bytes(256, (int)N, (int)esz)));
         h->grad_cap = std::max(N * D, (size_t)16 << 20);
         ok = hipMalloc(&h->piece, h->piece_cap) == hipSuccess
           && hipMalloc(&h->hidden_t, D * up_to((int)N, 32) * esz) == hipSuccess
@@ -284,17 +284,18 @@ tapout_status tapout_head_loss_grad(tapout_head *h, const tapout_logits *hidden,
     e = launch_head_transpose(t, dt, st);
     if (e != hipSuccess) return hip_fail(h, e, "hidden states transposed");
     // pieces of the vocabulary of equal length, as long as the scratch allows
-    const size_t per = piece_bytes(1, N, D, esz);
+    const size_t per = piece_bytes(1, N, esz);
     const int most = (int)std::min<size_t>(up_to(V, 256), h->piece_cap / per / 256 * 256);
     const int pieces = (V + most - 1) / most, len = up_to((V + pieces - 1) / pieces, 256);
-    // runs of k of the product by the hidden states: as many as it takes to give every compute unit two tiles
+    // runs of k of the product by the hidden states: as many as there are workgroups for at a time (two of them a unit: 1503 rows, dim =
+    // 1120 466 us with both products, see below), each long enough to be worth its partial sums
     const int tiles = head_product_tiles(D, N, dt), stages = up_to(std::min(len, V), 64) / (dt == TAPOUT_F32 ? 32 : 64);
-    int splits = std::max(1, std::min({512 / tiles, stages / 4, (int)(h->grad_cap / ((size_t)N * D))}));
+    int splits = std::max(1, std::min({head_product_slots(N, dt) / tiles, stages / 4, (int)(h->grad_cap / ((size_t)N * D))}));
     splits = (stages + (stages + splits - 1) / splits - 1) / ((stages + splits - 1) / splits);        // runs of equal length, none of them empty
     for (int v0 = 0; v0 < V; v0 += len) {
         const int n = std::min(len, V - v0), n_pad = up_to(n, 64);
         const char *rows = (const char *)weight->ptr + v0 * weight->stride * esz;
-        char *g = h->piece, *gt = g + (size_t)N * n_pad * esz, *wt = gt + (size_t)N_pad * n_pad * esz;
+        char *g = h->piece, *gt = g + (size_t)N * n_pad * esz;
         GradArgs a{};
         a.weight = Operand{rows, weight->stride * esz, n, D * esz, nullptr, 0};
         a.hidden = x;
@@ -303,11 +304,8 @@ tapout_status tapout_head_loss_grad(tapout_head *h, const tapout_logits *hidden,
         a.g = g; a.g_stride = n_pad; a.gt = gt; a.gt_stride = N_pad;
         e = launch_head_grad(a, dt, st);
         if (e != hipSuccess) return hip_fail(h, e, "head_grad");
-        const TransposeArgs t{rows, weight->stride, wt, n_pad, n, D, n_pad, V, nullptr, nullptr, nullptr};
-        e = launch_head_transpose(t, dt, st);
-        if (e != hipSuccess) return hip_fail(h, e, "weights transposed");
         ProductArgs p{};
-        p.I = Operand{wt, (int64_t)n_pad * esz, D, n_pad * esz, nullptr, 0};
+        p.I = a.weight;
         p.J = Operand{g, (int64_t)n_pad * esz, N, n_pad * esz, nullptr, 0};
         p.ni = D; p.nj = N; p.k = n_pad; p.splits = splits; p.first = v0 == 0; p.part = h->grad_part;
         e = launch_head_product(p, dt, st);

@@ -42,7 +42,7 @@ template <int KIND> struct Kind {
 };
 
 struct Operand {
-    const void *p;          // row 0, 16-byte aligned
+    const void *p;          // row 0, 16-byte aligned (I turned: step 0 of k)
     int64_t stride;         // bytes from row to row, a multiple of 16; 256 of them within 2^31 (checked on the host)
     int32_t rows;
     int32_t row_bytes;      // bytes of a row, a multiple of 16: what lies behind counts as zeros
@@ -64,7 +64,7 @@ template <int R> __device__ __forceinline__ int chunk_swap(int row)
 constexpr uint32_t kNoMemory = 0x80000000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, int64_t bytes)
 {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(bytes < 0x7fffffff ? bytes : 0x7fffffff), 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes <= 0 ? 0 : (int)(bytes < 0x7fffffff ? bytes : 0x7fffffff), 0x00020000);
 }
 
 // Which row of the tile lies at row q of its part of LDS, that is, which row a matrix instruction takes as its q % 16th.  A lane's
@@ -75,10 +75,24 @@ __device__ __forceinline__ int row_of_i(int q) { return (q & ~31) | (q & 12) << 
 template <int NJ> __device__ __forceinline__ int row_of_j(int q) { return q / (16 * NJ) * (16 * NJ) + (q & 15) * NJ + (q >> 4) % NJ; }
 template <int NJ> __device__ __forceinline__ int tile_row(int q) { if constexpr (NJ == 0) return row_of_i(q); else return row_of_j<NJ>(q); }
 
+// A wavefront's load of 64 x 16 bytes into LDS.  HIDDEN: not as the builtin, whose loads the compiler takes to be meant by every turning
+// read that follows, and waits for (the product by 1503 hidden states 754 instead of 250 us).  There are no registers to be written;
+// this wavefront and the others wait by number, below.  M0 needs no saving: a kernel that loads so has no other use for it.
+template <bool HIDDEN> __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t off, uint32_t from)
+{
+    const auto to = (__attribute__((address_space(3))) void *)lds;
+    if constexpr (HIDDEN) {
+        const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)to);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(off), "s"(rsrc), "s"(from) : "memory");
+    } else {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, off, from, 0, 0);
+    }
+}
+
 // T rows of R bytes of a stage, in pieces of a wavefront's load, W bytes a lane.  Every wavefront makes the same number of loads,
 // since it waits for them by their number: where there are fewer pieces than wavefronts, some are loaded twice.  Rows behind the
 // operand's last one and bytes behind a row's last one come as zeros.
-template <int T, int R, int W, int NW, int NJ> struct Stager {           // NJ = 0: I's rows
+template <int T, int R, int W, int NW, int NJ, bool HIDDEN = false> struct Stager {           // NJ = 0: I's rows
     static constexpr int pieces = T * R / (64 * W) < 1 ? 1 : T * R / (64 * W), per = (pieces + NW - 1) / NW, rows = 64 * W / R, lanes = R / W;
     static_assert(pieces % NW == 0 || pieces < NW, "");
     uint32_t off, now, at;           // of this lane: from the tile's first row; the same, or nowhere; its first byte in a row's R
@@ -92,10 +106,31 @@ template <int T, int R, int W, int NW, int NJ> struct Stager {           // NJ =
     // The row orders exchange bits of a row's number, and the wavefronts' pieces of one n differ in bits of their own.
     __device__ __forceinline__ void issue(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, int s, int64_t stride, int wave) const
     {
-        const auto to = (__attribute__((address_space(3))) void *)(lds + (wave % pieces + n * NW) * (64 * W));
+        char *to = lds + (wave % pieces + n * NW) * (64 * W);
         const uint32_t from = (uint32_t)(tile_row<NJ>(n * NW * rows) * stride) + (uint32_t)(s * R);
-        if constexpr (W == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, now, from, 0, 0);
-        else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 4, now, from, 0, 0);
+        if constexpr (W == 16) load_to_lds<HIDDEN>(rsrc, to, now, from);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)to, 4, now, from, 0, 0);
+    }
+};
+// The same of an operand whose rows are steps of k (its columns the rows of I): KS of them, T columns of E bytes each, 16 bytes a lane.
+// A lane of a matrix instruction wants neighbours in k of one column; the reads below turn them round.  They serve rows 8 g + 0..3 (bfloat16,
+// sixteen columns in 32 bytes) or 4 g + j (binary32, 64 bytes) of neighbouring g at a time, which the exchange of slots of that size
+// by bits of the row spreads over the banks.
+template <int T, int KS, int E, int NW> struct TurnedStager {
+    static constexpr int R = T * E, pieces = R * KS / 1024, per = pieces / NW, rows = 1024 / R, lanes = R / 16;
+    static_assert(pieces % NW == 0 && NW * rows % 8 == 0, "");
+    static __device__ __forceinline__ uint32_t swap(int row) { return E == 2 ? ((row & 3) | (row >> 1 & 4)) * 32u : (uint32_t)(row >> 2 & 3) * 64u; }
+    uint32_t row_off, chunk[2];      // of this lane's first row; its bytes in a row, of even and odd n
+    __device__ __forceinline__ void init(int64_t stride, int wave, int lane)
+    {
+        const int q = wave * rows + lane / lanes;
+        row_off = (uint32_t)(q * stride);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) chunk[n] = (uint32_t)(lane % lanes) * 16u ^ swap(q + n * NW * rows);
+    }
+    __device__ __forceinline__ void issue(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, int64_t stride, int wave) const
+    {
+        load_to_lds<E == 2>(rsrc, lds + (wave + n * NW) * 1024, row_off + chunk[NW * rows % 16 ? n & 1 : 0], (uint32_t)(n * NW * rows * stride));
     }
 };
 struct NoStager {
@@ -204,8 +239,12 @@ struct Work { int i0, j0, first, n; };
 //   i = i_of(mi) + r,   j = j_of(nj).
 // I's part of a stage has ring_i places in LDS, J's two: three and two are what 160 KB hold of 256 x 256 (128 x 128: twice a
 // compute unit).
-template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
+// TURNED: I lies with its columns contiguous; results of one lane are then four neighbours in I only.
+template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> struct Tile {
     using K = Kind<KIND>;
+    static_assert(!TURNED || KIND == kTileF32 || KIND == kTileBf16, "");
+    static constexpr int esz = KIND == kTileF32 ? 4 : 2;
+    static constexpr bool turned = TURNED;
     static constexpr int kind = KIND, TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, NW = WI * WJ, threads = NW * 64;
     static constexpr int MI = TI / WI / 16, NJ = TJ / WJ / 16;
     static_assert(MI % 2 == 0, "rows of I are ordered by pairs of blocks");
@@ -215,15 +254,19 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
     static constexpr int ring_i = KIND == kTileMx4 ? 2 : 3, ring_j = 2, ring_bytes = ring_i * bytes_i + ring_j * bytes_j;
     static constexpr int per_cu = 163840 / ring_bytes < 1 ? 1 : 163840 / ring_bytes > 2048 / threads ? 2048 / threads : 163840 / ring_bytes;
     using Acc = f32x4[MI][NJ];
-    using StagerI = Stager<TI, K::row_i, 16, NW, 0>;
-    using StagerJ = Stager<TJ, K::row_j, 16, NW, NJ>;
+    using StagerI = std::conditional_t<TURNED, TurnedStager<TI, K::elems, esz, NW>, Stager<TI, K::row_i, 16, NW, 0>>;
+    using StagerJ = Stager<TJ, K::row_j, 16, NW, NJ, TURNED && KIND == kTileBf16>;
     using ScalesI = std::conditional_t<(K::scale_i > 0), Stager<TI, (K::scale_i > 0 ? K::scale_i : 4), 4, NW, 0>, NoStager>;
     using ScalesJ = std::conditional_t<(K::scale_j > 0), Stager<TJ, (K::scale_j > 0 ? K::scale_j : 4), 4, NW, NJ>, NoStager>;
     static constexpr int li = StagerI::per + ScalesI::per, lj = StagerJ::per + ScalesJ::per;       // loads of a wavefront and stage
 
     static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
     static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-    static __device__ __forceinline__ int i_of(int mi) { return wave() / WJ * (MI * 16) + (mi >> 1) * 32 + (lane() >> 4) * 8 + (mi & 1) * 4; }
+    static __device__ __forceinline__ int i_of(int mi)
+    {
+        const int g = lane() >> 4;
+        return wave() / WJ * (MI * 16) + (TURNED ? mi * 16 + g * 4 : (mi >> 1) * 32 + g * 8 + (mi & 1) * 4);
+    }
     static __device__ __forceinline__ int j_of(int nj) { return wave() % WJ * (NJ * 16) + (lane() & 15) * NJ + nj; }
 
     // What a wavefront multiplies: blocks of I (those of the next step replace them one by one), and of J for two steps.
@@ -233,11 +276,17 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
     };
     // Where this lane reads: its row of the first block, and the chunk of step 0; steps exchange bits of the chunk.
     struct Places {
-        uint32_t a, b, sa, sb;
+        uint32_t a, b, sa, sb, turn = 0;
         __device__ __forceinline__ Places()
         {
             const int r16 = lane() & 15, g = lane() >> 4, ra = wave() / WJ * MI * 16 + r16, rb = wave() % WJ * NJ * 16 + r16;
             a = ra * K::row_i + (g ^ chunk_swap<K::row_i>(r16)) * 16;
+            if constexpr (TURNED) {
+                // row of step 0 and its bytes there, without the exchange of slots: bfloat16 a row for every four lanes, 8 bytes each
+                const int row = KIND == kTileBf16 ? g * 8 + r16 / 4 : g * 4;
+                a = row * (TI * esz) + (KIND == kTileBf16 ? r16 % 4 * 8 : r16 * 4);
+                turn = StagerI::swap(row);
+            }
             b = rb * K::row_j + ((KIND == kTileMx4W ? g * 4 : g) ^ chunk_swap<K::row_j>(r16)) * 16;
             sa = oSI + ra * K::scale_i + g;
             sb = oSJ + rb * K::scale_j + g;
@@ -245,7 +294,21 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
     };
     static __device__ __forceinline__ void read_a(int set, int m, const char *pi, int s, const Places &at, Frags &f)
     {
-        f.a[set][m] = *(const u32x4 *)(pi + (at.a ^ (s * 64)) + m * 16 * K::row_i);
+        if constexpr (TURNED) {
+            const char *p = pi + at.a + (((wave() / WJ * MI + m) * 16 * esz) ^ at.turn) + s * (K::elems / 2) * (TI * esz);
+            if constexpr (KIND == kTileBf16) {
+                using s16x4 = short __attribute__((ext_vector_type(4)));
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p + 4 * TI * esz));
+                const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
+                f.a[set][m] = u32x4{l.x, l.y, h.x, h.y};
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f.a[set][m][j] = *(const uint32_t *)(p + j * TI * esz);
+            }
+        } else {
+            f.a[set][m] = *(const u32x4 *)(pi + (at.a ^ (s * 64)) + m * 16 * K::row_i);
+        }
         // a byte of its own for every lane: shifted out of a word that four lanes read, it would hold up the matrix instructions, which
         // wait for results of the vector ALU (6.6 and 4.1 PFLOP/s of 4-bit products with nothing else in the loop)
         if constexpr (K::scale_i > 0) f.sa[set][m] = *(const uint8_t *)(pi + at.sa + s * 4 + m * 16 * K::scale_i);
@@ -297,16 +360,22 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
         hj.init(J.scale_stride, wave, lane);
         Work w = where(walk);                                    // the tile that is multiplied
         Walk ahead_walk = walk;                                  // the tile that is loaded
-        int ahead = 0, ahead_n = 0;                              // the next stage to be loaded, and where its tile's stages end
+        int from_i = 0, ahead = 0, ahead_n = 0;                              // the next stage to be loaded, and where its tile's stages end
         auto stage = [&] {
-            gi.stage(ahead, I.row_bytes);
+            if constexpr (TURNED) {
+                const int64_t k = (int64_t)ahead * K::elems;
+                ri = buffer_of((const char *)I.p + k * I.stride + from_i * esz, (I.rows - 1 - k) * I.stride + I.row_bytes - from_i * esz);
+            } else {
+                gi.stage(ahead, I.row_bytes);
+            }
             gj.stage(ahead, J.row_bytes);
             hi.stage(ahead, I.scale_stride);
             hj.stage(ahead, J.scale_stride);
         };
         auto load_from = [&](const Work &v) {
             const int64_t left_i = I.rows - v.i0, left_j = J.rows - v.j0;
-            ri = buffer_of((const char *)I.p + v.i0 * I.stride, (left_i - 1) * I.stride + I.row_bytes);
+            from_i = v.i0;
+            if constexpr (!TURNED) ri = buffer_of((const char *)I.p + v.i0 * I.stride, (left_i - 1) * I.stride + I.row_bytes);
             rj = buffer_of((const char *)J.p + v.j0 * J.stride, (left_j - 1) * J.stride + J.row_bytes);
             if constexpr (K::scale_i > 0) rsi = buffer_of(I.scales + (int64_t)v.i0 * I.scale_stride, left_i * I.scale_stride);
             if constexpr (K::scale_j > 0) rsj = buffer_of(J.scales + (int64_t)v.j0 * J.scale_stride, left_j * J.scale_stride);
@@ -316,7 +385,8 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_> struct Tile {
         };
         // Load x of either operand's part of stage `ahead`.  Behind the last tile: its last stage again, into memory that nobody reads.
         auto load_i = [&](int x, char *to) {
-            if (x < gi.per) gi.issue(x, ri, to, ahead, I.stride, wave);
+            if constexpr (TURNED) gi.issue(x, ri, to, I.stride, wave);
+            else if (x < gi.per) gi.issue(x, ri, to, ahead, I.stride, wave);
             else hi.issue(x - gi.per, rsi, to + oSI, ahead, I.scale_stride, wave);
         };
         auto load_j = [&](int x, char *to) {

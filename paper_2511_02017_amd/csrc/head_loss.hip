@@ -88,24 +88,38 @@ __global__ __launch_bounds__(T::threads) void head_loss_kernel(LossArgs a, int n
         });
 }
 
-// A wavefront a row: the tiles' maxima and sums to lse, in double.
-__global__ __launch_bounds__(256) void head_loss_join_kernel(LossArgs a, int ni)
+// A workgroup a row: the blocks' maxima and sums to lse, in double.
+__global__ __launch_bounds__(256) void head_loss_join_kernel(LossArgs a, int blocks)
 {
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (n >= a.N) return;
-    const float2 *p = a.part + (int64_t)n * ni;
+    __shared__ float maxima[4];
+    __shared__ double sums[4];
+    const int n = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float2 *p = a.part + (int64_t)n * blocks;
     float m = -INFINITY;
-    for (int x = lane; x < ni; x += 64) m = fmaxf(m, p[x].x);
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    const float ref = m == -INFINITY ? 0.f : m;
     double s = 0.0;
-    for (int x = lane; x < ni; x += 64) {
-        const float2 q = p[x];
-        s += (double)q.y * (double)__builtin_amdgcn_exp2f(((q.x == -INFINITY ? 0.f : q.x) - ref) * kLog2e);
+    for (int x = threadIdx.x; x < blocks; x += 1024) {
+        float2 q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = x + k * 256 < blocks ? p[x + k * 256] : float2{-INFINITY, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float top = fmaxf(m, q[k].x), ref = top == -INFINITY ? 0.f : top;
+            s = s * (double)__builtin_amdgcn_exp2f((fmaxf(m, -3.4e38f) - ref) * kLog2e) + (double)q[k].y * (double)__builtin_amdgcn_exp2f((fmaxf(q[k].x, -3.4e38f) - ref) * kLog2e);
+            m = top;
+        }
     }
+    const float own = m;
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if (lane == 0) maxima[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
+    const float ref = m == -INFINITY ? 0.f : m;
+    s *= (double)__builtin_amdgcn_exp2f((fmaxf(own, -3.4e38f) - ref) * kLog2e);
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    if (lane) return;
-    const double lse = (double)ref + log(s);
+    if (lane == 0) sums[wave] = s;
+    __syncthreads();
+    if (threadIdx.x) return;
+    const double lse = (double)ref + log(((sums[0] + sums[1]) + sums[2]) + sums[3]);
     const int t = counted_target(a.target[n], a.V);
     const bool bad = !(fabs(lse) < (double)INFINITY);
     const float nan = __uint_as_float(0x7fc00000u);
@@ -202,7 +216,7 @@ template <class T, class E>
 __global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int per_split, int splits)
 {
     extern __shared__ __align__(16) char lds[];
-    const float scale = a.part || !a.scale ? 1.f : *a.scale;
+    const float scale = T::turned || !a.scale ? 1.f : *a.scale;
     T::template work<0>(a.I, a.J, Walk(ni, nj, splits), lds,
         [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, t.split * per_split, min(per_split, stages - t.split * per_split)}; },
         [&](const Work &) {},
@@ -211,16 +225,19 @@ __global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a,
             for (int n = 0; n < T::NJ; ++n) {
                 const int j = w.j0 + T::j_of(n);
                 if (j >= a.nj) continue;
+                if constexpr (T::turned) {                        // partial sums
+                    float *to = a.part + ((int64_t)(w.first / per_split) * a.nj + j) * a.ni + w.i0;
 #pragma unroll
-                for (int mi = 0; mi < T::MI; mi += 2) {
-                    const int i = w.i0 + T::i_of(mi);
-                    if (i >= a.ni) continue;
-                    if (a.part) {
-                        f32x4 *to = (f32x4 *)(a.part + ((int64_t)(w.first / per_split) * a.nj + j) * a.ni + i);
-                        to[0] = a.first ? acc[mi][n] : to[0] + acc[mi][n];
-                        to[1] = a.first ? acc[mi + 1][n] : to[1] + acc[mi + 1][n];
-                    } else {
-                        store8((E *)a.out + (int64_t)j * a.out_stride + i, acc[mi][n] * scale, acc[mi + 1][n] * scale);
+                    for (int mi = 0; mi < T::MI; ++mi) {
+                        const int i = T::i_of(mi);
+                        if (w.i0 + i < a.ni) *(f32x4 *)(to + i) = a.first ? acc[mi][n] : *(const f32x4 *)(to + i) + acc[mi][n];
+                    }
+                } else {
+                    E *to = (E *)a.out + (int64_t)j * a.out_stride + w.i0;
+#pragma unroll
+                    for (int mi = 0; mi < T::MI; mi += 2) {
+                        const int i = T::i_of(mi);
+                        if (w.i0 + i < a.ni) store8(to + i, acc[mi][n] * scale, acc[mi + 1][n] * scale);
                     }
                 }
             }
@@ -289,7 +306,7 @@ template <class T> hipError_t loss_with(const LossArgs &a, hipStream_t st)
         head_loss_kernel<T><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
     });
     if (e != hipSuccess) return e;
-    head_loss_join_kernel<<<up(a.N, 4), 256, 0, st>>>(a, ni * T::WI);
+    head_loss_join_kernel<<<a.N, 256, 0, st>>>(a, ni * T::WI);
     return hipGetLastError();
 }
 
@@ -314,19 +331,20 @@ template <class T, class E> hipError_t product_with(const ProductArgs &a, hipStr
     });
 }
 
-template <int KIND> using Small = Tile<KIND, 128, 32, 4, 1>;
-template <int KIND> using Mid = Tile<KIND, 128, 128, 2, 2>;
-template <int KIND> using Large = Tile<KIND, 256, 256, 2, 4>;
+template <int KIND, bool TURNED = false> using Small = Tile<KIND, 128, 32, 4, 1, TURNED>;
+template <int KIND, bool TURNED = false> using Mid = Tile<KIND, 128, 128, 2, 2, TURNED>;
+template <int KIND, bool TURNED = false> using Large = Tile<KIND, 256, 256, 2, 4, TURNED>;
 
 // Which tile for how many tokens.  A tile of 32 tokens while more would be empty, of 128 while the vocabulary rows' bytes are what
 // takes the time anyway, else of 256, whose loads serve more products (cross entropy of V = 128256, dim = 2048, bfloat16, us with
 // tiles of 32 / 128 / 256 tokens: 32 rows 113 / 116 / 125, 48 rows 122 / 117 / 125, 128 rows 188 / 117 / 126, 192 rows 244 / 165 / 129,
 // 512 rows 560 / 328 / 220).  binary32 products are so much slower that a tile has to fit, and larger ones gain nothing (V = 32000,
 // dim = 1024: 40 rows 43 / 81 / 243, 128 rows 82 / 84 / 241, 256 rows 159 / 149 / 245).
-template <template <class> class F, class A> hipError_t by_tokens(const A &a, int tokens, int dtype, hipStream_t st)
+template <template <class> class F, bool TURNED, class A> hipError_t by_tokens(A &&a, int tokens, int dtype, hipStream_t st)
 {
-    if (dtype == TAPOUT_F32) return tokens <= 64 ? F<Small<kTileF32>>::launch(a, st) : F<Mid<kTileF32>>::launch(a, st);
-    return tokens <= 32 ? F<Small<kTileBf16>>::launch(a, st) : tokens <= 128 ? F<Mid<kTileBf16>>::launch(a, st) : F<Large<kTileBf16>>::launch(a, st);
+    if (dtype == TAPOUT_F32) return tokens <= 64 ? F<Small<kTileF32, TURNED>>::launch(a, st) : F<Mid<kTileF32, TURNED>>::launch(a, st);
+    return tokens <= 32 ? F<Small<kTileBf16, TURNED>>::launch(a, st)
+         : tokens <= 128 ? F<Mid<kTileBf16, TURNED>>::launch(a, st) : F<Large<kTileBf16, TURNED>>::launch(a, st);
 }
 
 template <class T> struct Loss { static hipError_t launch(const LossArgs &a, hipStream_t st) { return loss_with<T>(a, st); } };
@@ -335,14 +353,23 @@ template <class T> struct Product { static hipError_t launch(const ProductArgs &
 
 }  // namespace
 
-hipError_t launch_head_loss(const LossArgs &a, int dtype, hipStream_t st) { return by_tokens<Loss>(a, a.N, dtype, st); }
-hipError_t launch_head_grad(const GradArgs &a, int dtype, hipStream_t st) { return by_tokens<Grad>(a, a.N, dtype, st); }
-hipError_t launch_head_product(const ProductArgs &a, int dtype, hipStream_t st) { return by_tokens<Product>(a, a.nj, dtype, st); }
+hipError_t launch_head_loss(const LossArgs &a, int dtype, hipStream_t st) { return by_tokens<Loss, false>(a, a.N, dtype, st); }
+hipError_t launch_head_grad(const GradArgs &a, int dtype, hipStream_t st) { return by_tokens<Grad, false>(a, a.N, dtype, st); }
+hipError_t launch_head_product(const ProductArgs &a, int dtype, hipStream_t st) { return a.part ? by_tokens<Product, true>(a, a.nj, dtype, st) : by_tokens<Product, false>(a, a.nj, dtype, st); }
 
+template <class T> struct Slots { static hipError_t launch(int *out, hipStream_t) { *out = kCUs * T::per_cu; return hipSuccess; } };
+template <class T> struct Sizes { static hipError_t launch(int *out, hipStream_t) { out[0] = T::TI; out[1] = T::TJ; return hipSuccess; } };
+int head_product_slots(int nj, int dtype)
+{
+    int slots = 0;
+    (void)by_tokens<Slots, true>(&slots, nj, dtype, nullptr);
+    return slots;
+}
 int head_product_tiles(int ni, int nj, int dtype)
 {
-    const int tj = nj <= (dtype == TAPOUT_F32 ? 64 : 32) ? 32 : nj <= 128 || dtype == TAPOUT_F32 ? 128 : 256;
-    return up(ni, tj == 256 ? 256 : 128) * up(nj, tj);
+    int size[2] = {1, 1};
+    (void)by_tokens<Sizes, true>(size, nj, dtype, nullptr);
+    return up(ni, size[0]) * up(nj, size[1]);
 }
 
 hipError_t launch_head_transpose(const TransposeArgs &a, int dtype, hipStream_t st)
