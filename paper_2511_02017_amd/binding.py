@@ -661,55 +661,50 @@ def _on(t, dev, name):
         raise ValueError(f"{name} lives on {t.device}, expected {dev}")
 
 
-class _allocating_on:
-    """Outputs made inside belong to `stream`, so that their memory is not handed on while it still works on them."""
-
-    def __init__(self, stream):
-        self.ctx = torch.cuda.stream(stream) if stream is not None else None
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-
-    def __exit__(self, *e):
-        if self.ctx is not None:
-            self.ctx.__exit__(*e)
+def _empty(shape, dtype, device, stream):
+    """An output of a call on `stream`: its memory belongs to that stream, so that it is not handed on while the call still works on it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def mx4_quantize(x, out=None, stream=None):
     """tapout_mx4_quantize: x [rows, cols] to (codes uint8 [rows, P / 2], scales uint8 [rows, P / 32]), P = cols rounded up to 128.
     `out`: such a pair to write into."""
-    lib = load_library()
-    m = _matrix(x, "x")
+    lib = _lib or load_library()
+    if x.dim() != 2 or not x.is_cuda:
+        _matrix(x, "x")                                        # says what is wrong
     rows, cols = x.shape
     P = -(-cols // MX4_PAD) * MX4_PAD
-    with torch.cuda.device(x.device):
-        if out is None:
-            with _allocating_on(stream):
-                out = (torch.empty((rows, P // 2), dtype=torch.uint8, device=x.device), torch.empty((rows, P // 32), dtype=torch.uint8, device=x.device))
-        codes, scales = out
+    codes, scales = out if out is not None else (_empty((rows, P // 2), torch.uint8, x.device, stream), _empty((rows, P // 32), torch.uint8, x.device, stream))
+    st = _fast.mx4_quantize(x, codes, scales, _handle(stream))
+    if st is None:
+        m = _matrix(x, "x")
         _on(codes, x.device, "codes"), _on(scales, x.device, "scales")
-        st = lib.tapout_mx4_quantize(C.byref(m), rows, cols, _ptr(codes, torch.uint8, (rows, P // 2), "codes"),
-                                     _ptr(scales, torch.uint8, (rows, P // 32), "scales"), _stream(stream))
+        with torch.cuda.device(x.device):
+            st = lib.tapout_mx4_quantize(C.byref(m), rows, cols, _ptr(codes, torch.uint8, (rows, P // 2), "codes"),
+                                         _ptr(scales, torch.uint8, (rows, P // 32), "scales"), _stream(stream))
     if st != 0:
         raise TapoutError(st, lib.tapout_head_last_error(None).decode())
-    return out
+    return codes, scales
 
 
 def mx4_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, stream=None):
     """tapout_mx4_dequantize: the values [rows, cols] that codes and scales stand for."""
-    lib = load_library()
+    lib = _lib or load_library()
     rows, P = codes.shape[0], -(-cols // MX4_PAD) * MX4_PAD
-    with torch.cuda.device(codes.device):
-        if out is None:
-            with _allocating_on(stream):
-                out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+    if out is None:
+        out = _empty((rows, cols), dtype, codes.device, stream)
+    st = _fast.mx4_dequantize(codes, scales, cols, out, _handle(stream))
+    if st is None:
         m = _matrix(out, "out")
         if tuple(out.shape) != (rows, cols):
             raise ValueError(f"out: expected shape {(rows, cols)}, got {tuple(out.shape)}")
         _on(scales, codes.device, "scales"), _on(out, codes.device, "out")
-        st = lib.tapout_mx4_dequantize(_ptr(codes, torch.uint8, (rows, P // 2), "codes"), _ptr(scales, torch.uint8, (rows, P // 32), "scales"),
-                                       rows, cols, C.byref(m), _stream(stream))
+        with torch.cuda.device(codes.device):
+            st = lib.tapout_mx4_dequantize(_ptr(codes, torch.uint8, (rows, P // 2), "codes"), _ptr(scales, torch.uint8, (rows, P // 32), "scales"),
+                                           rows, cols, C.byref(m), _stream(stream))
     if st != 0:
         raise TapoutError(st, lib.tapout_head_last_error(None).decode())
     return out
@@ -729,9 +724,11 @@ class DraftHead:
         st = self._lib.tapout_head_create(C.byref(self._head), C.byref(self.cfg))
         if st != 0:
             raise TapoutError(st, self._lib.tapout_head_last_error(None).decode())
+        self._addr = self._head.value                           # for the native marshalling; 0 once closed
 
     def close(self):
         head = getattr(self, "_head", None)
+        self._addr = 0
         if head is not None and head.value:
             self._lib.tapout_head_destroy(head)
             self._head = None
@@ -741,6 +738,10 @@ class DraftHead:
     def _check(self, st):
         if st != 0:
             raise TapoutError(st, self._lib.tapout_head_last_error(self._head).decode())
+
+    def _on_stream(self, stream):
+        """The stream given, or the current one of the head's device."""
+        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream.cuda_stream
 
     def _hidden(self, t, name) -> TapoutLogits:
         if t.dim() != 3 or t.shape[2] != self.dim:
@@ -763,52 +764,59 @@ class DraftHead:
     def logits(self, hidden, codes, scales, k_len=None, act_bits: int = 16, dtype=torch.bfloat16, out=None, stream=None):
         """tapout_head_logits_mx4: the draft logits [B, K, V] of hidden states [B, K, dim] under the head codes, scales
         (mx4_quantize).  With k_len, rows behind it are left as they are in `out` (and undefined without)."""
-        hd = self._hidden(hidden, "hidden")
-        (B, K, _), V, P = hidden.shape, codes.shape[0], -(-self.dim // MX4_PAD) * MX4_PAD
+        (B, K, _), V = hidden.shape, codes.shape[0]
         if out is None:
-            with _allocating_on(stream):
-                out = torch.empty((B, K, V), dtype=dtype, device=self.device)
-        lg = _logits(out, "out")
+            out = _empty((B, K, V), dtype, self.device, stream)
+        st = _fast.head_logits(self._addr, self.dim, self.cfg.dtype, self.cfg.device, hidden, codes, scales, k_len, act_bits, out, _handle(stream))
+        if st == 0:
+            return out
+        hd, lg, P = self._hidden(hidden, "hidden"), _logits(out, "out"), -(-self.dim // MX4_PAD) * MX4_PAD
         if tuple(out.shape) != (B, K, V):
             raise ValueError(f"out: expected shape {(B, K, V)}, got {tuple(out.shape)}")
         for t, n in ((codes, "codes"), (scales, "scales"), (k_len, "k_len"), (out, "out")):
             _on(t, self.device, n)
-        self._check(self._lib.tapout_head_logits_mx4(
+        self._check(st if st is not None else self._lib.tapout_head_logits_mx4(
             self._head, C.byref(hd), _ptr(codes, torch.uint8, (V, P // 2), "codes"), _ptr(scales, torch.uint8, (V, P // 32), "scales"),
-            B, K, V, _ptr(k_len, torch.int32, (B,), "k_len"), int(act_bits), C.byref(lg), _stream(stream)))
+            B, K, V, _ptr(k_len, torch.int32, (B,), "k_len"), int(act_bits), C.byref(lg), self._on_stream(stream)))
         return out
 
     def loss(self, hidden, weight, target, out=None, stream=None):
         """tapout_head_loss.  Returns / fills a dict: loss, lse [B, K] float32, flags [B] int32."""
-        hd, w = self._hidden(hidden, "hidden"), self._weight(weight, "weight")
         B, K, _ = hidden.shape
         if out is None:
-            with _allocating_on(stream):
-                out = dict(loss=torch.empty((B, K), dtype=torch.float32, device=self.device), lse=torch.empty((B, K), dtype=torch.float32, device=self.device),
-                           flags=torch.empty(B, dtype=torch.int32, device=self.device))
-        _on(target, self.device, "target")
-        self._check(self._lib.tapout_head_loss(
+            out = dict(loss=_empty((B, K), torch.float32, self.device, stream), lse=_empty((B, K), torch.float32, self.device, stream),
+                       flags=_empty((B,), torch.int32, self.device, stream))
+        st = _fast.head_loss(self._addr, self.dim, self.cfg.dtype, self.cfg.device, hidden, weight, target, out, _handle(stream))
+        if st == 0:
+            return out
+        hd, w = self._hidden(hidden, "hidden"), self._weight(weight, "weight")
+        for t, n in ((target, "target"), (out["loss"], "loss"), (out["lse"], "lse"), (out.get("flags"), "flags")):
+            _on(t, self.device, n)
+        self._check(st if st is not None else self._lib.tapout_head_loss(
             self._head, C.byref(hd), C.byref(w), B, K, weight.shape[0], _ptr(target, torch.int32, (B, K), "target"),
             _ptr(out["loss"], torch.float32, (B, K), "loss"), _ptr(out["lse"], torch.float32, (B, K), "lse"),
-            _ptr(out.get("flags"), torch.int32, (B,), "flags"), _stream(stream)))
+            _ptr(out.get("flags"), torch.int32, (B,), "flags"), self._on_stream(stream)))
         return out
 
     def loss_grad(self, hidden, weight, target, lse, row_weight=None, scale=None, out=None, stream=None):
         """tapout_head_loss_grad.  Returns / fills a dict: grad_hidden [B, K, dim], grad_weight [V, dim], of the head's type."""
-        hd, w = self._hidden(hidden, "hidden"), self._weight(weight, "weight")
         B, K, _ = hidden.shape
         if out is None:
-            with _allocating_on(stream):
-                out = dict(grad_hidden=torch.empty((B, K, self.dim), dtype=self.dtype, device=self.device),
-                           grad_weight=torch.empty((weight.shape[0], self.dim), dtype=self.dtype, device=self.device))
+            out = dict(grad_hidden=_empty((B, K, self.dim), self.dtype, self.device, stream),
+                       grad_weight=_empty((weight.shape[0], self.dim), self.dtype, self.device, stream))
+        st = _fast.head_loss_grad(self._addr, self.dim, self.cfg.dtype, self.cfg.device, hidden, weight, target, lse, row_weight, scale,
+                                  out["grad_hidden"], out["grad_weight"], _handle(stream))
+        if st == 0:
+            return out
+        hd, w = self._hidden(hidden, "hidden"), self._weight(weight, "weight")
         gh, gw = self._hidden(out["grad_hidden"], "grad_hidden"), self._weight(out["grad_weight"], "grad_weight")
         if tuple(out["grad_hidden"].shape) != tuple(hidden.shape) or out["grad_weight"].shape[0] != weight.shape[0]:
             raise ValueError("grad_hidden and grad_weight must have the shapes of hidden and weight")
         for t, n in ((target, "target"), (lse, "lse"), (row_weight, "row_weight"), (scale, "scale")):
             _on(t, self.device, n)
         f32 = torch.float32
-        self._check(self._lib.tapout_head_loss_grad(
+        self._check(st if st is not None else self._lib.tapout_head_loss_grad(
             self._head, C.byref(hd), C.byref(w), B, K, weight.shape[0], _ptr(target, torch.int32, (B, K), "target"),
             _ptr(lse, f32, (B, K), "lse"), _ptr(row_weight, f32, (B, K), "row_weight"), _ptr(scale, f32, (1,), "scale"),
-            C.byref(gh), C.byref(gw), _stream(stream)))
+            C.byref(gh), C.byref(gw), self._on_stream(stream)))
         return out

@@ -128,11 +128,18 @@ template <class T, class E> hipError_t logits_with(const LogitsArgs &a, hipStrea
 
 template <class E> hipError_t logits_of(const LogitsArgs &a, int kind, hipStream_t st)
 {
+    // the smallest tile that holds the tokens, long in I where they are many; V = 128256, dim = 2048, us with tiles of 128 x 16 / 128 x 32 /
+    // 128 x 64 / 256 x 128 / 256 x 256: 1 row 22 / 23 / 24 / 25 / 34, 32 rows 33 / 24 / 26 / 28 / 36, 64 rows 60 / 35 / 28 / 29 / 38,
+    // 128 rows 109 / 62 / 42 / 35 / 40, 192 rows 153 / 90 / 62 / 55 / 44, 512 rows 403 / 229 / 157 / 119 / 96
     if (kind == kTileMx4)
-        return a.N <= 32 ? logits_with<Tile<kTileMx4, 128, 32, 4, 1>, E>(a, st)
-             : a.N <= 256 ? logits_with<Tile<kTileMx4, 128, 128, 2, 2>, E>(a, st) : logits_with<Tile<kTileMx4, 256, 256, 2, 4>, E>(a, st);
-    return a.N <= 32 ? logits_with<Tile<kTileMx4W, 128, 32, 4, 1>, E>(a, st)
-         : a.N <= 64 ? logits_with<Tile<kTileMx4W, 128, 64, 4, 1>, E>(a, st) : logits_with<Tile<kTileMx4W, 128, 128, 2, 2>, E>(a, st);
+        return a.N <= 16 ? logits_with<Tile<kTileMx4, 128, 16, 4, 1>, E>(a, st) : a.N <= 32 ? logits_with<Tile<kTileMx4, 128, 32, 4, 1>, E>(a, st)
+             : a.N <= 64 ? logits_with<Tile<kTileMx4, 128, 64, 4, 1>, E>(a, st) : a.N <= 128 ? logits_with<Tile<kTileMx4, 256, 128, 4, 2>, E>(a, st)
+             : logits_with<Tile<kTileMx4, 256, 256, 2, 4>, E>(a, st);
+    // hidden states of 16 bits: they pass through LDS with the weights, four times their bytes for a row each, so tiles are long in I; V = 128256,
+    // dim = 2048, us with tiles of 128 x 16 / 256 x 32 / 256 x 64 / 256 x 128: 1 row 27 / 28 / 36 / 55, 32 rows 45 / 30 / 36 / 52, 64 rows
+    // 81 / 51 / 39 / 55, 128 rows 150 / 93 / 68 / 59, 512 rows 572 / 354 / 272 / 217 (128 x 128: 304)
+    return a.N <= 16 ? logits_with<Tile<kTileMx4W, 128, 16, 4, 1>, E>(a, st) : a.N <= 32 ? logits_with<Tile<kTileMx4W, 256, 32, 8, 1>, E>(a, st)
+         : a.N <= 64 ? logits_with<Tile<kTileMx4W, 256, 64, 8, 1>, E>(a, st) : logits_with<Tile<kTileMx4W, 256, 128, 4, 2>, E>(a, st);
 }
 
 }  // namespace

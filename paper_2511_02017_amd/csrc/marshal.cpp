@@ -6,6 +6,7 @@
 // a tensor subclass, a wrong shape or device, a missing output) it returns None before anything is called, and the Python
 // code, which describes errors, takes over.  No results, addresses or tensors are kept.
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 
@@ -24,6 +25,12 @@ struct Library {
     decltype(&tapout_verify_accept_sharded) verify_accept_sharded;
     decltype(&tapout_shard_final_sums) shard_final_sums;
     decltype(&tapout_shard_final_token) shard_final_token;
+    // the draft head's; a library without them keeps the rest, and these calls go the Python way
+    decltype(&tapout_mx4_quantize) mx4_quantize;
+    decltype(&tapout_mx4_dequantize) mx4_dequantize;
+    decltype(&tapout_head_logits_mx4) head_logits;
+    decltype(&tapout_head_loss) head_loss;
+    decltype(&tapout_head_loss_grad) head_loss_grad;
 } g_lib = {};
 
 constexpr auto kF32 = at::kFloat, kF64 = at::kDouble, kI32 = at::kInt, kU8 = at::kByte;
@@ -99,10 +106,49 @@ struct Args {
         if (!p) ok = false;
         return (tapout_ctx *)p;
     }
+    // a matrix with contiguous rows
+    tapout_matrix matrix(PyObject *o, int64_t *rows, int64_t *cols)
+    {
+        tapout_matrix m = {};
+        const at::Tensor *t = tensor(o);
+        if (!t || t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1)) { ok = false; return m; }
+        if (t->scalar_type() == kF32) m.dtype = TAPOUT_F32;
+        else if (t->scalar_type() == at::kBFloat16) m.dtype = TAPOUT_BF16;
+        else { ok = false; return m; }
+        m.ptr = t->data_ptr(); m.stride = t->size(0) > 1 ? t->stride(0) : t->size(1);
+        *rows = t->size(0); *cols = t->size(1);
+        if (*rows > INT32_MAX || *cols > INT32_MAX) ok = false;
+        return m;
+    }
+    // hidden states [B, K, dim] of a type; the stride of an axis of one entry says nothing
+    tapout_logits hidden(PyObject *o, int64_t dim, int64_t dtype, int64_t *B, int64_t *K)
+    {
+        int64_t D = 0;
+        tapout_logits l = logits(o, B, K, &D);
+        if (D != dim || l.dtype != dtype) ok = false;
+        if (*B <= 1) l.stride_b = 0;
+        if (*K <= 1) l.stride_k = 0;
+        return l;
+    }
+    // every tensor there is lives on this device
+    void device(int64_t index, std::initializer_list<PyObject *> tensors)
+    {
+        for (PyObject *o : tensors) {
+            if (!ok || !o || o == Py_None) continue;
+            const at::Tensor *t = tensor(o);
+            if (t && t->device().index() != index) ok = false;
+        }
+    }
     PyObject *dict(PyObject *o)
     {
         if (!ok || !PyDict_CheckExact(o)) ok = false;
         return o;
+    }
+    // None: the current stream of the current device, which has to be `dev`
+    void *stream_on(int64_t dev, PyObject *o)
+    {
+        if (o == Py_None && c10::hip::current_device() != dev) ok = false;
+        return stream(o);
     }
     // None: the current stream of the current device
     void *stream(PyObject *o)
@@ -355,6 +401,95 @@ PyObject *shard_final_token(PyObject *const *p)
     return call(a, [&] { return g_lib.shard_final_token(c, &t, &d, (int32_t)B, (int32_t)(K1 - 1), (int32_t)V, off, (int32_t)G, g, jobs, sums, exact, u, tok, mass, need, st); });
 }
 
+int64_t codes_cols(int64_t cols) { return (cols + 127) / 128 * 128; }
+
+// (x, codes, scales, stream)
+PyObject *mx4_quantize(PyObject *const *p)
+{
+    Args a;
+    int64_t rows = 0, cols = 0;
+    const tapout_matrix x = a.matrix(p[0], &rows, &cols);
+    a.device(c10::hip::current_device(), {p[0], p[1], p[2]});
+    const int64_t P = codes_cols(cols);
+    uint8_t *codes = a.required<uint8_t>(p[1], kU8, {rows, P / 2}), *scales = a.required<uint8_t>(p[2], kU8, {rows, P / 32});
+    void *st = a.stream(p[3]);
+    if (!g_lib.mx4_quantize) a.ok = false;
+    return call(a, [&] { return g_lib.mx4_quantize(&x, (int32_t)rows, (int32_t)cols, codes, scales, st); });
+}
+
+// (codes, scales, cols, out, stream)
+PyObject *mx4_dequantize(PyObject *const *p)
+{
+    Args a;
+    int64_t rows = 0, cols = 0;
+    const tapout_matrix out = a.matrix(p[3], &rows, &cols);
+    a.device(c10::hip::current_device(), {p[0], p[1], p[3]});
+    if (cols != a.i32(p[2])) a.ok = false;
+    const int64_t P = codes_cols(cols);
+    uint8_t *codes = a.required<uint8_t>(p[0], kU8, {rows, P / 2}), *scales = a.required<uint8_t>(p[1], kU8, {rows, P / 32});
+    void *st = a.stream(p[4]);
+    if (!g_lib.mx4_dequantize) a.ok = false;
+    return call(a, [&] { return g_lib.mx4_dequantize(codes, scales, (int32_t)rows, (int32_t)cols, &out, st); });
+}
+
+// (head, dim, dtype, device, hidden, codes, scales, k_len, act_bits, out, stream)
+PyObject *head_logits(PyObject *const *p)
+{
+    Args a;
+    tapout_head *h = (tapout_head *)a.ctx(p[0]);
+    const int64_t dim = a.i32(p[1]), dtype = a.i32(p[2]), dev = a.i32(p[3]);
+    a.device(dev, {p[4], p[5], p[6], p[7], p[9]});
+    int64_t B = 0, K = 0, Bo = 0, Ko = 0, V = 0;
+    const tapout_logits x = a.hidden(p[4], dim, dtype, &B, &K), out = a.logits(p[9], &Bo, &Ko, &V);
+    if (Bo != B || Ko != K) a.ok = false;
+    const int64_t P = codes_cols(dim);
+    const uint8_t *codes = a.required<uint8_t>(p[5], kU8, {V, P / 2}), *scales = a.required<uint8_t>(p[6], kU8, {V, P / 32});
+    const int32_t *k_len = a.ptr<int32_t>(p[7], kI32, {B});
+    const int32_t act = a.i32(p[8]);
+    void *st = a.stream_on(dev, p[10]);
+    if (!g_lib.head_logits) a.ok = false;
+    return call(a, [&] { return g_lib.head_logits(h, &x, codes, scales, (int32_t)B, (int32_t)K, (int32_t)V, k_len, act, &out, st); });
+}
+
+// (head, dim, dtype, device, hidden, weight, target, out, stream)
+PyObject *head_loss(PyObject *const *p)
+{
+    Args a;
+    tapout_head *h = (tapout_head *)a.ctx(p[0]);
+    const int64_t dim = a.i32(p[1]), dtype = a.i32(p[2]), dev = a.i32(p[3]);
+    int64_t B = 0, K = 0, V = 0, D = 0;
+    const tapout_logits x = a.hidden(p[4], dim, dtype, &B, &K);
+    const tapout_matrix w = a.matrix(p[5], &V, &D);
+    if (D != dim || w.dtype != dtype) a.ok = false;
+    const int32_t *target = a.required<int32_t>(p[6], kI32, {B, K});
+    PyObject *out = a.dict(p[7]);
+    if (!a.ok) Py_RETURN_NONE;
+    float *loss = a.need<float>(out, "loss", kF32, {B, K}), *lse = a.need<float>(out, "lse", kF32, {B, K});
+    uint32_t *flags = a.out<uint32_t>(out, "flags", kI32, {B});
+    a.device(dev, {p[4], p[5], p[6], PyDict_GetItemString(out, "loss"), PyDict_GetItemString(out, "lse"), PyDict_GetItemString(out, "flags")});
+    void *st = a.stream_on(dev, p[8]);
+    if (!g_lib.head_loss) a.ok = false;
+    return call(a, [&] { return g_lib.head_loss(h, &x, &w, (int32_t)B, (int32_t)K, (int32_t)V, target, loss, lse, flags, st); });
+}
+
+// (head, dim, dtype, device, hidden, weight, target, lse, row_weight, scale, grad_hidden, grad_weight, stream)
+PyObject *head_loss_grad(PyObject *const *p)
+{
+    Args a;
+    tapout_head *h = (tapout_head *)a.ctx(p[0]);
+    const int64_t dim = a.i32(p[1]), dtype = a.i32(p[2]), dev = a.i32(p[3]);
+    a.device(dev, {p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11]});
+    int64_t B = 0, K = 0, V = 0, D = 0, Bg = 0, Kg = 0, Vg = 0, Dg = 0;
+    const tapout_logits x = a.hidden(p[4], dim, dtype, &B, &K), gh = a.hidden(p[10], dim, dtype, &Bg, &Kg);
+    const tapout_matrix w = a.matrix(p[5], &V, &D), gw = a.matrix(p[11], &Vg, &Dg);
+    if (D != dim || w.dtype != dtype || Dg != dim || gw.dtype != dtype || Bg != B || Kg != K || Vg != V) a.ok = false;
+    const int32_t *target = a.required<int32_t>(p[6], kI32, {B, K});
+    const float *lse = a.required<float>(p[7], kF32, {B, K}), *rw = a.ptr<float>(p[8], kF32, {B, K}), *scale = a.ptr<float>(p[9], kF32, {1});
+    void *st = a.stream_on(dev, p[12]);
+    if (!g_lib.head_loss_grad) a.ok = false;
+    return call(a, [&] { return g_lib.head_loss_grad(h, &x, &w, (int32_t)B, (int32_t)K, (int32_t)V, target, lse, rw, scale, &gh, &gw, st); });
+}
+
 // load(path): the entry points of this build of the library
 PyObject *load(PyObject *, PyObject *arg)
 {
@@ -374,6 +509,8 @@ PyObject *load(PyObject *, PyObject *arg)
     get(l.verify_accept_sharded, "tapout_verify_accept_sharded"); get(l.shard_final_sums, "tapout_shard_final_sums");
     get(l.shard_final_token, "tapout_shard_final_token");
     if (!ok) { PyErr_Format(PyExc_ImportError, "%s lacks an entry point", path); return nullptr; }
+    get(l.mx4_quantize, "tapout_mx4_quantize"); get(l.mx4_dequantize, "tapout_mx4_dequantize"); get(l.head_logits, "tapout_head_logits_mx4");
+    get(l.head_loss, "tapout_head_loss"); get(l.head_loss_grad, "tapout_head_loss_grad");
     g_lib = l;
     Py_RETURN_NONE;
 }
@@ -394,6 +531,7 @@ PyMethodDef g_methods[] = {
     {"load", load, METH_O, nullptr}, {"current_stream", current_stream, METH_NOARGS, nullptr},
     ENTRY(bandit_select, 8), ENTRY(draft_stats, 9), ENTRY(verify, 12), ENTRY(bandit_update, 9), ENTRY(bandit_update_select, 13),
     ENTRY(shard_stats, 8), ENTRY(draft_stats_sharded, 11), ENTRY(verify_accept_sharded, 13), ENTRY(shard_final_sums, 6), ENTRY(shard_final_token, 14),
+    ENTRY(mx4_quantize, 4), ENTRY(mx4_dequantize, 5), ENTRY(head_logits, 11), ENTRY(head_loss, 9), ENTRY(head_loss_grad, 13),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

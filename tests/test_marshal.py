@@ -176,3 +176,15 @@ def test_streams_views_and_parameters():
     for got in (a, b, c):
         assert torch.equal(got["top1_id"], want["top1_id"])
         assert torch.allclose(got["lse"], want["lse"], rtol=0, atol=1e-5) and torch.allclose(got["logq_tok"], want["logq_tok"], rtol=0, atol=1e-5)
+
+
+def test_the_draft_heads_arguments_that_are_not_in_order_go_to_the_python_code():
+    binding.load_library()
+    fast = binding._fast
+    h, w, t, c = torch.zeros(2, 3, 64), torch.zeros(8, 64), torch.zeros(2, 3, dtype=i32), torch.zeros(8, 64, dtype=u8)
+    assert fast.mx4_quantize(w, c, c, None) is None                                 # not on a GPU
+    assert fast.mx4_dequantize(c, c, 64, w, None) is None
+    assert fast.head_logits(1, 64, 0, 0, h, c, c, None, 16, h, None) is None
+    assert fast.head_loss(1, 64, 0, 0, h, w, t, {}, None) is None
+    assert fast.head_loss_grad(1, 64, 0, 0, h, w, t, h, None, None, h, w, None) is None
+    assert fast.head_loss(0, 64, 0, 0, h, w, t, {}, None) is None and fast.mx4_quantize() is None
