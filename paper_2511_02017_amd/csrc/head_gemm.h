@@ -505,6 +505,22 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
     }
 };
 
+// Row and column of element base + off, base the same for the workgroup and off below 2^16, of rows of `per`: one long division for the
+// workgroup, none for a lane (a division each was what quantising took longest for).
+struct RowColumn {
+    int r, c;
+    __device__ __forceinline__ RowColumn(int64_t base, int off, int per)
+    {
+        const int64_t r0 = base / per;
+        const int in = (int)(base - r0 * per) + off;
+        int q = (int)((float)in * (1.f / (float)per));         // off by less than one: in < 2^17
+        if (q * per > in) --q;
+        if ((q + 1) * per <= in) ++q;
+        r = (int)r0 + q;
+        c = in - q * per;
+    }
+};
+
 constexpr int kCUs = 256;
 // Workgroups of a launch: as many as are resident at once.
 template <class T> inline int grid_of(int64_t tiles) { return (int)(tiles < (int64_t)kCUs * T::per_cu ? tiles : (int64_t)kCUs * T::per_cu); }

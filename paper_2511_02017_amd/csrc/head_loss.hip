@@ -248,9 +248,8 @@ __global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a,
 template <class E>
 __global__ __launch_bounds__(256) void head_grad_hidden_kernel(GradHiddenArgs a)
 {
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int per = a.D / 4;
-    const int n = (int)(x / per), d = (int)(x % per) * 4;
+    const RowColumn at((int64_t)blockIdx.x * 256, threadIdx.x, a.D / 4);
+    const int n = at.r, d = at.c * 4;
     if (n >= a.N) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (row_counts(a.target[n], a.V, a.lse, a.row_weight, n)) {
@@ -279,9 +278,8 @@ template <class E>
 __global__ __launch_bounds__(256) void head_pack_kernel(PackArgs a)
 {
     constexpr int V16 = 16 / sizeof(E);
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int per = a.cols / V16;
-    const int n = (int)(x / per), c = (int)(x % per) * V16;
+    const RowColumn at((int64_t)blockIdx.x * 256, threadIdx.x, a.cols / V16);
+    const int n = at.r, c = at.c * V16;
     if (n < a.N) *(u32x4 *)((E *)a.dst + (int64_t)n * a.cols + c) = *(const u32x4 *)((const E *)a.src + (n / a.K) * a.stride_b + (n % a.K) * a.stride_k + c);
 }
 
