@@ -659,7 +659,9 @@ TAPOUT_API tapout_status tapout_profile_read(tapout_ctx *ctx, int32_t kind, doub
  * Layout.  Hidden states are [B,K,dim] with the last axis contiguous, weights
  * [V,dim] with contiguous rows; strides are in elements.  Unlike logits, they must be
  * 16-byte aligned, strides included (TAPOUT_EINVAL otherwise), and dim must be a
- * multiple of 32.  Row strides of weights are at most 8 MiB.
+ * multiple of 32.  Row strides of weights are at most 8 MiB, max_rows * dim at
+ * most 2^33 and vocab * dim at most 2^35.  Products of binary32 inputs have the
+ * error of binary32 sums; magnitudes from 3.39e38 on count as infinite.
  */
 typedef struct tapout_head tapout_head;
 
@@ -699,7 +701,8 @@ TAPOUT_API const char *tapout_head_last_error(const tapout_head *head);
  *           2n in the low half of byte n; 16-byte aligned
  *   scales  [rows, P / 32] u8, 4-byte aligned
  * tapout_mx4_quantize writes the columns behind cols as zeros (scale byte 0).
- * cols: a multiple of 32; x and out 16-byte aligned, strides included.
+ * cols: a multiple of 32 up to 65536, rows * P at most 2^34; x and out 16-byte
+ * aligned, strides included.
  * tapout_mx4_dequantize writes the values that codes stand for, which are exact
  * in either type (magnitudes beyond its range: infinite).
  */

@@ -18,6 +18,7 @@ struct LossArgs {
     int32_t N, V, D, rows_per_seq, B;
     const int32_t *target;       // [N]
     float2 *part;                // [N, blocks]: maximum and sum of exp(z - maximum) over a wavefront's vocabulary rows
+    int64_t part_cap;            // elements it has room for; a launch that needs more is refused
     float *target_logit;         // [N]
     float *loss, *lse;           // [N]
     uint32_t *flags;             // [B] or NULL
@@ -57,8 +58,8 @@ struct ProductArgs {
     const float *scale;          // device, or NULL (1)
 };
 hipError_t launch_head_product(const ProductArgs &a, int dtype, hipStream_t st);
-int head_product_tiles(int ni, int nj, int dtype);       // tiles of one run, and workgroups resident at a time
-int head_product_slots(int nj, int dtype);
+int head_product_tiles(int ni, int nj, int dtype);       // tiles of one run of the turned product
+int head_product_slots(int nj, int dtype);               // its workgroups resident at a time
 
 // grad_hidden = scale * (sum of the partial sums), rows that do not count: zeros.
 struct GradHiddenArgs {

@@ -11,7 +11,7 @@ using namespace tapout;
 
 struct tapout_head {
     tapout_head_config cfg;
-    float2 *part = nullptr;              // [N, blocks of a wavefront's vocabulary rows]: at least 64 of them, 32 up to N = 64
+    float2 *part = nullptr;  size_t part_cap = 0;             // [N, blocks of a wavefront's vocabulary rows]: at least 64 of them, 32 up to N = 64
     float *target_logit = nullptr;       // [max_rows]
     void *packed = nullptr;              // [max_rows, dim]: hidden states whose rows lie unevenly
     uint8_t *act_codes = nullptr, *act_scales = nullptr;      // quantised hidden states (bfloat16 heads)
@@ -25,6 +25,7 @@ struct tapout_head {
 namespace {
 
 constexpr int kMaxRows = 1 << 20, kMaxDim = 65536, kMaxVocab = 1 << 24;
+constexpr int64_t kMaxHidden = 1ll << 33, kMaxWeights = 1ll << 35, kMaxBlocks = 1ll << 34;      // elements: a grid has fewer than 2^32 lanes
 constexpr int64_t kMaxRowBytes = 8 << 20;            // 255 rows of a tile lie within 2^31 bytes
 constexpr size_t kPieceBytes = (size_t)1 << 30;
 thread_local char g_err[256] = {0};
@@ -126,6 +127,8 @@ tapout_status tapout_head_create(tapout_head **out, const tapout_head_config *cf
     if (cfg->vocab < 1 || cfg->vocab > kMaxVocab) return fail(nullptr, TAPOUT_EINVAL, "vocab = %d outside [1, %d]", cfg->vocab, kMaxVocab);
     if (cfg->dtype != TAPOUT_F32 && cfg->dtype != TAPOUT_BF16) return fail(nullptr, TAPOUT_EINVAL, "unknown dtype %d", cfg->dtype);
     if (cfg->training != 0 && cfg->training != 1) return fail(nullptr, TAPOUT_EINVAL, "training must be 0 or 1");
+    if ((int64_t)cfg->max_rows * cfg->dim > kMaxHidden) return fail(nullptr, TAPOUT_EUNSUPPORTED, "max_rows * dim beyond 2^33");
+    if ((int64_t)cfg->vocab * cfg->dim > kMaxWeights) return fail(nullptr, TAPOUT_EUNSUPPORTED, "vocab * dim beyond 2^35");
     int ndev = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || cfg->device < 0 || cfg->device >= ndev)
         return fail(nullptr, TAPOUT_EHIP, "device %d not available (%d HIP devices)", cfg->device, ndev);
@@ -135,7 +138,8 @@ tapout_status tapout_head_create(tapout_head **out, const tapout_head_config *cf
     DeviceGuard guard(cfg->device);
     const size_t N = cfg->max_rows, D = cfg->dim, esz = size_of(cfg->dtype), P = mx4_cols(cfg->dim);
     const size_t blocks = (cfg->vocab + 127) / 128;
-    bool ok = hipMalloc(&h->part, (N + std::min<size_t>(N, 64)) * 2 * blocks * sizeof(float2)) == hipSuccess
+    h->part_cap = (N + std::min<size_t>(N, 64)) * 2 * blocks;
+    bool ok = hipMalloc(&h->part, h->part_cap * sizeof(float2)) == hipSuccess
            && hipMalloc(&h->target_logit, N * sizeof(float)) == hipSuccess
            && hipMalloc(&h->packed, N * D * esz) == hipSuccess;
     if (ok && cfg->dtype == TAPOUT_BF16)
@@ -172,6 +176,7 @@ tapout_status tapout_mx4_quantize(const tapout_matrix *x, int32_t rows, int32_t 
 {
     if (rows < 0) return fail(nullptr, TAPOUT_EINVAL, "rows = %d is negative", rows);
     if (cols < 32 || cols % 32 || cols > kMaxDim) return fail(nullptr, TAPOUT_EINVAL, "cols = %d is not a multiple of 32 in [32, %d]", cols, kMaxDim);
+    if ((int64_t)rows * mx4_cols(cols) > kMaxBlocks) return fail(nullptr, TAPOUT_EUNSUPPORTED, "rows * cols beyond 2^34");
     if (rows == 0) return TAPOUT_OK;
     if (tapout_status st = check_matrix(nullptr, x, "x")) return st;
     if (!codes || !scales) return fail(nullptr, TAPOUT_EINVAL, "codes or scales is NULL");
@@ -185,6 +190,7 @@ tapout_status tapout_mx4_dequantize(const uint8_t *codes, const uint8_t *scales,
 {
     if (rows < 0) return fail(nullptr, TAPOUT_EINVAL, "rows = %d is negative", rows);
     if (cols < 32 || cols % 32 || cols > kMaxDim) return fail(nullptr, TAPOUT_EINVAL, "cols = %d is not a multiple of 32 in [32, %d]", cols, kMaxDim);
+    if ((int64_t)rows * mx4_cols(cols) > kMaxBlocks) return fail(nullptr, TAPOUT_EUNSUPPORTED, "rows * cols beyond 2^34");
     if (rows == 0) return TAPOUT_OK;
     if (tapout_status st = check_matrix(nullptr, out, "out")) return st;
     if (out->stride < cols && rows > 1) return fail(nullptr, TAPOUT_EINVAL, "out: rows overlap");
@@ -248,7 +254,7 @@ tapout_status tapout_head_loss(tapout_head *h, const tapout_logits *hidden, cons
     const int esz = size_of(h->cfg.dtype);
     a.weight = Operand{weight->ptr, weight->stride * esz, V, h->cfg.dim * esz, nullptr, 0};
     a.N = B * K; a.V = V; a.D = h->cfg.dim; a.rows_per_seq = K; a.B = B;
-    a.target = target; a.part = h->part; a.target_logit = h->target_logit; a.loss = loss; a.lse = lse; a.flags = flags;
+    a.target = target; a.part = h->part; a.part_cap = (int64_t)h->part_cap; a.target_logit = h->target_logit; a.loss = loss; a.lse = lse; a.flags = flags;
     e = launch_head_loss(a, h->cfg.dtype, st);
     return e == hipSuccess ? TAPOUT_OK : hip_fail(h, e, "head_loss");
 }
@@ -287,8 +293,8 @@ tapout_status tapout_head_loss_grad(tapout_head *h, const tapout_logits *hidden,
     const size_t per = piece_bytes(1, N, esz);
     const int most = (int)std::min<size_t>(up_to(V, 256), h->piece_cap / per / 256 * 256);
     const int pieces = (V + most - 1) / most, len = up_to((V + pieces - 1) / pieces, 256);
-    // runs of k of the product by the hidden states: as many as there are workgroups for at a time (two of them a unit: 1503 rows, dim =
-    // 1120 466 us with both products, see below), each long enough to be worth its partial sums
+    // runs of k of the product by the hidden states: as many as there are workgroups for at a time (twice as many: 293 us instead of 192 at
+    // 1503 rows, dim = 1120, V = 50257, bfloat16), each long enough to be worth its partial sums
     const int tiles = head_product_tiles(D, N, dt), stages = up_to(std::min(len, V), 64) / (dt == TAPOUT_F32 ? 32 : 64);
     int splits = std::max(1, std::min({head_product_slots(N, dt) / tiles, stages / 4, (int)(h->grad_cap / ((size_t)N * D))}));
     splits = (stages + (stages + splits - 1) / splits - 1) / ((stages + splits - 1) / splits);        // runs of equal length, none of them empty

@@ -23,7 +23,8 @@ using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
 
 // What the two operands of a product are.
 enum TileKind {
-    kTileF32,    // both binary32
+    kTileF32,    // both binary32, multiplied as they are
+    kTileF32x3,  // both binary32, multiplied as sums of three bfloat16 each (see split3)
     kTileBf16,   // both bfloat16
     kTileMx4,    // both 4-bit codes with a scale byte for 32 of them
     kTileMx4W    // I: 4-bit codes with scales; J: bfloat16
@@ -32,7 +33,7 @@ enum TileKind {
 // Bytes of an operand's row in a stage, elements of k in a stage, and matrix steps: a step takes 64 bytes of each of 16 I rows
 // (16 a lane).
 template <int KIND> struct Kind {
-    static constexpr int elems = KIND == kTileF32 ? 32 : KIND == kTileBf16 ? 64 : KIND == kTileMx4 ? 256 : 128;
+    static constexpr int elems = KIND == kTileF32 || KIND == kTileF32x3 ? 32 : KIND == kTileBf16 ? 64 : KIND == kTileMx4 ? 256 : 128;
     static constexpr int row_i = KIND == kTileMx4W ? 64 : 128;
     static constexpr int row_j = KIND == kTileMx4W ? 256 : 128;
     static constexpr int steps = row_i / 64;
@@ -76,7 +77,7 @@ template <int NJ> __device__ __forceinline__ int row_of_j(int q) { return q / (1
 template <int NJ> __device__ __forceinline__ int tile_row(int q) { if constexpr (NJ == 0) return row_of_i(q); else return row_of_j<NJ>(q); }
 
 // A wavefront's load of 64 x 16 bytes into LDS.  HIDDEN: not as the builtin, whose loads the compiler takes to be meant by every turning
-// read that follows, and waits for (the product by 1503 hidden states 754 instead of 250 us).  There are no registers to be written;
+// read that follows, and waits for (the product by 1503 hidden states 754 instead of 293 us).  There are no registers to be written;
 // this wavefront and the others wait by number, below.  M0 needs no saving: a kernel that loads so has no other use for it.
 template <bool HIDDEN> __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t off, uint32_t from)
 {
@@ -150,6 +151,29 @@ __device__ __forceinline__ f32x4 mma_f32(u32x4 a, u32x4 b, f32x4 c)
 __device__ __forceinline__ f32x4 mma_bf16(u32x4 a, u32x4 b, f32x4 c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// Eight binary32 as three bfloat16 each, x = h + m + l: each part is what is left, rounded to nearest and taken off exactly, and 24 bits
+// are three times eight, so nothing is left behind l.  With |m| <= 2^-8 |x| and |l| <= 2^-16 |x|, the three smallest of the nine products
+// of two such sums are below 2^-23 |x y| together, and like a rounding of the product either way; they are left out.  Six bfloat16
+// products take 96 cycles of the matrix unit for 16 x 16 x 32, the binary32 ones 256.  An infinity becomes a NaN here,
+// and so does what bfloat16 rounds to one (3.39e38 on).
+struct Split3 { u32x4 h, m, l; };
+__device__ __forceinline__ Split3 split3(u32x4 a, u32x4 b)
+{
+    Split3 r;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float x = __uint_as_float(q < 2 ? a[2 * q] : b[2 * q - 4]), y = __uint_as_float(q < 2 ? a[2 * q + 1] : b[2 * q - 3]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const bf16x2 v = {(__bf16)x, (__bf16)y};
+            const uint32_t w = __builtin_bit_cast(uint32_t, v);
+            (p == 0 ? r.h : p == 1 ? r.m : r.l)[q] = w;
+            x -= __uint_as_float(w << 16);
+            y -= __uint_as_float(w & 0xffff0000u);
+        }
+    }
+    return r;
 }
 __device__ __forceinline__ f32x4 mma_mx4(u32x4 a, uint32_t sa, u32x4 b, uint32_t sb, f32x4 c)
 {
@@ -242,8 +266,9 @@ struct Work { int i0, j0, first, n; };
 // TURNED: I lies with its columns contiguous; results of one lane are then four neighbours in I only.
 template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> struct Tile {
     using K = Kind<KIND>;
-    static_assert(!TURNED || KIND == kTileF32 || KIND == kTileBf16, "");
-    static constexpr int esz = KIND == kTileF32 ? 4 : 2;
+    static_assert(!TURNED || KIND == kTileF32 || KIND == kTileF32x3 || KIND == kTileBf16, "");
+    static constexpr int esz = KIND == kTileF32 || KIND == kTileF32x3 ? 4 : 2;
+    static constexpr bool split = KIND == kTileF32x3;
     static constexpr bool turned = TURNED;
     static constexpr int kind = KIND, TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, NW = WI * WJ, threads = NW * 64;
     static constexpr int MI = TI / WI / 16, NJ = TJ / WJ / 16;
@@ -251,7 +276,7 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
     static constexpr int up256(int n) { return (n + 255) & ~255; }
     static constexpr int oSI = TI * K::row_i, bytes_i = oSI + up256(TI * K::scale_i);
     static constexpr int oSJ = TJ * K::row_j, bytes_j = oSJ + up256(TJ * K::scale_j);
-    static constexpr int ring_i = KIND == kTileMx4 ? 2 : 3, ring_j = 2, ring_bytes = ring_i * bytes_i + ring_j * bytes_j;
+    static constexpr int ring_i = KIND == kTileMx4 || KIND == kTileF32x3 ? 2 : 3, ring_j = 2, ring_bytes = ring_i * bytes_i + ring_j * bytes_j;
     static constexpr int per_cu = 163840 / ring_bytes < 1 ? 1 : 163840 / ring_bytes > 2048 / threads ? 2048 / threads : 163840 / ring_bytes;
     using Acc = f32x4[MI][NJ];
     using StagerI = std::conditional_t<TURNED, TurnedStager<TI, K::elems, esz, NW>, Stager<TI, K::row_i, 16, NW, 0>>;
@@ -271,7 +296,7 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
 
     // What a wavefront multiplies: blocks of I (those of the next step replace them one by one), and of J for two steps.
     struct Frags {
-        u32x4 a[KIND == kTileMx4W ? 2 : 1][MI], b[2][NJ];
+        u32x4 a[KIND == kTileMx4W || split ? 2 : 1][MI], b[2][NJ];
         uint32_t sa[KIND == kTileMx4W ? 2 : 1][K::scale_i ? MI : 1], sb[2][K::scale_j ? NJ : 1];
     };
     // Where this lane reads: its row of the first block, and the chunk of step 0; steps exchange bits of the chunk.
@@ -421,6 +446,12 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
         for (int x = 0; x < NJ; ++x) read_b(0, x, j0p, 0, places, f);
 #pragma unroll
         for (int x = 0; x < MI; ++x) read_a(0, x, i0p, 0, places, f);
+        if constexpr (split) {
+#pragma unroll
+            for (int x = 0; x < NJ; ++x) read_b(1, x, j0p, 1, places, f);
+#pragma unroll
+            for (int x = 0; x < MI; ++x) read_a(1, x, i0p, 1, places, f);
+        }
         int stores = 0;                                          // 1: STORES stores are younger than the loads that are waited for next
         constexpr int steps = KIND == kTileMx4W ? 4 : K::steps, last = steps - 1;
         constexpr int hold = KIND == kTileMx4W || MI < 4 ? 0 : 1;          // the row of blocks behind which a stage is handed on
@@ -492,9 +523,46 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
                 char *p = i0p; i0p = i1p; i1p = ring_i == 3 ? i2p : p; i2p = p;
                 p = j0p; j0p = j1p; j1p = p;
             };
+            // Split products: a stage's operands were read while the stage before multiplied, so the barrier that hands both places on comes
+            // first; J's blocks are split once, I's as their rows come.
+            auto split_stage = [&] {
+                if constexpr (split) {
+                    hand_on();
+                    Split3 b[NJ];
+#pragma unroll
+                    for (int n = 0; n < NJ; ++n) b[n] = split3(f.b[0][n], f.b[1][n]);
+#pragma unroll
+                    for (int mi = 0; mi < MI; ++mi) {
+                        const Split3 a = split3(f.a[0][mi], f.a[1][mi]);
+#pragma unroll
+                        for (int x = mi * lj / MI; x < (mi + 1) * lj / MI; ++x) load_j(x, j0p);
+#pragma unroll
+                        for (int x = mi * li / MI; x < (mi + 1) * li / MI; ++x) load_i(x, i0p);
+#pragma unroll
+                        for (int x = mi * NJ / MI; x < (mi + 1) * NJ / MI; ++x) {
+                            read_b(0, x, j1p, 0, places, f);
+                            read_b(1, x, j1p, 1, places, f);
+                        }
+                        read_a(0, mi, i1p, 0, places, f);
+                        read_a(1, mi, i1p, 1, places, f);
+#pragma unroll
+                        for (int p = 0; p < 6; ++p)               // the smallest products first; neighbouring instructions have sums of their own
+#pragma unroll
+                            for (int n = 0; n < NJ; ++n)
+                                acc[mi][n] = mma_bf16(p == 0 ? a.l : p == 2 || p == 3 ? a.m : a.h, p == 1 ? b[n].l : p == 2 || p == 4 ? b[n].m : b[n].h, acc[mi][n]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    advance();
+                    char *p = i0p; i0p = i1p; i1p = p; i2p = p;
+                    p = j0p; j0p = j1p; j1p = p;
+                }
+            };
             for (int s = 0; s < w.n; ++s) {
-                early_steps();
-                last_step();
+                if constexpr (split) split_stage();
+                else {
+                    early_steps();
+                    last_step();
+                }
             }
             stores = finish(w, acc);
             if (!walk.more()) break;

@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void head_transpose_kernel(TransposeArgs a)
 {
     constexpr int V16 = 16 / sizeof(E), S = 64, L = S + V16 / 2;
     __shared__ __align__(16) E tile[S * L];
-    const int r0 = blockIdx.x * S, c0 = blockIdx.y * S;
+    const int r0 = blockIdx.y * S, c0 = blockIdx.x * S;
     for (int x = threadIdx.x; x < S * (S / V16); x += 256) {
         const int r = x / (S / V16), c = x % (S / V16) * V16;
         E v[V16];
@@ -298,8 +298,8 @@ inline int up(int a, int b) { return (a + b - 1) / b; }
 template <class T> hipError_t loss_with(const LossArgs &a, hipStream_t st)
 {
     using K = Kind<T::kind>;
-    static_assert(T::TI / T::WI >= (T::TJ > 32 ? 64 : 32), "part has room for as many blocks");
     const int ni = up(a.V, T::TI), nj = up(a.N, T::TJ), stages = up(a.D, K::elems);
+    if ((int64_t)a.N * ni * T::WI > a.part_cap) return hipErrorInvalidValue;
     hipError_t e = with_lds<T>((const void *)head_loss_kernel<T>, T::ring_bytes, [&] {
         head_loss_kernel<T><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
     });
@@ -336,18 +336,20 @@ template <int KIND, bool TURNED = false> using Large = Tile<KIND, 256, 256, 2, 4
 // Which tile for how many tokens.  A tile of 32 tokens while more would be empty, of 128 while the vocabulary rows' bytes are what
 // takes the time anyway, else of 256, whose loads serve more products (cross entropy of V = 128256, dim = 2048, bfloat16, us with
 // tiles of 32 / 128 / 256 tokens: 32 rows 113 / 116 / 125, 48 rows 122 / 117 / 125, 128 rows 188 / 117 / 126, 192 rows 244 / 165 / 129,
-// 512 rows 560 / 328 / 220).  binary32 products are so much slower that a tile has to fit, and larger ones gain nothing (V = 32000,
-// dim = 1024: 40 rows 43 / 81 / 243, 128 rows 82 / 84 / 241, 256 rows 159 / 149 / 245).
+// 512 rows 560 / 328 / 220).
+// binary32: products as they are while the tile is nearly empty, three bfloat16 each where the matrix unit sets the pace (V = 32000,
+// dim = 1024, us with 32 native / 128 native / 128 split: 33 rows 44 / 81 / 70, 64 rows 45 / 81 / 70, 128 rows 82 / 85 / 75, 256 rows
+// 159 / 148 / 117, 1000 rows - / 527 / 417, 3000 rows - / 1561 / 1160, which is 169 TFLOP/s of binary32).
 template <template <class> class F, bool TURNED, class A> hipError_t by_tokens(A &&a, int tokens, int dtype, hipStream_t st)
 {
-    if (dtype == TAPOUT_F32) return tokens <= 64 ? F<Small<kTileF32, TURNED>>::launch(a, st) : F<Mid<kTileF32, TURNED>>::launch(a, st);
+    if (dtype == TAPOUT_F32) return tokens <= 64 ? F<Small<kTileF32, TURNED>>::launch(a, st) : F<Mid<kTileF32x3, TURNED>>::launch(a, st);
     return tokens <= 32 ? F<Small<kTileBf16, TURNED>>::launch(a, st)
          : tokens <= 128 ? F<Mid<kTileBf16, TURNED>>::launch(a, st) : F<Large<kTileBf16, TURNED>>::launch(a, st);
 }
 
 template <class T> struct Loss { static hipError_t launch(const LossArgs &a, hipStream_t st) { return loss_with<T>(a, st); } };
-template <class T> struct Grad { static hipError_t launch(const GradArgs &a, hipStream_t st) { return grad_with<T, typename ElemOf<T::kind == kTileF32 ? TAPOUT_F32 : TAPOUT_BF16>::T>(a, st); } };
-template <class T> struct Product { static hipError_t launch(const ProductArgs &a, hipStream_t st) { return product_with<T, typename ElemOf<T::kind == kTileF32 ? TAPOUT_F32 : TAPOUT_BF16>::T>(a, st); } };
+template <class T> struct Grad { static hipError_t launch(const GradArgs &a, hipStream_t st) { return grad_with<T, typename ElemOf<T::esz == 4 ? TAPOUT_F32 : TAPOUT_BF16>::T>(a, st); } };
+template <class T> struct Product { static hipError_t launch(const ProductArgs &a, hipStream_t st) { return product_with<T, typename ElemOf<T::esz == 4 ? TAPOUT_F32 : TAPOUT_BF16>::T>(a, st); } };
 
 }  // namespace
 
@@ -372,7 +374,7 @@ int head_product_tiles(int ni, int nj, int dtype)
 
 hipError_t launch_head_transpose(const TransposeArgs &a, int dtype, hipStream_t st)
 {
-    const dim3 grid(up(a.rows_pad, 64), up(a.cols, 64));
+    const dim3 grid(up(a.cols, 64), up(a.rows_pad, 64));             // cols: up to 2^24, more than a grid's second axis holds
     if (dtype == TAPOUT_F32) head_transpose_kernel<float><<<grid, 256, 0, st>>>(a);
     else head_transpose_kernel<__bf16><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();

@@ -95,6 +95,18 @@ def test_logits_sizes(B, K, V, D, act):
     check_logits(B, K, V, D, act, f32, seed=V + 1)
 
 
+# so many tiles that a workgroup multiplies several, of a stage or two each
+@pytest.mark.parametrize("act,out", [(16, bf16), (16, f32), (4, bf16), (4, f32)])
+@pytest.mark.parametrize("B,K,V,D,lengths", [
+    (5, 1, 300001, 32, False), (2, 8, 300000, 160, True), (31, 1, 150001, 64, False), (8, 4, 150016, 288, False), (5, 10, 150001, 96, False),
+    (64, 1, 100224, 256, True), (13, 9, 70001, 64, False), (64, 2, 70144, 288, False), (300, 1, 70001, 32, False), (64, 4, 70144, 544, False),
+    (30, 10, 70144, 96, True),
+])
+def test_logits_of_many_tiles(B, K, V, D, lengths, act, out):
+    k_len = (torch.arange(B, dtype=torch.int32) % (K + 2)).clamp(max=K).to(DEV) if lengths else None
+    check_logits(B, K, V, D, act, out, seed=V, k_len=k_len)
+
+
 @pytest.mark.parametrize("act", [16, 4])
 @pytest.mark.parametrize("out", [bf16, f32])
 @pytest.mark.parametrize("B,K", [(3, 2), (9, 9), (40, 8)])
@@ -175,6 +187,14 @@ def test_loss_and_gradients(B, K, V, D, dtype):
         within(b["grad_hidden"].reshape(-1, D), dh, bh)
         within(b["grad_weight"], dw, bw)
         assert (b["grad_hidden"].cpu()[t < 0] == 0).all()
+
+
+# one more and one fewer token than a tile is chosen for, over vocabularies of more tiles than run at a time
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("B,K,V,D", [(4, 8, 70001, 64), (33, 1, 40000, 96), (8, 8, 40001, 32), (13, 5, 40001, 96), (16, 8, 35000, 64), (3, 43, 70001, 32),
+                                     (1, 40, 1300, 1120), (5, 17, 1280, 2080), (140, 1, 1111, 1120)])
+def test_loss_and_gradients_over_long_axes(B, K, V, D, dtype):
+    test_loss_and_gradients(B, K, V, D, dtype)
 
 
 @pytest.mark.parametrize("dtype,N,V", [(bf16, 8192, 40000), (f32, 4096, 36000)])
@@ -269,6 +289,32 @@ def test_no_rows():
     assert (b["grad_weight"] == 0).all()
     c, s = binding.mx4_quantize(w)
     assert head.logits(h, c, s).shape == (0, 3, 300)
+
+
+def test_no_rows_and_a_vocabulary_beyond_a_grid_axis():
+    V = 4_200_001
+    head = binding.DraftHead(1, 32, V, training=True)
+    h, t = torch.empty(0, 1, 32, dtype=bf16, device=DEV), torch.empty(0, 1, dtype=torch.int32, device=DEV)
+    w, lse = torch.zeros(V, 32, dtype=bf16, device=DEV), torch.empty(0, 1, device=DEV)
+    gw = torch.ones_like(w)
+    head.loss_grad(h, w, t, lse, out=dict(grad_hidden=torch.empty_like(h), grad_weight=gw))
+    assert not gw.any()
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+def test_one_hidden_state_for_all_rows(dtype):
+    """Strides of zero, of the hidden states and of the weights: as copies of them."""
+    B, K, V, D = 11, 7, 300, 96
+    _, w, t = loss_inputs(B, K, V, D, dtype, seed=12)
+    one = rand(1, 1, D, seed=13, dtype=dtype).to(DEV).expand(B, K, D)
+    head = binding.DraftHead(B * K, D, V, dtype=dtype, training=True)
+    wd, td = w.to(DEV), t.to(DEV)
+    same = wd[:1].expand(V, D)
+    for x, y in ((one, wd), (one, same)):
+        a, b = head.loss(x, y, td), head.loss(x.contiguous(), y.contiguous(), td)
+        assert torch.equal(a["loss"], b["loss"]) and torch.equal(a["lse"], b["lse"])
+        a, b = head.loss_grad(x, y, td, a["lse"]), head.loss_grad(x.contiguous(), y.contiguous(), td, a["lse"])
+        assert torch.equal(a["grad_hidden"], b["grad_hidden"]) and torch.equal(a["grad_weight"], b["grad_weight"])
 
 
 @pytest.mark.parametrize("dtype", [bf16, f32])
@@ -378,6 +424,26 @@ def test_same_bits_on_another_stream_and_in_a_replayed_graph(B, K, V, D):
         same(out, want[k])
         same(all_calls(head, *sets[0], scale), want[0])            # eager work of the same head between the replays
         torch.cuda.synchronize()
+
+
+def test_two_heads_on_two_streams():
+    """Calls of two heads under way at once: each as alone."""
+    B, K, V, D = 8, 16, 3001, 160
+    sets = [[x.to(DEV) for x in loss_inputs(B, K, V, D, bf16, seed=s)] for s in (5, 6)]
+    heads = [binding.DraftHead(B * K, D, V, training=True) for _ in sets]
+    scale = torch.tensor([0.5], device=DEV)
+    want = [all_calls(heads[0], *x, scale) for x in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(6):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(all_calls(heads[i], *sets[i], scale))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for g in got[i]:
+            same(g, want[i])
 
 
 # ---- refusals -------------------------------------------------------------------------------------------------------

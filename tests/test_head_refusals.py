@@ -26,6 +26,24 @@ def test_create_rejects_bad_configurations(change, word):
     assert word in lib.tapout_head_last_error(None).decode()
 
 
+@pytest.mark.parametrize("change,word", [(dict(max_rows=1 << 20, dim=8224), "max_rows"), (dict(vocab=1 << 24, dim=2080), "vocab")])
+def test_create_refuses_more_elements_than_a_grid_has_lanes(change, word):
+    lib = binding.load_library()
+    h = C.c_void_p()
+    assert lib.tapout_head_create(C.byref(h), C.byref(head_config(**change))) == 2 and h.value is None
+    assert word in lib.tapout_head_last_error(None).decode()
+
+
+def test_mx4_calls_refuse_more_elements_than_a_grid_has_lanes():
+    lib = binding.load_library()
+    m = binding.TapoutMatrix(4096, binding.BF16, 65536)
+    rows = (1 << 18) + 1
+    assert lib.tapout_mx4_quantize(C.byref(m), rows, 65536, 4096, 4096, None) == 2
+    assert "2^34" in lib.tapout_head_last_error(None).decode()
+    assert lib.tapout_mx4_dequantize(4096, 4096, rows, 65536, C.byref(m), None) == 2
+    assert "2^34" in lib.tapout_head_last_error(None).decode()
+
+
 def test_null_handles():
     lib = binding.load_library()
     h = C.c_void_p()
