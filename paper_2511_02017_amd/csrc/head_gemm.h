@@ -37,7 +37,6 @@ template <int KIND> struct Kind {
     static constexpr int row_i = KIND == kTileMx4W ? 64 : 128;
     static constexpr int row_j = KIND == kTileMx4W ? 256 : 128;
     static constexpr int steps = row_i / 64;
-    static constexpr int step_elems = elems / steps;
     static constexpr int scale_i = KIND == kTileMx4 || KIND == kTileMx4W ? elems / 32 : 0;     // scale bytes of a row in a stage
     static constexpr int scale_j = KIND == kTileMx4 ? elems / 32 : 0;
 };

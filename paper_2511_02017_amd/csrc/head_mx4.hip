@@ -170,7 +170,9 @@ template <class E> static hipError_t quantize(const QuantArgs &a, hipStream_t st
 {
     const int per = (a.cols + kMx4Pad - 1) / kMx4Pad * kMx4Pad / 8;
     const int64_t groups = (int64_t)a.rows * per;
-    if (groups >= 256 * 4 * 2 * kCUs) mx4_quantize_kernel<E, 4><<<(groups + 1023) / 1024, 256, 0, st>>>(a, per, groups);
+    // four groups a lane where the values come from memory, not from the 256 MiB cache before it (one / four a lane, us, rows of 2048 bfloat16:
+    // 64 rows 2.6 / 4.5, 4096 rows 6.3 / 7.2, 32768 rows 33.2 / 34.3, 65536 rows 64 / 60, 128256 rows 126 / 114; 50257 x 1120 binary32 48.2 / 49.4)
+    if (groups * 8 * (int)sizeof(E) >= 1 << 28) mx4_quantize_kernel<E, 4><<<(groups + 1023) / 1024, 256, 0, st>>>(a, per, groups);
     else mx4_quantize_kernel<E, 1><<<(groups + 255) / 256, 256, 0, st>>>(a, per, groups);
     return hipGetLastError();
 }

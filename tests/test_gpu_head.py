@@ -67,6 +67,21 @@ def test_mx4_rows_strides_and_given_outputs(rows):
     assert (c[:rows, 32:] == 0).all() and (s[:rows, 2:] == 0).all()
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(65539, 2048, bf16), (58301, 1120, f32), (524297, 32, f32)])
+def test_mx4_of_more_values_than_the_caches_hold(rows, cols, dtype):
+    """In one call as in calls of a few thousand rows; the first and last rows as the plain form."""
+    x = (torch.randn(rows, cols, generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV) * 0.02).to(dtype)
+    c, s = binding.mx4_quantize(x)
+    for r in range(0, rows, 8000):
+        c1, s1 = binding.mx4_quantize(x[r:r + 8000])
+        assert torch.equal(c[r:r + 8000], c1) and torch.equal(s[r:r + 8000], s1)
+    v = binding.mx4_dequantize(c, s, cols, dtype=dtype)
+    for part in (slice(0, 40), slice(rows - 40, rows)):
+        code, byte, val = hu.mx4(x[part].cpu())
+        assert torch.equal(hu.unpack(c[part])[:, :code.shape[1]], code) and torch.equal(s[part].cpu().long(), byte.long())
+        assert torch.equal(v[part].cpu().double(), val)
+
+
 # ---- logits under a 4-bit head -----------------------------------------------------------------------------
 def check_logits(B, K, V, D, act, out, seed=0, hidden=None, k_len=None, target=None):
     w = rand(V, D, seed=seed + 1, scale=2.0 / D ** 0.5)
