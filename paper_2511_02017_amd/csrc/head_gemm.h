@@ -2,7 +2,8 @@
 // contiguous.  I is always the long side that is streamed (vocabulary rows, or columns of a gradient), J the tokens.
 //
 // A stage is a piece of k that both operands bring into LDS by the asynchronous global-to-LDS loads (16 bytes a lane, no
-// registers in between); two stages alternate, the next one is under way while the matrix instructions work on this one.
+// registers in between).  I has places for three stages and J for two (both two where three do not fit), so that up to two stages
+// are under way while the matrix instructions work on a third, across the tiles of a workgroup too.
 // Rows of a stage lie behind each other without padding (the loads write 64 x 16 bytes in a row), so the 16-byte chunks of a
 // row are exchanged by an XOR with bits of the row number: the 16 lanes that read one chunk column of 16 rows then meet every
 // bank once.  The exchange is made on the source address, which stays within the row.
