@@ -660,8 +660,8 @@ TAPOUT_API tapout_status tapout_profile_read(tapout_ctx *ctx, int32_t kind, doub
  * [V,dim] with contiguous rows; strides are in elements.  Unlike logits, they must be
  * 16-byte aligned, strides included (TAPOUT_EINVAL otherwise), and dim must be a
  * multiple of 32.  Row strides of weights are at most 8 MiB, max_rows * dim at
- * most 2^33 and vocab * dim at most 2^35.  Products of binary32 inputs have the
- * error of binary32 sums; magnitudes from 3.39e38 on count as infinite.
+ * most 2^33 and vocab * dim at most 2^35.  Products of binary32 inputs may be off
+ * by 2^-21 of themselves each (2^-24 in the mean) before they are summed in binary32.
  */
 typedef struct tapout_head tapout_head;
 

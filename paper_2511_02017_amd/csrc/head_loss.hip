@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256) void head_transpose_kernel(TransposeArgs a)
 // ---- products of the gradient ---------------------------------------------------------------------------
 // dh with the weights turned, its sums in binary32 over runs of the vocabulary; dW at once.  Bound by the matrix unit where rows are many
 // (8192 rows, V = 128256, dim = 2048, bfloat16: dh 3.3 ms, 1.30 PFLOP/s, dW 2.85 ms, 1.51), by dW's own bytes where they are few
-// (40 rows, 32000 x 1024 binary32: 46 us for 131 MB, half of it the splitting of its operands).
+// (40 rows, 32000 x 1024 binary32: 46 us for 131 MB).
 template <class T, class E>
 __global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int per_split, int splits)
 {
@@ -349,8 +349,8 @@ template <int KIND, bool TURNED = false> using Large = Tile<KIND, 256, 256, 2, 4
 // tiles of 32 / 128 / 256 tokens: 32 rows 113 / 116 / 125, 48 rows 122 / 117 / 125, 128 rows 188 / 117 / 126, 192 rows 244 / 165 / 129,
 // 512 rows 560 / 328 / 220).
 // binary32: products as they are while the tile is nearly empty, three bfloat16 each where the matrix unit sets the pace (V = 32000,
-// dim = 1024, us with 32 native / 128 native / 128 split: 33 rows 44 / 81 / 70, 64 rows 45 / 81 / 70, 128 rows 82 / 85 / 75, 256 rows
-// 159 / 148 / 117, 1000 rows - / 527 / 417, 3000 rows - / 1561 / 1160, which is 169 TFLOP/s of binary32).
+// dim = 1024, us with 32 native / 128 native / 128 split: 33 rows 44 / 81 / 65, 64 rows 45 / 81 / 65, 128 rows 82 / 85 / 72, 256 rows
+// 159 / 148 / 103, 1000 rows - / 527 / 375, 3000 rows - / 1561 / 1030, which is 191 TFLOP/s of binary32).
 template <template <class> class F, bool TURNED, class A> hipError_t by_tokens(A &&a, int tokens, int dtype, hipStream_t st)
 {
     if (dtype == TAPOUT_F32) return tokens <= 64 ? F<Small<kTileF32, TURNED>>::launch(a, st) : F<Mid<kTileF32x3, TURNED>>::launch(a, st);
