@@ -668,6 +668,8 @@ typedef struct tapout_head tapout_head;
 typedef struct {
     int32_t device;                       /* HIP device ordinal                                 */
     int32_t max_rows;                     /* largest B * K of any call, at most 2^20            */
+                                          /* (scratch: 8 bytes a row and 64 vocabulary rows,    */
+                                          /* a copy of the hidden states in each form)          */
     int32_t dim;                          /* length of a hidden state: a multiple of 32, at most 65536 */
     int32_t vocab;                        /* largest V of any call, at most 2^24                */
     int32_t dtype;                        /* tapout_dtype of hidden states and weights          */
