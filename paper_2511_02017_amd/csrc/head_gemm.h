@@ -59,7 +59,8 @@ template <int R> __device__ __forceinline__ int chunk_swap(int row)
     else return (row & 3) | (row & 8) | (row & 8) >> 1;                       // one row; lane's chunk 4 (l / 16) + t
 }
 
-// The memory of `bytes` bytes from p on, at most 2^31 - 1 of them: loads of what lies behind bring zeros, into LDS too.
+// The memory of `bytes` bytes from p on, at most 2^31 - 1 of them: loads of what lies behind bring zeros, into LDS too.  The compiler
+// leaves the scalar offset of a buffer load out of what it says of the range check, so the whole address is a lane's offset.
 constexpr uint32_t kNoMemory = 0x80000000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, int64_t bytes)
 {
@@ -77,14 +78,14 @@ template <int NJ> __device__ __forceinline__ int tile_row(int q) { if constexpr 
 // A wavefront's load of 64 x 16 bytes into LDS.  HIDDEN: not as the builtin, whose loads the compiler takes to be meant by every turning
 // read that follows, and waits for (the product by 1503 hidden states 754 instead of 293 us).  There are no registers to be written;
 // this wavefront and the others wait by number, below.  M0 needs no saving: a kernel that loads so has no other use for it.
-template <bool HIDDEN> __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t off, uint32_t from)
+template <bool HIDDEN> __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t off)
 {
     const auto to = (__attribute__((address_space(3))) void *)lds;
     if constexpr (HIDDEN) {
         const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)to);
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(off), "s"(rsrc), "s"(from) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(rsrc) : "memory");
     } else {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, off, from, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, off, 0, 0, 0);
     }
 }
 
@@ -94,21 +95,22 @@ template <bool HIDDEN> __device__ __forceinline__ void load_to_lds(__amdgpu_buff
 template <int T, int R, int W, int NW, int NJ, bool HIDDEN = false> struct Stager {           // NJ = 0: I's rows
     static constexpr int pieces = T * R / (64 * W) < 1 ? 1 : T * R / (64 * W), per = (pieces + NW - 1) / NW, rows = 64 * W / R, lanes = R / W;
     static_assert(pieces % NW == 0 || pieces < NW, "");
-    uint32_t off, now, at;           // of this lane: from the tile's first row; the same, or nowhere; its first byte in a row's R
+    uint32_t off, now, at;           // of this lane: from the tile's first row; the same of a stage, or nowhere; its first byte in a row's R
     __device__ __forceinline__ void init(int64_t stride, int wave, int lane)
     {
         const int q = wave % pieces * rows + lane / lanes;
         at = (uint32_t)((lane % lanes) ^ (W == 16 ? chunk_swap<R>(q) : 0)) * W;
         off = (uint32_t)(tile_row<NJ>(q) * stride) + at;
     }
-    __device__ __forceinline__ void stage(int s, int row_bytes) { now = s * R + (int)at < row_bytes ? off : kNoMemory; }
-    // The row orders exchange bits of a row's number, and the wavefronts' pieces of one n differ in bits of their own.
-    __device__ __forceinline__ void issue(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, int s, int64_t stride, int wave) const
+    __device__ __forceinline__ void stage(int s, int row_bytes) { now = s * R + (int)at < row_bytes ? off + (uint32_t)(s * R) : kNoMemory; }
+    // The row orders exchange bits of a row's number, and the wavefronts' pieces of one n differ in bits of their own.  All rows of a tile lie
+    // within 2^31 bytes, so the sum does not wrap, of a lane that is nowhere either.
+    __device__ __forceinline__ void issue(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, int64_t stride, int wave) const
     {
         char *to = lds + (wave % pieces + n * NW) * (64 * W);
-        const uint32_t from = (uint32_t)(tile_row<NJ>(n * NW * rows) * stride) + (uint32_t)(s * R);
-        if constexpr (W == 16) load_to_lds<HIDDEN>(rsrc, to, now, from);
-        else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)to, 4, now, from, 0, 0);
+        const uint32_t from = now + (uint32_t)(tile_row<NJ>(n * NW * rows) * stride);
+        if constexpr (W == 16) load_to_lds<HIDDEN>(rsrc, to, from);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)to, 4, from, 0, 0, 0);
     }
 };
 // The same of an operand whose rows are steps of k (its columns the rows of I): KS of them, T columns of E bytes each, 16 bytes a lane.
@@ -129,14 +131,14 @@ template <int T, int KS, int E, int NW> struct TurnedStager {
     }
     __device__ __forceinline__ void issue(int n, __amdgpu_buffer_rsrc_t rsrc, char *lds, int64_t stride, int wave) const
     {
-        load_to_lds<E == 2>(rsrc, lds + (wave + n * NW) * 1024, row_off + chunk[NW * rows % 16 ? n & 1 : 0], (uint32_t)(n * NW * rows * stride));
+        load_to_lds<E == 2>(rsrc, lds + (wave + n * NW) * 1024, row_off + chunk[NW * rows % 16 ? n & 1 : 0] + (uint32_t)(n * NW * rows * stride));
     }
 };
 struct NoStager {
     static constexpr int per = 0;
     __device__ __forceinline__ void init(int64_t, int, int) {}
     __device__ __forceinline__ void stage(int, int) {}
-    __device__ __forceinline__ void issue(int, __amdgpu_buffer_rsrc_t, char *, int, int64_t, int) const {}
+    __device__ __forceinline__ void issue(int, __amdgpu_buffer_rsrc_t, char *, int64_t, int) const {}
 };
 
 __device__ __forceinline__ f32x4 mma_f32(u32x4 a, u32x4 b, f32x4 c)
@@ -409,12 +411,12 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
         // Load x of either operand's part of stage `ahead`.  Behind the last tile: its last stage again, into memory that nobody reads.
         auto load_i = [&](int x, char *to) {
             if constexpr (TURNED) gi.issue(x, ri, to, I.stride, wave);
-            else if (x < gi.per) gi.issue(x, ri, to, ahead, I.stride, wave);
-            else hi.issue(x - gi.per, rsi, to + oSI, ahead, I.scale_stride, wave);
+            else if (x < gi.per) gi.issue(x, ri, to, I.stride, wave);
+            else hi.issue(x - gi.per, rsi, to + oSI, I.scale_stride, wave);
         };
         auto load_j = [&](int x, char *to) {
-            if (x < gj.per) gj.issue(x, rj, to, ahead, J.stride, wave);
-            else hj.issue(x - gj.per, rsj, to + oSJ, ahead, J.scale_stride, wave);
+            if (x < gj.per) gj.issue(x, rj, to, J.stride, wave);
+            else hj.issue(x - gj.per, rsj, to + oSJ, J.scale_stride, wave);
         };
         auto advance = [&] {
             if (ahead + 1 < ahead_n) {
