@@ -753,7 +753,8 @@ TAPOUT_API tapout_status tapout_head_loss(tapout_head *head, const tapout_logits
  * share belongs into scale: it meets the sums, in binary32), the results once.
  * Rows that are left out (a target outside [0, V), an lse that is not finite, a
  * row_weight of 0) contribute nothing, whatever their hidden states hold, and
- * get zeros.
+ * get zeros; where no row is left, so does grad_weight, whatever scale is (a
+ * mean's is infinite then).
  *   lse         [B,K] f32 of tapout_head_loss on the same inputs
  *   row_weight  [B,K] f32 or NULL (1)
  *   scale       [1] f32 on the device, or NULL (1): for a mean, 1 / rows

@@ -55,7 +55,9 @@ struct ProductArgs {
     int32_t splits, first;
     float *part;                 // [splits, nj, ni]
     void *out; int64_t out_stride;             // elements
-    const float *scale;          // device, or NULL (1)
+    const float *scale;          // device, or NULL (1); the sums are zeros whatever it is where none of the rows counts
+    int32_t rows, V;
+    const int32_t *target; const float *lse, *row_weight;
 };
 hipError_t launch_head_product(const ProductArgs &a, int dtype, hipStream_t st);
 int head_product_tiles(int ni, int nj, int dtype);       // tiles of one run of the turned product

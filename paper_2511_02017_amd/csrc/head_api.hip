@@ -321,6 +321,7 @@ tapout_status tapout_head_loss_grad(tapout_head *h, const tapout_logits *hidden,
         p.J = Operand{gt, (int64_t)N_pad * esz, n, N_pad * esz, nullptr, 0};
         p.ni = D; p.nj = n; p.k = N_pad; p.splits = 1;
         p.out = (char *)grad_weight->ptr + v0 * grad_weight->stride * esz; p.out_stride = grad_weight->stride; p.scale = scale;
+        p.rows = N; p.V = V; p.target = target; p.lse = lse; p.row_weight = row_weight;
         e = launch_head_product(p, dt, st);
         if (e != hipSuccess) return hip_fail(h, e, "grad_weight");
     }

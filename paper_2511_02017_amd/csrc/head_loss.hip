@@ -218,6 +218,19 @@ __global__ __launch_bounds__(256) void head_transpose_kernel(TransposeArgs a)
 }
 
 // ---- products of the gradient ---------------------------------------------------------------------------
+// What a sum is multiplied by.  The mean over the rows that count, where none does, has an infinite factor: the sums, zeros, stay zeros.  The
+// rows are looked through for that only where the factor is not finite.
+__device__ __forceinline__ float sum_scale(const ProductArgs &a)
+{
+    const float s = a.scale ? *a.scale : 1.f;
+    if (fabsf(s) < INFINITY) return s;
+    for (int n0 = 0; n0 < a.rows; n0 += kWave) {
+        const int n = n0 + (threadIdx.x & (kWave - 1));
+        if (__any(n < a.rows && row_counts(a.target[n], a.V, a.lse, a.row_weight, n))) return s;
+    }
+    return 0.f;
+}
+
 // dh with the weights turned, its sums in binary32 over runs of the vocabulary; dW at once.  Bound by the matrix unit where rows are many
 // (8192 rows, V = 128256, dim = 2048, bfloat16: dh 3.3 ms, 1.30 PFLOP/s, dW 2.85 ms, 1.51), by dW's own bytes where they are few
 // (40 rows, 32000 x 1024 binary32: 46 us for 131 MB).
@@ -225,7 +238,7 @@ template <class T, class E>
 __global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int per_split, int splits)
 {
     extern __shared__ __align__(16) char lds[];
-    const float scale = T::turned || !a.scale ? 1.f : *a.scale;
+    const float scale = T::turned ? 1.f : sum_scale(a);
     T::template work<0>(a.I, a.J, Walk(ni, nj, splits), lds,
         [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, t.split * per_split, min(per_split, stages - t.split * per_split)}; },
         [&](const Work &) {},

@@ -68,3 +68,29 @@ def test_what_earlier_calls_left_in_the_scratch_is_not_read(dtype, N):
     torch.cuda.synchronize()
     assert all(torch.isfinite(v).all() for v in got[1].values())
     same(*got)
+
+
+# vocabularies on every tile of the weights' gradient
+@pytest.mark.parametrize("dtype,N,V", [(bf16, 5, 20), (bf16, 96, 100), (bf16, 300, 333), (f32, 5, 40), (f32, 96, 333), (f32, 300, 64)])
+@pytest.mark.parametrize("factor", [float("inf"), -float("inf"), float("nan")])
+def test_gradients_are_zeros_where_no_row_counts_whatever_the_factor(dtype, N, V, factor):
+    """The mean over no rows has an infinite factor: a batch of prompts only leaves the weights as they are."""
+    D = 96
+    h, w, t = (x.to(DEV) for x in loss_inputs(1, N, V, D, dtype, seed=N + V))
+    t[t < 0] = 0
+    head = binding.DraftHead(N, D, V, dtype=dtype, training=True)
+    lse = head.loss(h, w, t)["lse"]
+    scale = torch.tensor([factor], device=DEV)
+    none = torch.full_like(lse, float("nan"))
+    for left_out in (dict(target=torch.full_like(t, -1), lse=lse), dict(target=t, lse=lse, row_weight=torch.zeros_like(lse)), dict(target=t, lse=none)):
+        out = dict(grad_hidden=torch.ones_like(h), grad_weight=torch.ones_like(w))
+        head.loss_grad(h, w, scale=scale, out=out, **left_out)
+        torch.cuda.synchronize()
+        assert (out["grad_hidden"] == 0).all() and (out["grad_weight"] == 0).all()
+    # the last row alone counts: its gradient meets the factor
+    last = torch.full_like(t, -1)
+    last[0, -1] = t[0, -1]
+    b = head.loss_grad(h, w, last, lse, scale=scale)
+    torch.cuda.synchronize()
+    assert not torch.isfinite(b["grad_hidden"][0, -1]).any() and (b["grad_hidden"][0, :-1] == 0).all()
+    assert not torch.isfinite(b["grad_weight"][t[0, -1].long()]).any()
