@@ -220,9 +220,8 @@ __global__ __launch_bounds__(256) void head_transpose_kernel(TransposeArgs a)
 // ---- products of the gradient ---------------------------------------------------------------------------
 // What a sum is multiplied by.  The mean over the rows that count, where none does, has an infinite factor: the sums, zeros, stay zeros.  The
 // rows are looked through for that only where the factor is not finite.
-__device__ __forceinline__ float sum_scale(const ProductArgs &a)
+__device__ __forceinline__ float sum_scale(const ProductArgs &a, float s)
 {
-    const float s = a.scale ? *a.scale : 1.f;
     if (fabsf(s) < INFINITY) return s;
     for (int n0 = 0; n0 < a.rows; n0 += kWave) {
         const int n = n0 + (threadIdx.x & (kWave - 1));
@@ -238,11 +237,12 @@ template <class T, class E>
 __global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int per_split, int splits)
 {
     extern __shared__ __align__(16) char lds[];
-    const float scale = T::turned ? 1.f : sum_scale(a);
+    const float factor = T::turned || !a.scale ? 1.f : *a.scale;
     T::template work<0>(a.I, a.J, Walk(ni, nj, splits), lds,
         [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, t.split * per_split, min(per_split, stages - t.split * per_split)}; },
         [&](const Work &) {},
         [&](const Work &w, typename T::Acc &acc) {
+            const float scale = T::turned ? 1.f : sum_scale(a, factor);          // here: the first loads do not wait for the factor
 #pragma unroll
             for (int n = 0; n < T::NJ; ++n) {
                 const int j = w.j0 + T::j_of(n);
