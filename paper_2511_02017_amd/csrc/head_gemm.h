@@ -157,7 +157,7 @@ __device__ __forceinline__ f32x4 mma_bf16(u32x4 a, u32x4 b, f32x4 c)
 // such sums are below 2^-21 |x y| together, 2^-24 in the mean, and are left out.  Six bfloat16 products take 96 cycles of the matrix unit for
 // 16 x 16 x 32, the binary32 ones 256.  Parts cut off are a third fewer vector instructions than parts rounded by conversions (cross
 // entropy of 1000 / 3000 rows, V = 32000, dim = 1024: 375 / 1030 us instead of 425 / 1160); the splitting between the products of the
-// row of blocks before, two instructions each, gains nothing there (385 / 1026).  An infinity becomes a NaN.
+// row of blocks before, two instructions each, gains nothing there (385 / 1026).  An infinity becomes a NaN (see Tile::multiply_as_they_are).
 struct Split3 { u32x4 h, m, l; };
 __device__ __forceinline__ Split3 split3(u32x4 a, u32x4 b)
 {
@@ -278,6 +278,9 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
     static constexpr int oSJ = TJ * K::row_j, bytes_j = oSJ + up256(TJ * K::scale_j);
     static constexpr int ring_i = KIND == kTileMx4 || KIND == kTileF32x3 ? 2 : 3, ring_j = 2, ring_bytes = ring_i * bytes_i + ring_j * bytes_j;
     static constexpr int per_cu = 163840 / ring_bytes < 1 ? 1 : 163840 / ring_bytes > 2048 / threads ? 2048 / threads : 163840 / ring_bytes;
+    // wavefronts that have to fit a SIMD: where a tile is multiplied a second time (below) the compiler takes more registers than leave room
+    // for a unit's second workgroup (gradient of 1000 x 32000 x 1024 by the logits: 556 us instead of 413)
+    static constexpr int per_simd = split ? per_cu * NW / 4 : 1;
     using Acc = f32x4[MI][NJ];
     using StagerI = std::conditional_t<TURNED, TurnedStager<TI, K::elems, esz, NW>, Stager<TI, K::row_i, 16, NW, 0>>;
     using StagerJ = Stager<TJ, K::row_j, 16, NW, NJ, TURNED && KIND == kTileBf16>;
@@ -362,13 +365,52 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
         }
     }
 
+    // The tile of `w` once more, as binary32 products, each lane's operands straight from memory.  Parts of an infinity are no number, nor is
+    // its product with a part that is zero, so a tile of split products has a NaN wherever one of its operands is infinite; where the
+    // logits of a vocabulary row that is masked by infinite weights are infinite they have to come out so.  A wavefront whose results hold a
+    // NaN makes them again; the others go on (cross entropy of 1000 x 32000 x 1024 with one masked vocabulary row 482 us, without 386).
+    static __device__ __forceinline__ void multiply_as_they_are(const Operand &I, const Operand &J, const Work &w, Acc &acc)
+    {
+        const int r16 = lane() & 15, g = lane() >> 4, qi = wave() / WJ * MI * 16 + r16, qj = wave() % WJ * NJ * 16 + r16;
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+            for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int k0 = w.first * K::elems; k0 < (w.first + w.n) * K::elems; k0 += 16) {
+            const int k = k0 + g * 4;
+            u32x4 b[NJ];
+#pragma unroll
+            for (int n = 0; n < NJ; ++n) {
+                const int j = w.j0 + row_of_j<NJ>(qj + n * 16);
+                b[n] = u32x4{0, 0, 0, 0};
+                if (j < J.rows && k * 4 < J.row_bytes) b[n] = *(const u32x4 *)((const char *)J.p + j * J.stride + k * 4);
+            }
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) {
+                const int q = qi + mi * 16, i = w.i0 + (TURNED ? q : row_of_i(q));
+                u32x4 a = {0, 0, 0, 0};
+                if constexpr (TURNED) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (k + e < I.rows && i * 4 < I.row_bytes) a[e] = *(const uint32_t *)((const char *)I.p + (k + e) * I.stride + i * 4);
+                } else {
+                    if (i < I.rows && k * 4 < I.row_bytes) a = *(const u32x4 *)((const char *)I.p + i * I.stride + k * 4);
+                }
+#pragma unroll
+                for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = mma_f32(a, b[nj], acc[mi][nj]);
+            }
+        }
+    }
+
     // Works through the tiles of `walk`.  where(walk): its Work, with n >= 1; before(w): fetches what its results need from memory; finish(w, acc): hands the results on, out of the registers, and says
-    // whether it made STORES stores exactly.
+    // whether it made STORES stores exactly.  LOST_J: results of a row of J that is not finite are lost either way (a token whose hidden state
+    // holds an infinity has no finite lse: none of its logits is finite).
     //
     // Stages of all tiles form one stream, of which the loads are two stages ahead of the products: a tile is finished while the
     // first stages of the next one arrive.  Stores count like loads where a wavefront waits for its loads by number: behind a
     // tile whose stores are known in number, the next stage is not waited for longer on their account.
-    template <int STORES, class Where, class Before, class Finish>
+    template <int STORES, bool LOST_J, class Where, class Before, class Finish>
     static __device__ __forceinline__ void work(const Operand &I, const Operand &J, Walk walk, char *lds, Where where, Before before, Finish finish)
     {
         const int wave = Tile::wave(), lane = Tile::lane();
@@ -563,6 +605,27 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
                     early_steps();
                     last_step();
                 }
+            }
+            if constexpr (split) {
+                // an operand's row that is not finite has NaN results throughout, so one of J without any says that I's rows are finite
+                bool again = LOST_J;
+#pragma unroll
+                for (int nj = 0; nj < NJ; ++nj) {
+                    bool none = true;
+#pragma unroll
+                    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) none &= acc[mi][nj][r] == acc[mi][nj][r];
+                    uint64_t lanes = __ballot(none);
+                    if constexpr (LOST_J) {
+                        lanes &= lanes >> 32;                    // the four lanes of a row of J
+                        lanes &= lanes >> 16;
+                        again &= !(lanes & 0xffff);
+                    } else {
+                        again |= lanes != ~0ull;
+                    }
+                }
+                if (again) multiply_as_they_are(I, J, w, acc);
             }
             stores = finish(w, acc);
             if (!walk.more()) break;

@@ -34,13 +34,13 @@ __device__ __forceinline__ bool row_counts(int t, int V, const float *lse, const
 // PFLOP/s; 8192 rows 3.1 ms, 1.39 PFLOP/s, where the clock gives way under the load and a library product of these sizes makes 1.41), by the
 // weights' bytes below (32 rows 113 us, 4.6 TB/s).
 template <class T>
-__global__ __launch_bounds__(T::threads) void head_loss_kernel(LossArgs a, int ni, int nj, int stages)
+__global__ __launch_bounds__(T::threads, T::per_simd) void head_loss_kernel(LossArgs a, int ni, int nj, int stages)
 {
     extern __shared__ __align__(16) char lds[];
     if (blockIdx.x == 0 && a.flags)
         for (int b = threadIdx.x; b < a.B; b += T::threads) a.flags[b] = 0;
     int target[T::NJ];
-    T::template work<0>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
+    T::template work<0, true>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
         [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, 0, stages}; },
         [&](const Work &w) {
 #pragma unroll
@@ -138,12 +138,12 @@ __global__ __launch_bounds__(256) void head_loss_join_kernel(LossArgs a, int blo
 // The loss's product once more, then e^(z - lse) and two stores of each g: rows of g as they are for dh, columns for dW.  The stores are what it
 // takes longer for than the loss (8192 rows, V = 128256, dim = 2048: 3.8 ms against 3.1, matrix unit 55 % busy against 68 %).
 template <class T, class E>
-__global__ __launch_bounds__(T::threads) void head_grad_kernel(GradArgs a, int ni, int nj, int stages, int n_pad, int N_pad)
+__global__ __launch_bounds__(T::threads, T::per_simd) void head_grad_kernel(GradArgs a, int ni, int nj, int stages, int n_pad, int N_pad)
 {
     extern __shared__ __align__(16) char lds[];
     int target[T::NJ];                                        // -1: the row does not count
     float lse[T::NJ], weight[T::NJ];
-    T::template work<0>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
+    T::template work<0, true>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
         [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, 0, stages}; },
         [&](const Work &w) {
 #pragma unroll
@@ -234,11 +234,11 @@ __device__ __forceinline__ float sum_scale(const ProductArgs &a, float s)
 // (8192 rows, V = 128256, dim = 2048, bfloat16: dh 3.3 ms, 1.30 PFLOP/s, dW 2.85 ms, 1.51), by dW's own bytes where they are few
 // (40 rows, 32000 x 1024 binary32: 46 us for 131 MB).
 template <class T, class E>
-__global__ __launch_bounds__(T::threads) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int per_split, int splits)
+__global__ __launch_bounds__(T::threads, T::per_simd) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int per_split, int splits)
 {
     extern __shared__ __align__(16) char lds[];
     const float factor = T::turned || !a.scale ? 1.f : *a.scale;
-    T::template work<0>(a.I, a.J, Walk(ni, nj, splits), lds,
+    T::template work<0, false>(a.I, a.J, Walk(ni, nj, splits), lds,
         [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, t.split * per_split, min(per_split, stages - t.split * per_split)}; },
         [&](const Work &) {},
         [&](const Work &w, typename T::Acc &acc) {

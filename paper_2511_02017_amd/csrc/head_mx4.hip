@@ -109,7 +109,7 @@ __global__ __launch_bounds__(T::threads) void head_logits_kernel(LogitsArgs a, i
 {
     extern __shared__ __align__(16) char lds[];
     const float k_inverse = 1.f / (float)a.K;
-    T::template work<T::MI * T::NJ * (int)sizeof(E) / 4>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
+    T::template work<T::MI * T::NJ * (int)sizeof(E) / 4, false>(a.weight, a.hidden, Walk(ni, nj, 1), lds,
         [&](const Walk &t) { return Work{t.i() * T::TI, t.j() * T::TJ, 0, stages}; },
         [&](const Work &) {},
         [&](const Work &w, typename T::Acc &acc) {

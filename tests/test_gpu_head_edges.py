@@ -3,7 +3,8 @@ import pytest
 import torch
 
 from paper_2511_02017_amd import binding
-from tests.test_gpu_head import DEV, bf16, f32, loss_inputs, rand, same
+from tests import head_util as hu
+from tests.test_gpu_head import DEV, bf16, f32, loss_inputs, rand, same, within
 
 pytestmark = pytest.mark.gpu
 BEHIND = 300                             # rows: more than the largest tile has
@@ -94,3 +95,96 @@ def test_gradients_are_zeros_where_no_row_counts_whatever_the_factor(dtype, N, V
     torch.cuda.synchronize()
     assert not torch.isfinite(b["grad_hidden"][0, -1]).any() and (b["grad_hidden"][0, :-1] == 0).all()
     assert not torch.isfinite(b["grad_weight"][t[0, -1].long()]).any()
+
+
+# binary32: the same products as they are up to 64 tokens, as sums of three bfloat16 from 65 on
+@pytest.mark.parametrize("dtype,N", [(bf16, 20), (bf16, 100), (bf16, 299), (f32, 64), (f32, 65), (f32, 299)])
+def test_vocabulary_rows_masked_by_infinite_weights(dtype, N):
+    """A constant hidden element and a weight of -inf there: the token's logit is -inf, whatever the number of rows."""
+    V, D = 700, 96
+    h, w, t = loss_inputs(1, N, V, D, dtype, seed=N)
+    masked = torch.zeros(V, dtype=torch.bool)
+    masked[3], masked[256:400], masked[V - 1] = True, True, True
+    h[..., 0] = 1.0
+    t[0][(t[0] >= 0) & masked[t[0].clamp(min=0).long()]] = 5
+    wm = w.clone()
+    wm[masked, 0] = -float("inf")
+    head = binding.DraftHead(N, D, V, dtype=dtype, training=True)
+    hd, wd, td = h.to(DEV), wm.to(DEV), t.to(DEV)
+    f = head.loss(hd, wd, td)
+    b = head.loss_grad(hd, wd, td, f["lse"])
+    torch.cuda.synchronize()
+    assert (f["flags"] == 0).all()
+    kept = torch.where(t[0] < 0, t[0], (torch.cumsum(~masked, 0) - 1).to(torch.int32)[t[0].clamp(min=0).long()])      # targets among the other rows
+    loss, lse, z, dz = hu.cross_entropy(h[0], w[~masked], kept)
+    bound = hu.lse_bound(z, dz, lse)
+    within(f["lse"][0], lse, bound)
+    within(f["loss"][0], loss, bound + dz.amax(-1) + 2 * hu.U32 * (loss.abs() + 1))
+    dh, dw, bh, bw = hu.gradients(h[0], w[~masked], kept, lse, torch.ones(N), 1.0, dtype)
+    live = t[0] >= 0
+    within(b["grad_hidden"][0][:, 1:], dh[:, 1:], bh[:, 1:])
+    assert b["grad_hidden"][0][live.to(DEV), 0].isnan().all() and (b["grad_hidden"][0][~live.to(DEV)] == 0).all()       # 0 times -inf
+    within(b["grad_weight"][~masked.to(DEV)], dw, bw)
+    assert (b["grad_weight"][masked.to(DEV)] == 0).all()
+    # the target itself is masked: an infinite loss of a good row, whose gradient takes its hidden state off the masked row
+    t[0, 2] = 3
+    f = head.loss(hd, wd, t.to(DEV))
+    b = head.loss_grad(hd, wd, t.to(DEV), f["lse"])
+    torch.cuda.synchronize()
+    assert (f["flags"] == 0).all() and f["loss"][0, 2] == float("inf") and torch.isfinite(f["lse"]).all()
+    assert torch.equal(b["grad_weight"][3], -hd[0, 2])
+    # logits of +inf: no finite lse
+    h[0, 1, 0] = -1.0
+    f = head.loss(h.to(DEV), wd, t.clamp(min=0).to(DEV))
+    torch.cuda.synchronize()
+    assert int(f["flags"][0]) == binding.FLAG_BAD_ROW and f["loss"][0, 1].isnan() and torch.isfinite(f["lse"][0, torch.arange(N) != 1]).all()
+
+
+@pytest.mark.parametrize("N", [64, 65, 299])
+def test_hidden_states_that_are_not_finite_beside_masked_vocabulary_rows(N):
+    """Rows that are left out hold NaN and infinities, in every tile of tokens or in all of one but a few: the others as without them."""
+    V, D = 700, 96
+    h, w, t = loss_inputs(1, N, V, D, f32, seed=N)
+    t[t < 0] = 1
+    h[..., 0] = 1.0
+    w[300, 0] = w[V - 1, 0] = -float("inf")
+    t[0][(t[0] == 300) | (t[0] == V - 1)] = 5
+    out = torch.zeros(N, dtype=torch.bool)
+    out[::3], out[8:60] = True, True
+    t[0, out] = -1
+    dirty = h.clone()
+    dirty[0, out] = torch.where(torch.arange(int(out.sum()))[:, None] % 2 == 0, float("nan"), float("inf"))
+    head = binding.DraftHead(N, D, V, dtype=f32, training=True)
+    hd, wd, td = dirty.to(DEV), w.to(DEV), t.to(DEV)
+    f = head.loss(hd, wd, td)
+    b = head.loss_grad(hd, wd, td, f["lse"])
+    torch.cuda.synchronize()
+    assert (f["flags"] == 0).all() and f["lse"][0, out.to(DEV)].isnan().all()
+    rows = [v for v in range(V) if v not in (300, V - 1)]
+    kept = t[0, ~out] - (t[0, ~out] > 300).to(torch.int32)
+    loss, lse, z, dz = hu.cross_entropy(h[0, ~out], w[rows], kept)
+    bound = hu.lse_bound(z, dz, lse)
+    within(f["lse"][0, (~out).to(DEV)], lse, bound)
+    within(f["loss"][0, (~out).to(DEV)], loss, bound + dz.amax(-1) + 2 * hu.U32 * (loss.abs() + 1))
+    dh, dw, bh, bw = hu.gradients(h[0, ~out], w[rows], kept, lse, torch.ones(len(kept)), 1.0, f32)
+    within(b["grad_hidden"][0, (~out).to(DEV)][:, 1:], dh[:, 1:], bh[:, 1:])
+    within(b["grad_weight"][rows], dw, bw)
+    assert (b["grad_hidden"][0, out.to(DEV)] == 0).all() and (b["grad_weight"][[300, V - 1]] == 0).all()
+
+
+@pytest.mark.parametrize("N", [64, 65])
+def test_binary32_results_by_infinite_operands_are_those_of_the_formula(N):
+    """One vocabulary row against a row of zeros, hidden states with one element: each logit is one product."""
+    inf, nan, D = float("inf"), float("nan"), 32
+    pairs = [(1.0, -inf), (-1.0, inf), (2.0 ** -100, -inf), (1.0 + 2.0 ** -23, -inf), (0.0, 1.0), (3.0e38, -2.0), (1.0, nan), (0.0, -inf), (1.0, inf), (inf, 1.0), (-inf, 0.0)]
+    head = binding.DraftHead(N, D, 2, dtype=f32)
+    for x, y in pairs:
+        h, w = torch.zeros(1, N, D), torch.zeros(2, D)
+        h[..., 7], w[1, 7] = x, y
+        f = head.loss(h.to(DEV), w.to(DEV), torch.zeros(1, N, dtype=torch.int32, device=DEV))
+        torch.cuda.synchronize()
+        z = torch.tensor(x) * torch.tensor(y) + (0.0 if abs(x) < inf else nan)               # inf times the row of zeros
+        if z <= 0:
+            assert (f["loss"] == (0.0 if z < 0 else torch.tensor(2.0).log())).all() and f["flags"][0] == 0, (x, y)
+        else:
+            assert f["loss"].isnan().all() and int(f["flags"][0]) == binding.FLAG_BAD_ROW, (x, y)
