@@ -76,14 +76,14 @@ template <int NJ> __device__ __forceinline__ int row_of_j(int q) { return q / (1
 template <int NJ> __device__ __forceinline__ int tile_row(int q) { if constexpr (NJ == 0) return row_of_i(q); else return row_of_j<NJ>(q); }
 
 // A wavefront's load of 64 x 16 bytes into LDS.  HIDDEN: not as the builtin, whose loads the compiler takes to be meant by every turning
-// read that follows, and waits for (the product by 1503 hidden states 754 instead of 293 us).  There are no registers to be written;
-// this wavefront and the others wait by number, below.  M0 needs no saving: a kernel that loads so has no other use for it.
+// read that follows, and waits for (the product by 1503 hidden states 754 instead of 293 us).  There are no registers to be written
+// but M0; this wavefront and the others wait by number, below.
 template <bool HIDDEN> __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t off)
 {
     const auto to = (__attribute__((address_space(3))) void *)lds;
     if constexpr (HIDDEN) {
         const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)to);
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(rsrc) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(rsrc) : "memory", "m0");
     } else {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, off, 0, 0, 0);
     }
