@@ -188,3 +188,42 @@ def test_binary32_results_by_infinite_operands_are_those_of_the_formula(N):
             assert (f["loss"] == (0.0 if z < 0 else torch.tensor(2.0).log())).all() and f["flags"][0] == 0, (x, y)
         else:
             assert f["loss"].isnan().all() and int(f["flags"][0]) == binding.FLAG_BAD_ROW, (x, y)
+
+
+def test_binary32_split_products_are_as_precise_as_documented():
+    """Off by 2^-21 of a product at most and 2^-24 in the mean where it is a sum of three bfloat16 by three: single products, so that nothing
+    hides them.  Beside that a matrix instruction's sums: the last one a step of 2^-23 of the result, in the mean half of it, those before
+    that add to less than 2^-6 of it a 64th each.  (Without the products by third parts: 2^-14 and 2^-16.)"""
+    most, mean = 2.0 ** -21 + 2.0 ** -23 + 5 * 2.0 ** -29, 2.0 ** -24 + 2.0 ** -24 + 5 * 2.0 ** -30
+    g = torch.Generator().manual_seed(1)
+
+    def mantissas(*shape):
+        return torch.exp2(torch.rand(*shape, generator=g)).float()
+
+    def check(got, x, y):
+        off = (got.double().cpu() / (x.double().cpu() * y.double().cpu()) - 1).abs()
+        assert float(off.max()) <= most and float(off.mean()) <= mean, (float(off.max()), float(off.mean()))
+    # logits: -z of a row with one element against 0 of a row of zeros; ln(1 + e^z) of z < -32 is below 2^-46
+    N, D = 1024, 1024
+    x, y = 8 * mantissas(N), -4 * mantissas(D)
+    w = torch.zeros(2, D)
+    w[1] = y
+    h = torch.diag(x)[None]
+    f = binding.DraftHead(N, D, 2, dtype=f32).loss(h.to(DEV), w.to(DEV), torch.ones(1, N, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    check(-f["loss"][0], x, y)
+    # gradients: one row counts, so each element by the weights is g of its token times a hidden element, and with one vocabulary row that is not
+    # zeros each by the hidden state is g times a weight; an element of 1 says what g is
+    N, V = 70, 70
+    h, w = torch.zeros(1, N, D), torch.zeros(V, D)
+    h[0, 5], w[9] = mantissas(D) / 64, -mantissas(D) / 8
+    h[0, 5, 0], w[9, 0] = 1.0, 1.0
+    t = torch.full((1, N), -1, dtype=torch.int32)
+    t[0, 5] = 3
+    head = binding.DraftHead(N, D, V, dtype=f32, training=True)
+    hd, wd, td = h.to(DEV), w.to(DEV), t.to(DEV)
+    b = head.loss_grad(hd, wd, td, head.loss(hd, wd, td)["lse"])
+    torch.cuda.synchronize()
+    dh, dw = b["grad_hidden"][0, 5].cpu(), b["grad_weight"].cpu()
+    check(dw, dw[:, :1], h[0, 5][None])
+    check(dh, dh[:1], w[9])
