@@ -677,14 +677,14 @@ def mx4_quantize(x, out=None, stream=None):
         _matrix(x, "x")                                        # says what is wrong
     rows, cols = x.shape
     P = -(-cols // MX4_PAD) * MX4_PAD
-    codes, scales = out if out is not None else (_empty((rows, P // 2), torch.uint8, x.device, stream), _empty((rows, P // 32), torch.uint8, x.device, stream))
+    codes, scales = out if out is not None else (_empty((rows, P // 2), torch.uint8, x.device, stream), _empty((rows, P // MX4_BLOCK), torch.uint8, x.device, stream))
     st = _fast.mx4_quantize(x, codes, scales, _handle(stream))
     if st is None:
         m = _matrix(x, "x")
         _on(codes, x.device, "codes"), _on(scales, x.device, "scales")
         with torch.cuda.device(x.device):
             st = lib.tapout_mx4_quantize(C.byref(m), rows, cols, _ptr(codes, torch.uint8, (rows, P // 2), "codes"),
-                                         _ptr(scales, torch.uint8, (rows, P // 32), "scales"), _stream(stream))
+                                         _ptr(scales, torch.uint8, (rows, P // MX4_BLOCK), "scales"), _stream(stream))
     if st != 0:
         raise TapoutError(st, lib.tapout_head_last_error(None).decode())
     return codes, scales
@@ -703,7 +703,7 @@ def mx4_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, str
             raise ValueError(f"out: expected shape {(rows, cols)}, got {tuple(out.shape)}")
         _on(scales, codes.device, "scales"), _on(out, codes.device, "out")
         with torch.cuda.device(codes.device):
-            st = lib.tapout_mx4_dequantize(_ptr(codes, torch.uint8, (rows, P // 2), "codes"), _ptr(scales, torch.uint8, (rows, P // 32), "scales"),
+            st = lib.tapout_mx4_dequantize(_ptr(codes, torch.uint8, (rows, P // 2), "codes"), _ptr(scales, torch.uint8, (rows, P // MX4_BLOCK), "scales"),
                                            rows, cols, C.byref(m), _stream(stream))
     if st != 0:
         raise TapoutError(st, lib.tapout_head_last_error(None).decode())
@@ -776,7 +776,7 @@ class DraftHead:
         for t, n in ((codes, "codes"), (scales, "scales"), (k_len, "k_len"), (out, "out")):
             _on(t, self.device, n)
         self._check(st if st is not None else self._lib.tapout_head_logits_mx4(
-            self._head, C.byref(hd), _ptr(codes, torch.uint8, (V, P // 2), "codes"), _ptr(scales, torch.uint8, (V, P // 32), "scales"),
+            self._head, C.byref(hd), _ptr(codes, torch.uint8, (V, P // 2), "codes"), _ptr(scales, torch.uint8, (V, P // MX4_BLOCK), "scales"),
             B, K, V, _ptr(k_len, torch.int32, (B,), "k_len"), int(act_bits), C.byref(lg), self._on_stream(stream)))
         return out
 

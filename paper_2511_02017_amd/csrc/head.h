@@ -5,12 +5,23 @@
 
 namespace tapout {
 
-constexpr int kMx4Block = 32;        // elements that share a scale
 constexpr int kMx4Pad = 128;         // a row of codes is padded to whole matrix steps
 inline int mx4_cols(int cols) { return (cols + kMx4Pad - 1) / kMx4Pad * kMx4Pad; }
 
 // The target of row n if the row counts in the loss: a token of the vocabulary; -1: the row is left out, -2: no such token.
 __host__ __device__ __forceinline__ int counted_target(int t, int V) { return t < 0 ? -1 : t < V ? t : -2; }
+
+// A launch with `bytes` of LDS, which has to be asked for from 64 KB on.
+template <class F> hipError_t with_lds(const void *kernel, int bytes, F launch)
+{
+    if (bytes > 65536) {
+        const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    launch();
+    return hipGetLastError();
+}
+inline int up(int a, int b) { return (a + b - 1) / b; }
 
 // ---- cross entropy -----------------------------------------------------------------------------------
 struct LossArgs {

@@ -307,24 +307,12 @@ __global__ __launch_bounds__(256) void head_pack_kernel(PackArgs a)
     if (n < a.N) *(u32x4 *)((E *)a.dst + (int64_t)n * a.cols + c) = *(const u32x4 *)((const E *)a.src + (n / a.K) * a.stride_b + (n % a.K) * a.stride_k + c);
 }
 
-template <class T, class F> hipError_t with_lds(const void *kernel, int bytes, F launch)
-{
-    if (bytes > 65536) {
-        const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e != hipSuccess) return e;
-    }
-    launch();
-    return hipGetLastError();
-}
-
-inline int up(int a, int b) { return (a + b - 1) / b; }
-
 template <class T> hipError_t loss_with(const LossArgs &a, hipStream_t st)
 {
     using K = Kind<T::kind>;
     const int ni = up(a.V, T::TI), nj = up(a.N, T::TJ), stages = up(a.D, K::elems);
     if ((int64_t)a.N * ni * T::WI > a.part_cap) return hipErrorInvalidValue;
-    hipError_t e = with_lds<T>((const void *)head_loss_kernel<T>, T::ring_bytes, [&] {
+    hipError_t e = with_lds((const void *)head_loss_kernel<T>, T::ring_bytes, [&] {
         head_loss_kernel<T><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
     });
     if (e != hipSuccess) return e;
@@ -337,7 +325,7 @@ template <class T, class E> hipError_t grad_with(const GradArgs &a, hipStream_t 
     using K = Kind<T::kind>;
     const int n_pad = up(a.n, 64) * 64, N_pad = up(a.N, 32) * 32;
     const int ni = up(n_pad, T::TI), nj = up(N_pad, T::TJ), stages = up(a.D, K::elems);
-    return with_lds<T>((const void *)head_grad_kernel<T, E>, T::ring_bytes, [&] {
+    return with_lds((const void *)head_grad_kernel<T, E>, T::ring_bytes, [&] {
         head_grad_kernel<T, E><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages, n_pad, N_pad);
     });
 }
@@ -347,7 +335,7 @@ template <class T, class E> hipError_t product_with(const ProductArgs &a, hipStr
     using K = Kind<T::kind>;
     const int ni = up(a.ni, T::TI), nj = up(a.nj, T::TJ), stages = up(a.k, K::elems);
     const int per_split = up(stages, a.splits), splits = up(stages, per_split);
-    return with_lds<T>((const void *)head_product_kernel<T, E>, T::ring_bytes, [&] {
+    return with_lds((const void *)head_product_kernel<T, E>, T::ring_bytes, [&] {
         head_product_kernel<T, E><<<grid_of<T>((int64_t)ni * nj * splits), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages,
                                                                                              per_split, splits);
     });

@@ -7,8 +7,6 @@
 namespace tapout {
 namespace {
 
-inline int up(int a, int b) { return (a + b - 1) / b; }
-
 // Values are read and written once, past the caches' idea of what is used again (128256 x 2048 bfloat16, us with ordinary / nontemporal
 // accesses: to 4 bits 144 / 110, back 124 / 90; binary32 50257 x 1120 to 4 bits 60 / 49).
 __device__ __forceinline__ void load8(const float *p, float (&x)[8])
@@ -144,12 +142,9 @@ template <class T, class E> hipError_t logits_with(const LogitsArgs &a, hipStrea
 {
     using K = Kind<T::kind>;
     const int ni = up(a.V, T::TI), nj = up(a.N, T::TJ), stages = up(a.D, K::elems);
-    if (T::ring_bytes > 65536) {
-        const hipError_t e = hipFuncSetAttribute((const void *)head_logits_kernel<T, E>, hipFuncAttributeMaxDynamicSharedMemorySize, T::ring_bytes);
-        if (e != hipSuccess) return e;
-    }
-    head_logits_kernel<T, E><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
-    return hipGetLastError();
+    return with_lds((const void *)head_logits_kernel<T, E>, T::ring_bytes, [&] {
+        head_logits_kernel<T, E><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
+    });
 }
 
 template <class E> hipError_t logits_of(const LogitsArgs &a, int kind, hipStream_t st)
@@ -172,7 +167,7 @@ template <class E> hipError_t logits_of(const LogitsArgs &a, int kind, hipStream
 
 template <class E> static hipError_t quantize(const QuantArgs &a, hipStream_t st)
 {
-    const int per = (a.cols + kMx4Pad - 1) / kMx4Pad * kMx4Pad / 8;
+    const int per = mx4_cols(a.cols) / 8;
     const int64_t groups = (int64_t)a.rows * per;
     // four groups a lane where the values come from memory, not from the 256 MiB cache before it (one / four a lane, us, rows of 2048 bfloat16:
     // 64 rows 2.6 / 4.5, 4096 rows 6.3 / 7.2, 32768 rows 33.2 / 34.3, 65536 rows 64 / 60, 128256 rows 126 / 114; 50257 x 1120 binary32 48.2 / 49.4)
@@ -188,7 +183,7 @@ hipError_t launch_mx4_quantize(const QuantArgs &a, int dtype, hipStream_t st)
 
 hipError_t launch_mx4_dequantize(const DequantArgs &a, int dtype, hipStream_t st)
 {
-    const int per = (a.cols + kMx4Pad - 1) / kMx4Pad * kMx4Pad / 8;
+    const int per = mx4_cols(a.cols) / 8;
     const int64_t grid = ((int64_t)a.rows * per + 255) / 256;
     if (dtype == TAPOUT_F32) mx4_dequantize_kernel<float><<<grid, 256, 0, st>>>(a, per);
     else mx4_dequantize_kernel<__bf16><<<grid, 256, 0, st>>>(a, per);
