@@ -661,7 +661,8 @@ TAPOUT_API tapout_status tapout_profile_read(tapout_ctx *ctx, int32_t kind, doub
  * 16-byte aligned, strides included (TAPOUT_EINVAL otherwise), and dim must be a
  * multiple of 32.  Row strides of weights are at most 8 MiB, max_rows * dim at
  * most 2^33 and vocab * dim at most 2^35.  Products of binary32 inputs may be off
- * by 2^-21 of themselves each (2^-24 in the mean) before they are summed in binary32.
+ * by 2^-21 of themselves each (2^-24 in the mean) before they are summed in binary32;
+ * infinities among them (logits of -infinity by infinite weights, say) keep their meaning.
  */
 typedef struct tapout_head tapout_head;
 
@@ -669,14 +670,16 @@ typedef struct {
     int32_t device;                       /* HIP device ordinal                                 */
     int32_t max_rows;                     /* largest B * K of any call, at most 2^20            */
                                           /* (scratch: 8 bytes a row and 64 vocabulary rows,    */
-                                          /* a copy of the hidden states in each form)          */
+                                          /* 16 for the first 64 rows; a copy of the hidden     */
+                                          /* states, of bfloat16 ones one in 4 bits too)        */
     int32_t dim;                          /* length of a hidden state: a multiple of 32, at most 65536 */
     int32_t vocab;                        /* largest V of any call, at most 2^24                */
     int32_t dtype;                        /* tapout_dtype of hidden states and weights          */
     int32_t training;                     /* 1: tapout_head_loss_grad may be called; adds       */
                                           /* scratch: up to 1 GiB for a piece of the vocabulary */
-                                          /* (more where 256 vocabulary rows need more), and 4  */
-                                          /* bytes an element of the hidden states, at least 64 MiB */
+                                          /* (more where 256 vocabulary rows need more), 4      */
+                                          /* bytes an element of the hidden states, at least 64 MiB, */
+                                          /* and a transposed copy of the hidden states         */
 } tapout_head_config;
 
 typedef struct {
@@ -717,6 +720,7 @@ TAPOUT_API tapout_status tapout_mx4_dequantize(const uint8_t *codes, const uint8
  * Draft logits of hidden states under a head held in 4 bits:
  *   out[b,k,v] = sum_d h[b,k,d] w[v,d],  w the values of codes / scales [V, dim]
  * summed in binary32 and rounded once.  For bfloat16 heads.
+ *   codes, scales  as tapout_mx4_quantize writes them, zeros behind dim included
  *   act_bits 16: h as it is;  4: h is quantised like the weights first (two to
  *            three times the rate where rows are many; scores get noise of the
  *            order of a tenth of their spread)

@@ -76,7 +76,7 @@ template <int NJ> __device__ __forceinline__ int row_of_j(int q) { return q / (1
 template <int NJ> __device__ __forceinline__ int tile_row(int q) { if constexpr (NJ == 0) return row_of_i(q); else return row_of_j<NJ>(q); }
 
 // A wavefront's load of 64 x 16 bytes into LDS.  HIDDEN: not as the builtin, whose loads the compiler takes to be meant by every turning
-// read that follows, and waits for (the product by 1503 hidden states 754 instead of 293 us).  There are no registers to be written
+// read that follows, and waits for (a product by 1503 hidden states in twice as many runs of k as now: 754 instead of 293 us).  There are no registers to be written
 // but M0; this wavefront and the others wait by number, below.
 template <bool HIDDEN> __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char *lds, uint32_t off)
 {
@@ -156,7 +156,7 @@ __device__ __forceinline__ f32x4 mma_bf16(u32x4 a, u32x4 b, f32x4 c)
 // three times eight, so nothing is left behind l.  With |m| < 2^-7 |x| and |l| < 2^-15 |x|, the three smallest of the nine products of two
 // such sums are below 2^-21 |x y| together, 2^-24 in the mean, and are left out.  Six bfloat16 products take 96 cycles of the matrix unit for
 // 16 x 16 x 32, the binary32 ones 256.  Parts cut off are a third fewer vector instructions than parts rounded by conversions (cross
-// entropy of 1000 / 3000 rows, V = 32000, dim = 1024: 375 / 1030 us instead of 425 / 1160); the splitting between the products of the
+// entropy of 1000 / 3000 rows, V = 32000, dim = 1024: 375 / 1030 us instead of 425 / 1160, with no look for a NaN yet); the splitting between the products of the
 // row of blocks before, two instructions each, gains nothing there (385 / 1026).  An infinity becomes a NaN (see Tile::multiply_as_they_are).
 struct Split3 { u32x4 h, m, l; };
 __device__ __forceinline__ Split3 split3(u32x4 a, u32x4 b)

@@ -30,8 +30,8 @@ __device__ __forceinline__ bool row_counts(int t, int V, const float *lse, const
 
 // ---- forward -----------------------------------------------------------------------------------------
 // Every wavefront leaves the maximum and sum of its own MI * 16 vocabulary rows for each of its tokens: 2 / (MI * 16) of the logits' bytes,
-// joined by the next kernel.  Bound by the matrix unit from some 200 tokens on (V = 128256, dim = 2048, bfloat16: 512 rows 228 us, 1.18
-// PFLOP/s; 8192 rows 3.1 ms, 1.39 PFLOP/s, where the clock gives way under the load and a library product of these sizes makes 1.41), by the
+// joined by the next kernel.  Bound by the matrix unit from some 200 tokens on (V = 128256, dim = 2048, bfloat16: 512 rows 224 us, 1.20
+// PFLOP/s; 8192 rows 3.14 ms, 1.37 PFLOP/s, where the clock gives way under the load and a library product of these sizes makes 1.41), by the
 // weights' bytes below (32 rows 113 us, 4.6 TB/s).
 template <class T>
 __global__ __launch_bounds__(T::threads, T::per_simd) void head_loss_kernel(LossArgs a, int ni, int nj, int stages)
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256) void head_loss_join_kernel(LossArgs a, int blo
 
 // ---- gradient by the logits of one piece ---------------------------------------------------------------
 // The loss's product once more, then e^(z - lse) and two stores of each g: rows of g as they are for dh, columns for dW.  The stores are what it
-// takes longer for than the loss (8192 rows, V = 128256, dim = 2048: 3.8 ms against 3.1, matrix unit 55 % busy against 68 %).
+// takes longer for than the loss (8192 rows, V = 128256, dim = 2048: 3.95 ms against 3.14, matrix unit 55 % busy against 72 %).
 template <class T, class E>
 __global__ __launch_bounds__(T::threads, T::per_simd) void head_grad_kernel(GradArgs a, int ni, int nj, int stages, int n_pad, int N_pad)
 {
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(T::threads, T::per_simd) void head_grad_kernel(Grad
         });
 }
 
-// 64 x 64 through LDS, 16 bytes a lane on either side (8192 x 2048 bfloat16: 16 us, 4.1 TB/s).
+// 64 x 64 through LDS, 16 bytes a lane on either side (8192 x 2048 bfloat16: 17 us, 4.0 TB/s; two thirds of its LDS cycles are bank conflicts).
 template <class E>
 __global__ __launch_bounds__(256) void head_transpose_kernel(TransposeArgs a)
 {
@@ -231,8 +231,9 @@ __device__ __forceinline__ float sum_scale(const ProductArgs &a, float s)
 }
 
 // dh with the weights turned, its sums in binary32 over runs of the vocabulary; dW at once.  Bound by the matrix unit where rows are many
-// (8192 rows, V = 128256, dim = 2048, bfloat16: dh 3.3 ms, 1.30 PFLOP/s, dW 2.85 ms, 1.51), by dW's own bytes where they are few
-// (40 rows, 32000 x 1024 binary32: 46 us for 131 MB).
+// (8192 rows, V = 128256, dim = 2048, bfloat16: dh 3.28 ms, 1.31 PFLOP/s, dW 2.83 ms, 1.52), by dW's stores where they are few (40 rows,
+// 32000 x 1024 binary32: 45 us for 131 MB, 2.9 TB/s where a fill makes 6.8: a tile's two stages have its stores behind them, not beside).
+// Partial sums of a later piece of the vocabulary are added block by block, a round trip each.
 template <class T, class E>
 __global__ __launch_bounds__(T::threads, T::per_simd) void head_product_kernel(ProductArgs a, int ni, int nj, int stages, int per_split, int splits)
 {
@@ -351,7 +352,8 @@ template <int KIND, bool TURNED = false> using Large = Tile<KIND, 256, 256, 2, 4
 // 512 rows 560 / 328 / 220).
 // binary32: products as they are while the tile is nearly empty, three bfloat16 each where the matrix unit sets the pace (V = 32000,
 // dim = 1024, us with 32 native / 128 native / 128 split: 33 rows 44 / 81 / 65, 64 rows 45 / 81 / 65, 128 rows 82 / 85 / 72, 256 rows
-// 159 / 148 / 103, 1000 rows - / 527 / 375, 3000 rows - / 1561 / 1030, which is 191 TFLOP/s of binary32).
+// 159 / 148 / 103, 1000 rows - / 527 / 385, 3000 rows - / 1561 / 1046, which is 188 TFLOP/s of binary32).  By tokens alone: with a vocabulary
+// shorter than these the largest tile leaves units empty.
 template <template <class> class F, bool TURNED, class A> hipError_t by_tokens(A &&a, int tokens, int dtype, hipStream_t st)
 {
     if (dtype == TAPOUT_F32) return tokens <= 64 ? F<Small<kTileF32, TURNED>>::launch(a, st) : F<Mid<kTileF32x3, TURNED>>::launch(a, st);

@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t max_of_four(uint32_t v)
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false));   // lanes 2 3 0 1
 }
 
-// Eight elements a lane, four lanes a block; U such groups, all requested first.  Bound by memory (128256 x 2048 bfloat16: 112 us, 5.9 TB/s).
+// Eight elements a lane, four lanes a block; U such groups, all requested first.  Bound by memory (128256 x 2048 bfloat16: 110 us, 6.0 TB/s).
 template <class E, int U>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(QuantArgs a, int per, int64_t groups)      // per: groups of eight in a padded row
 {
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(QuantArgs a, int per,
     }
 }
 
-// Bound by memory (128256 x 2048 to bfloat16: 90 us, 7.4 TB/s of mostly writes).
+// Bound by memory (128256 x 2048 to bfloat16: 91 us, 7.3 TB/s of mostly writes).
 template <class E>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(DequantArgs a, int per)
 {
@@ -101,7 +101,7 @@ __device__ __forceinline__ void store8(__bf16 *to, f32x4 a, f32x4 b)
 
 // z = h W^T, rounded once.  Few rows: bound by the codes' and the results' bytes (64 rows, V = 128256, dim = 2048, 16-bit hidden states, bfloat16 results: 41 us,
 // 3.9 TB/s).  Many: by the matrix unit and the conversion of codes beside it with 16-bit hidden states (512 rows 217 us, 1.24 PFLOP/s), with 4-bit ones by the
-// results (512 rows 97 us; 4096 rows over V = 151936 810 us, 3.1 PFLOP/s, 620 without a store): they leave in bursts behind a tile.
+// results (512 rows 93 us; 4096 rows over V = 151936 902 us, 781 at the highest clock, 2.8 and 3.3 PFLOP/s, 620 without a store): they leave in bursts behind a tile.
 template <class T, class E>
 __global__ __launch_bounds__(T::threads) void head_logits_kernel(LogitsArgs a, int ni, int nj, int stages)
 {
