@@ -607,15 +607,18 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
                 }
             }
             if constexpr (split) {
-                // an operand's row that is not finite has NaN results throughout, so one of J without any says that I's rows are finite
+                // an operand's row that is not finite has NaN results throughout, so one of J without any says that I's rows are finite; columns behind
+                // those of a turned I hold anything (what lies behind its rows is zeros)
                 bool again = LOST_J;
 #pragma unroll
                 for (int nj = 0; nj < NJ; ++nj) {
                     bool none = true;
 #pragma unroll
-                    for (int mi = 0; mi < MI; ++mi)
+                    for (int mi = 0; mi < MI; ++mi) {
+                        const bool behind = TURNED && (w.i0 + i_of(mi)) * 4 >= I.row_bytes;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) none &= acc[mi][nj][r] == acc[mi][nj][r];
+                        for (int r = 0; r < 4; ++r) none &= behind || acc[mi][nj][r] == acc[mi][nj][r];
+                    }
                     uint64_t lanes = __ballot(none);
                     if constexpr (LOST_J) {
                         lanes &= lanes >> 32;                    // the four lanes of a row of J

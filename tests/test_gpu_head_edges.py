@@ -32,6 +32,23 @@ def test_what_lies_behind_the_rows_of_loss_and_gradient_is_not_read(dtype, N, V,
     same(*got)
 
 
+@pytest.mark.parametrize("dtype,N", [(bf16, 21), (bf16, 101), (bf16, 299), (f32, 45), (f32, 101), (f32, 299)])
+@pytest.mark.parametrize("V,D", [(333, 96), (777, 160)])
+def test_what_lies_beside_the_columns_of_loss_and_gradient_is_not_read(dtype, N, V, D):
+    h, w, t = (x.to(DEV) for x in loss_inputs(N, 1, V, D, dtype, seed=N + V))
+    head = binding.DraftHead(N, D, V, dtype=dtype, training=True)
+    got = []
+    for junk in (0.0, float("nan"), float("inf")):
+        x, y = torch.full((N, 1, D + 64), junk, dtype=dtype, device=DEV)[..., :D], torch.full((V, D + 64), junk, dtype=dtype, device=DEV)[:, :D]
+        x.copy_(h), y.copy_(w)
+        f = head.loss(x, y, t)
+        got.append(dict(f, **head.loss_grad(x, y, t, f["lse"])))
+    torch.cuda.synchronize()
+    assert all(torch.isfinite(v).all() for v in got[0].values())
+    same(got[1], got[0])
+    same(got[2], got[0])
+
+
 @pytest.mark.parametrize("act", [16, 4])
 @pytest.mark.parametrize("N", [1, 21, 50, 101, 299])
 @pytest.mark.parametrize("V,D", [(1, 32), (333, 96), (777, 160)])
