@@ -244,3 +244,100 @@ def test_binary32_split_products_are_as_precise_as_documented():
     dh, dw = b["grad_hidden"][0, 5].cpu(), b["grad_weight"].cpu()
     check(dw, dw[:, :1], h[0, 5][None])
     check(dh, dh[:1], w[9])
+
+
+# ---- the largest sizes -------------------------------------------------------------------------------------
+def test_matrices_whose_offsets_pass_32_bits():
+    """More than 2^32 bytes of weights, codes and logits: the far end as in a call that has it alone."""
+    V, D, far = 1_100_033, 2048, 769
+    w = torch.randn(V, D, dtype=bf16, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)) * 0.05
+    c, s = binding.mx4_quantize(w)
+    c1, s1 = binding.mx4_quantize(w[-far:])
+    assert torch.equal(c[-far:], c1) and torch.equal(s[-far:], s1)
+    assert torch.equal(binding.mx4_dequantize(c, s, D)[-far:], binding.mx4_dequantize(c1, s1, D))
+    h = rand(1, 2100, D, seed=2, dtype=bf16).to(DEV)
+    head = binding.DraftHead(2100, D, V)
+    for act in (16, 4):
+        z = head.logits(h, c, s, act_bits=act)
+        assert z.numel() > 2 ** 31 and torch.equal(z[..., -far:], head.logits(h, c1, s1, act_bits=act))
+        del z
+    del head, c, s
+    N = 40
+    head = binding.DraftHead(N, D, V, training=True)
+    h, t = h[:, :N], torch.arange(V - N, V, dtype=torch.int32, device=DEV)[None]
+    f = head.loss(h, w, t)
+    b = head.loss_grad(h, w, t, f["lse"])
+    torch.cuda.synchronize()
+    z = torch.cat([h[0].float() @ p.float().T for p in w.split(65536)], 1).double()
+    lse = torch.logsumexp(z, -1)
+    # binary32 products of the reference too: both are within (D + 2) / 2^23 of sum |h w|, at most |h| |w| a row
+    dz = 2 * (D + 2) * 2.0 ** -23 * h[0].float().norm(dim=-1).double() * float(w.float().norm(dim=-1).max())
+    within(f["lse"][0], lse.cpu(), (dz + 2.0 ** -18 + 1024 * hu.U32 + 2 * hu.U32 * lse.abs()).cpu())
+    p = torch.exp(z[:, -far:] - lse[:, None])
+    p[torch.arange(N), torch.arange(far - N, far)] -= 1.0
+    dw = p.T @ h[0].double()
+    bw = ((2 * dz[:, None] + 2.0 ** -8 + 2.0 ** -16) * p.abs()).T @ h[0].double().abs()
+    within(b["grad_weight"][-far:], dw.cpu(), (bw + 2.0 ** -8 * (dw.abs() + bw) + 1e-9).cpu())
+
+
+@pytest.mark.parametrize("dtype,N", [(bf16, 20), (bf16, 101), (bf16, 299), (f32, 45), (f32, 101)])
+def test_rows_as_far_apart_as_they_may_lie(dtype, N):
+    """Weights and their gradient at 8 MiB a row, hidden states beyond that (which are copied first): as close together."""
+    V, D = 300, 96
+    stride = (8 << 20) // torch.tensor([], dtype=dtype).element_size()
+    h, w, t = (x.to(DEV) for x in loss_inputs(1, N, V, D, dtype, seed=N))
+    room = torch.full((V * stride,), float("nan"), dtype=dtype, device=DEV)
+    far_w = room.as_strided((V, D), (stride, 1))
+    far_w.copy_(w)
+    head = binding.DraftHead(N, D, V, dtype=dtype, training=True)
+    f = head.loss(h, w, t)
+    want = dict(f, **head.loss_grad(h, w, t, f["lse"]))
+    f = head.loss(h, far_w, t)
+    got = head.loss_grad(h, far_w, t, f["lse"], out=dict(grad_hidden=torch.empty_like(h), grad_weight=room.as_strided((V, D), (stride, 1), 2 * D)))
+    torch.cuda.synchronize()
+    same({k: v.contiguous() for k, v in dict(f, **got).items()}, want)
+    del room, far_w, got
+    room = torch.full((N * (stride + 64),), float("nan"), dtype=dtype, device=DEV)
+    far_h = room.as_strided((1, N, D), (0, stride + 64, 1))
+    far_h.copy_(h)
+    f = head.loss(far_h, w, t)
+    got = head.loss_grad(far_h, w, t, f["lse"], out=dict(grad_hidden=room.as_strided((1, N, D), (0, stride + 64, 1), 2 * D), grad_weight=torch.empty_like(w)))
+    torch.cuda.synchronize()
+    same({k: v.contiguous() for k, v in dict(f, **got).items()}, want)
+    with pytest.raises(binding.TapoutError, match="8 MiB"):
+        head.loss(h, torch.empty(stride + 64 + D, device=DEV, dtype=dtype).as_strided((2, D), (stride + 64, 1)), t.clamp(max=1))
+
+
+@pytest.mark.parametrize("dtype,N", [(bf16, 3), (bf16, 101), (bf16, 140), (f32, 3), (f32, 70)])
+def test_the_longest_hidden_states(dtype, N):
+    V, D = 130, 65536
+    h, w, t = loss_inputs(1, N, V, D, dtype, seed=N)
+    head = binding.DraftHead(N, D, V, dtype=dtype, training=True)
+    hd, wd, td = h.to(DEV), w.to(DEV), t.to(DEV)
+    f = head.loss(hd, wd, td)
+    b = head.loss_grad(hd, wd, td, f["lse"])
+    torch.cuda.synchronize()
+    loss, lse, z, dz = hu.cross_entropy(hd[0], wd, td[0])
+    within(f["lse"][0], lse.cpu(), hu.lse_bound(z, dz, lse).cpu())
+    dh, dw, bh, bw = hu.gradients(hd[0], wd, td[0], f["lse"][0].double(), torch.ones(N, device=DEV), 1.0, dtype)
+    within(b["grad_hidden"][0], dh.cpu(), bh.cpu())
+    within(b["grad_weight"], dw.cpu(), bw.cpu())
+    if dtype == bf16:
+        c, s = binding.mx4_quantize(wd)
+        values = binding.mx4_dequantize(c, s, D, dtype=f32)
+        ch, sh = binding.mx4_quantize(hd[0])
+        for act, x in ((16, hd[0]), (4, binding.mx4_dequantize(ch, sh, D, dtype=f32))):
+            z, bound = hu.logits(x, values)
+            within(head.logits(hd, c, s, act_bits=act, dtype=f32)[0], z.cpu(), (bound + 1e-37).cpu())
+
+
+def test_a_closed_head_refuses_its_calls():
+    h, w, t = (x.to(DEV) for x in loss_inputs(1, 3, 50, 64, bf16, seed=1))
+    head = binding.DraftHead(3, 64, 50, training=True)
+    c, s = binding.mx4_quantize(w)
+    f = head.loss(h, w, t)
+    head.close()
+    head.close()
+    for call in (lambda: head.loss(h, w, t), lambda: head.loss_grad(h, w, t, f["lse"]), lambda: head.logits(h, c, s)):
+        with pytest.raises(binding.TapoutError, match="NULL"):
+            call()
