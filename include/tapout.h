@@ -671,11 +671,12 @@ typedef struct {
     int32_t max_rows;                     /* largest B * K of any call, at most 2^20            */
                                           /* (scratch: 8 bytes a row and 64 vocabulary rows,    */
                                           /* 16 for the first 64 rows; a copy of the hidden     */
-                                          /* states, of bfloat16 ones one in 4 bits too)        */
+                                          /* states, one in 8 bits, of bfloat16 ones one in 4   */
+                                          /* bits too)                                          */
     int32_t dim;                          /* length of a hidden state: a multiple of 32, at most 65536 */
     int32_t vocab;                        /* largest V of any call, at most 2^24                */
     int32_t dtype;                        /* tapout_dtype of hidden states and weights          */
-    int32_t training;                     /* 1: tapout_head_loss_grad may be called; adds       */
+    int32_t training;                     /* 1: the calls named _grad may be made; adds         */
                                           /* scratch: up to 1 GiB for a piece of the vocabulary */
                                           /* (more where 256 vocabulary rows need more), 4      */
                                           /* bytes an element of the hidden states, at least 64 MiB, */
@@ -691,7 +692,7 @@ typedef struct {
 TAPOUT_API tapout_status tapout_head_create(tapout_head **out, const tapout_head_config *cfg);
 TAPOUT_API tapout_status tapout_head_destroy(tapout_head *head);
 /* Text of the last error on head; with NULL the text of the last failed
- * tapout_head_create or tapout_mx4_* call on this thread.                     */
+ * tapout_head_create, tapout_mx4_* or tapout_fp8_* call on this thread.       */
 TAPOUT_API const char *tapout_head_last_error(const tapout_head *head);
 
 /*
@@ -735,6 +736,75 @@ TAPOUT_API tapout_status tapout_head_logits_mx4(tapout_head *head, const tapout_
                                   const tapout_logits *out, void *stream);
 
 /*
+ * 8-bit floating point (OCP E4M3: largest value 448, no infinities) with a
+ * binary32 scale for each block of 128 columns and block_rows rows, 1 (hidden
+ * states) or 128 (weights):
+ *   scale = max(max|x| over the block, 448 2^-126) * (1/448), a binary32 product
+ *           with the constant rounded to binary32
+ *   code  = x / scale, a binary32 quotient, to nearest, ties to even
+ * A block that holds a NaN or an infinity gets a NaN scale: all its elements
+ * stand for NaN.  No context, on the CURRENT HIP device.
+ *   codes   [rows, P] u8, P = cols rounded up to a multiple of 128; 16-byte aligned
+ *   scales  [ceil(rows / block_rows), P / 128] f32
+ * tapout_fp8_quantize writes the columns behind cols as zeros.  cols: a multiple
+ * of 32 up to 65536, rows * P at most 2^34; x and out 16-byte aligned, strides
+ * included.  tapout_fp8_dequantize writes code * scale, rounded once.
+ */
+TAPOUT_API tapout_status tapout_fp8_quantize(const tapout_matrix *x, int32_t rows, int32_t cols, int32_t block_rows,
+                                  uint8_t *codes, float *scales, void *stream);
+TAPOUT_API tapout_status tapout_fp8_dequantize(const uint8_t *codes, const float *scales, int32_t rows, int32_t cols,
+                                  int32_t block_rows, const tapout_matrix *out, void *stream);
+
+/*
+ * Draft logits under a head held in 8 bits:
+ *   out[b,k,v] = sum over blocks of 128 d: sa[b,k,block] sw[v / 128,block]
+ *                sum_d qa[b,k,d] qw[v,d]
+ * summed in binary32 and rounded once.  For heads of either type.
+ *   hidden   [B,K,dim], quantised here with a scale for 128 elements of a row; or
+ *            NULL with act_codes [B*K, P], act_scales [B*K, P / 128] as
+ *            tapout_head_norm writes them
+ *   codes, scales  of the weights: tapout_fp8_quantize with block_rows = 128 (or
+ *            a checkpoint's in this layout; zeros behind dim included)
+ *   k_len, out  as tapout_head_logits_mx4
+ */
+TAPOUT_API tapout_status tapout_head_logits_fp8(tapout_head *head, const tapout_logits *hidden,
+                                  const uint8_t *act_codes, const float *act_scales,
+                                  const uint8_t *codes, const float *scales,
+                                  int32_t B, int32_t K, int32_t V, const int32_t *k_len,
+                                  const tapout_logits *out, void *stream);
+
+/*
+ * The norm in front of the head, with the residual's addition:
+ *   s = x + residual, rounded to the head's type (x itself without a residual)
+ *   rstd = 1 / sqrt(mean over dim of s^2 + eps),  y = s rstd weight
+ *   x, residual [B,K,dim] (residual or NULL), weight [dim] (16-byte aligned): the
+ *            head's type
+ *   sum      [B,K,dim] or NULL: s, the residual stream; may be the memory of x
+ *            or of residual themselves
+ *   out      [B,K,dim] or NULL: y in the head's type
+ *   codes, scales [B*K, P], [B*K, P / 128], or both NULL: y in 8 bits, as
+ *            tapout_fp8_quantize (block_rows = 1) makes them of y in binary32
+ *   rstd     [B,K] f32 or NULL
+ *
+ * tapout_head_norm_grad (heads created with training = 1), from the gradient g
+ * by y and that of the rows' other use as a residual stream:
+ *   u = g weight,  h = s rstd
+ *   grad_x = rstd (u - h mean(u h)) + grad_sum   (the residual's is the same)
+ *   grad_weight = sum over rows of g h, in binary32 and in the same order for the
+ *            same sizes
+ *   grad_out, sum, grad_x [B,K,dim], grad_sum [B,K,dim] or NULL, weight,
+ *            grad_weight [dim] (16-byte aligned): the head's type;  rstd [B,K]
+ *   grad_x may be the memory of grad_out, sum or grad_sum themselves
+ */
+TAPOUT_API tapout_status tapout_head_norm(tapout_head *head, const tapout_logits *x, const tapout_logits *residual,
+                                  const void *weight, float eps, int32_t B, int32_t K,
+                                  const tapout_logits *sum, const tapout_logits *out,
+                                  uint8_t *codes, float *scales, float *rstd, void *stream);
+TAPOUT_API tapout_status tapout_head_norm_grad(tapout_head *head, const tapout_logits *grad_out, const tapout_logits *sum,
+                                  const void *weight, const float *rstd, const tapout_logits *grad_sum,
+                                  int32_t B, int32_t K, const tapout_logits *grad_x, void *grad_weight, void *stream);
+
+/*
  * Cross entropy of softmax(h W^T) at one target token a row:
  *   z = h W^T,  lse = ln sum_v exp(z_v),  loss = lse - z[target]
  *   hidden  [B,K,dim], weight [V,dim]: the head's type
@@ -766,6 +836,39 @@ TAPOUT_API tapout_status tapout_head_loss(tapout_head *head, const tapout_logits
  */
 TAPOUT_API tapout_status tapout_head_loss_grad(tapout_head *head, const tapout_logits *hidden, const tapout_matrix *weight,
                                   int32_t B, int32_t K, int32_t V, const int32_t *target, const float *lse,
+                                  const float *row_weight, const float *scale,
+                                  const tapout_logits *grad_hidden, const tapout_matrix *grad_weight, void *stream);
+
+/*
+ * Distillation: the divergence of softmax(h W^T) from a teacher's distribution,
+ * of which each row lists the largest logits (the target model's, say):
+ *   t_k = exp(top_logits_k - lse_T),  z = h W^T,  lse = ln sum_v exp(z_v)
+ *   loss = sum_k t_k (ln t_k - z[top_ids_k] + lse)
+ * with lse_T = teacher_lse, the teacher's own over its whole vocabulary (what the
+ * list leaves out then has no term), or, without, that of the row's list.
+ *   top_ids    [B,K,T] i32, 1 <= T <= TAPOUT_MAX_TOP; negative: the entry is left
+ *              out; a row without entries is left out (loss 0).  A token listed
+ *              more than once counts as often
+ *   top_logits [B,K,T] f32, -infinity allowed (t = 0);  teacher_lse [B,K] or NULL
+ *   loss, lse  [B,K] f32;  top [B,K,T] f32: z at the listed tokens (0 where
+ *              there is none), which the gradient takes
+ *   flags      [B] u32 or NULL (overwritten): BAD_TOKEN, an id >= V (loss NaN);
+ *              BAD_ROW, a row with entries whose logits z hold a NaN or have no
+ *              finite lse, or whose teacher has none (loss NaN; lse NaN if z's)
+ *
+ * tapout_head_distill_grad: with g = row_weight (sum_k t_k softmax(z) - t),
+ *   grad_hidden = scale g W,  grad_weight = scale g^T h
+ * as tapout_head_loss_grad forms and rounds them; lse and top are those of
+ * tapout_head_distill on the same inputs, rows without loss (above), with a
+ * NaN, or with a row_weight of 0 contribute nothing and get zeros.
+ */
+#define TAPOUT_MAX_TOP 1024
+TAPOUT_API tapout_status tapout_head_distill(tapout_head *head, const tapout_logits *hidden, const tapout_matrix *weight,
+                                  int32_t B, int32_t K, int32_t V, const int32_t *top_ids, const float *top_logits, int32_t T,
+                                  const float *teacher_lse, float *loss, float *lse, float *top, uint32_t *flags, void *stream);
+TAPOUT_API tapout_status tapout_head_distill_grad(tapout_head *head, const tapout_logits *hidden, const tapout_matrix *weight,
+                                  int32_t B, int32_t K, int32_t V, const int32_t *top_ids, const float *top_logits, int32_t T,
+                                  const float *teacher_lse, const float *lse, const float *top,
                                   const float *row_weight, const float *scale,
                                   const tapout_logits *grad_hidden, const tapout_matrix *grad_weight, void *stream);
 

@@ -38,7 +38,9 @@ EXPORTS = ("tapout_default_config", "tapout_create", "tapout_destroy", "tapout_l
            "tapout_set_option",
            "tapout_profile_enable", "tapout_profile_read",
            "tapout_head_create", "tapout_head_destroy", "tapout_head_last_error", "tapout_mx4_quantize", "tapout_mx4_dequantize",
-           "tapout_head_logits_mx4", "tapout_head_loss", "tapout_head_loss_grad")
+           "tapout_head_logits_mx4", "tapout_head_loss", "tapout_head_loss_grad",
+           "tapout_fp8_quantize", "tapout_fp8_dequantize", "tapout_head_logits_fp8", "tapout_head_norm", "tapout_head_norm_grad",
+           "tapout_head_distill", "tapout_head_distill_grad")
 
 PROFILE_KINDS = ("select", "draft_pass", "draft_finalize", "target_pass", "verify_head", "verify_slices", "verify_locate", "update",
                  "sample_head", "sample_slices", "sample_locate", "stream_pair")
@@ -150,6 +152,13 @@ def load_library(path: str = None):
         lib.tapout_head_logits_mx4.argtypes = [vp, lg, vp, vp, i32, i32, i32, vp, i32, lg, vp]
         lib.tapout_head_loss.argtypes = [vp, lg, mx, i32, i32, i32] + [vp] * 5
         lib.tapout_head_loss_grad.argtypes = [vp, lg, mx, i32, i32, i32, vp, vp, vp, vp, lg, mx, vp]
+        lib.tapout_fp8_quantize.argtypes = [mx, i32, i32, i32, vp, vp, vp]
+        lib.tapout_fp8_dequantize.argtypes = [vp, vp, i32, i32, i32, mx, vp]
+        lib.tapout_head_logits_fp8.argtypes = [vp, lg, vp, vp, vp, vp, i32, i32, i32, vp, lg, vp]
+        lib.tapout_head_norm.argtypes = [vp, lg, lg, vp, C.c_float, i32, i32, lg, lg, vp, vp, vp, vp]
+        lib.tapout_head_norm_grad.argtypes = [vp, lg, lg, vp, vp, lg, i32, i32, lg, vp, vp]
+        lib.tapout_head_distill.argtypes = [vp, lg, mx, i32, i32, i32, vp, vp, i32] + [vp] * 6
+        lib.tapout_head_distill_grad.argtypes = [vp, lg, mx, i32, i32, i32, vp, vp, i32] + [vp] * 5 + [lg, mx, vp]
         _lib = lib
     return _lib
 
@@ -710,9 +719,57 @@ def mx4_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, str
     return out
 
 
+FP8_BLOCK = 128
+
+
+def fp8_quantize(x, block_rows: int = 1, out=None, stream=None):
+    """tapout_fp8_quantize: x [rows, cols] to (codes uint8 [rows, P], scales float32 [ceil(rows / block_rows), P / 128]), P = cols
+    rounded up to 128; block_rows 1 for hidden states, 128 for weights.  `out`: such a pair to write into."""
+    lib = _lib or load_library()
+    if x.dim() != 2 or not x.is_cuda:
+        _matrix(x, "x")                                        # says what is wrong
+    rows, cols = x.shape
+    P, R = -(-cols // FP8_BLOCK) * FP8_BLOCK, -(-rows // max(int(block_rows), 1))
+    codes, scales = out if out is not None else (_empty((rows, P), torch.uint8, x.device, stream), _empty((R, P // FP8_BLOCK), torch.float32, x.device, stream))
+    st = _fast.fp8_quantize(x, int(block_rows), codes, scales, _handle(stream))
+    if st is None:
+        m = _matrix(x, "x")
+        _on(codes, x.device, "codes"), _on(scales, x.device, "scales")
+        with torch.cuda.device(x.device):
+            st = lib.tapout_fp8_quantize(C.byref(m), rows, cols, int(block_rows), _ptr(codes, torch.uint8, (rows, P), "codes"),
+                                         _ptr(scales, torch.float32, (R, P // FP8_BLOCK), "scales"), _stream(stream))
+    if st != 0:
+        raise TapoutError(st, lib.tapout_head_last_error(None).decode())
+    return codes, scales
+
+
+def fp8_dequantize(codes, scales, cols: int, block_rows: int = 1, dtype=torch.bfloat16, out=None, stream=None):
+    """tapout_fp8_dequantize: the values [rows, cols] that codes and scales stand for; of codes [..., P] with scales [..., P / 128], as norm
+    writes them, [..., cols]."""
+    lib = _lib or load_library()
+    if codes.dim() > 2 and block_rows == 1 and scales.dim() == codes.dim() and (out is None or out.is_contiguous()):
+        flat = fp8_dequantize(codes.flatten(0, -2), scales.flatten(0, -2), cols, 1, dtype, None if out is None else out.flatten(0, -2), stream)
+        return flat.view(*codes.shape[:-1], cols) if out is None else out
+    rows, P, R = codes.shape[0], -(-cols // FP8_BLOCK) * FP8_BLOCK, -(-codes.shape[0] // max(int(block_rows), 1))
+    if out is None:
+        out = _empty((rows, cols), dtype, codes.device, stream)
+    st = _fast.fp8_dequantize(codes, scales, cols, int(block_rows), out, _handle(stream))
+    if st is None:
+        m = _matrix(out, "out")
+        if tuple(out.shape) != (rows, cols):
+            raise ValueError(f"out: expected shape {(rows, cols)}, got {tuple(out.shape)}")
+        _on(scales, codes.device, "scales"), _on(out, codes.device, "out")
+        with torch.cuda.device(codes.device):
+            st = lib.tapout_fp8_dequantize(_ptr(codes, torch.uint8, (rows, P), "codes"), _ptr(scales, torch.float32, (R, P // FP8_BLOCK), "scales"),
+                                           rows, cols, int(block_rows), C.byref(m), _stream(stream))
+    if st != 0:
+        raise TapoutError(st, lib.tapout_head_last_error(None).decode())
+    return out
+
+
 class DraftHead:
     """One tapout_head on one GPU: the scratch memory of a draft model's output head [V, dim] with V <= vocab, for calls of up to
-    max_rows hidden states.  training: loss_grad may be called."""
+    max_rows hidden states.  training: the gradients may be called."""
 
     def __init__(self, max_rows: int, dim: int, vocab: int, *, dtype=torch.bfloat16, device: int = 0, training: bool = False):
         self._lib = load_library()
@@ -818,5 +875,137 @@ class DraftHead:
         self._check(st if st is not None else self._lib.tapout_head_loss_grad(
             self._head, C.byref(hd), C.byref(w), B, K, weight.shape[0], _ptr(target, torch.int32, (B, K), "target"),
             _ptr(lse, f32, (B, K), "lse"), _ptr(row_weight, f32, (B, K), "row_weight"), _ptr(scale, f32, (1,), "scale"),
+            C.byref(gh), C.byref(gw), self._on_stream(stream)))
+        return out
+
+    # -- 8 bits ----------------------------------------------------------------
+    def logits_fp8(self, hidden, codes, scales, act_scales=None, k_len=None, dtype=torch.bfloat16, out=None, stream=None):
+        """tapout_head_logits_fp8: the draft logits [B, K, V] under the head codes, scales (fp8_quantize with block_rows = 128) of hidden
+        states [B, K, dim], or, with act_scales [B, K, P / 128], of their 8-bit codes [B, K, P] (norm with fp8).  k_len as in logits."""
+        (B, K, _), V = hidden.shape, codes.shape[0]
+        if out is None:
+            out = _empty((B, K, V), dtype, self.device, stream)
+        st = _fast.head_logits_fp8(self._addr, self.dim, self.cfg.dtype, self.cfg.device, hidden, act_scales, codes, scales, k_len, out, _handle(stream))
+        if st == 0:
+            return out
+        lg, P = _logits(out, "out"), -(-self.dim // FP8_BLOCK) * FP8_BLOCK
+        if tuple(out.shape) != (B, K, V):
+            raise ValueError(f"out: expected shape {(B, K, V)}, got {tuple(out.shape)}")
+        for t, n in ((hidden, "hidden"), (act_scales, "act_scales"), (codes, "codes"), (scales, "scales"), (k_len, "k_len"), (out, "out")):
+            _on(t, self.device, n)
+        if act_scales is None:
+            hd, ac, sc = C.byref(self._hidden(hidden, "hidden")), None, None
+        else:
+            hd, ac = None, _ptr(hidden, torch.uint8, (B, K, P), "hidden")
+            sc = _ptr(act_scales, torch.float32, (B, K, P // FP8_BLOCK), "act_scales")
+        self._check(st if st is not None else self._lib.tapout_head_logits_fp8(
+            self._head, hd, ac, sc, _ptr(codes, torch.uint8, (V, P), "codes"),
+            _ptr(scales, torch.float32, (-(-V // FP8_BLOCK), P // FP8_BLOCK), "scales"), B, K, V, _ptr(k_len, torch.int32, (B,), "k_len"),
+            C.byref(lg), self._on_stream(stream)))
+        return out
+
+    # -- norm ------------------------------------------------------------------
+    def _vector(self, t, name):
+        _on(t, self.device, name)
+        return _ptr(t, self.dtype, (self.dim,), name)
+
+    def norm(self, x, weight, residual=None, eps: float = 1e-5, fp8: bool = False, out=None, stream=None):
+        """tapout_head_norm.  Returns / fills a dict: sum [B, K, dim] (x + residual; x itself without one), and out [B, K, dim] and rstd
+        [B, K] float32, or, with fp8, codes uint8 [B, K, P] and scales float32 [B, K, P / 128].  A dict given as `out` has any of these
+        five; sum may be x or residual."""
+        B, K, _ = x.shape
+        P = -(-self.dim // FP8_BLOCK) * FP8_BLOCK
+        if out is None:
+            e = lambda shape, dt: _empty(shape, dt, self.device, stream)                                   # noqa: E731
+            out = dict(sum=x if residual is None else e((B, K, self.dim), self.dtype))
+            if fp8:
+                out.update(codes=e((B, K, P), torch.uint8), scales=e((B, K, P // FP8_BLOCK), torch.float32))
+            else:
+                out.update(out=e((B, K, self.dim), self.dtype), rstd=e((B, K), torch.float32))
+        total = out.get("sum")
+        given = None if total is x and residual is None else total
+        st = _fast.head_norm(self._addr, self.dim, self.cfg.dtype, self.cfg.device, x, residual, weight, float(eps), given, out, _handle(stream))
+        if st == 0:
+            return out
+        refs = []
+        for t, n in ((x, "x"), (residual, "residual"), (given, "sum"), (out.get("out"), "out")):
+            if t is not None and tuple(t.shape) != tuple(x.shape):
+                raise ValueError(f"{n}: expected shape {tuple(x.shape)}, got {tuple(t.shape)}")
+            refs.append(None if t is None else C.byref(self._hidden(t, n)))
+        for n in ("codes", "scales", "rstd"):
+            _on(out.get(n), self.device, n)
+        self._check(st if st is not None else self._lib.tapout_head_norm(
+            self._head, refs[0], refs[1], self._vector(weight, "weight"), float(eps), B, K, refs[2], refs[3],
+            _ptr(out.get("codes"), torch.uint8, (B, K, P), "codes"), _ptr(out.get("scales"), torch.float32, (B, K, P // FP8_BLOCK), "scales"),
+            _ptr(out.get("rstd"), torch.float32, (B, K), "rstd"), self._on_stream(stream)))
+        return out
+
+    def norm_grad(self, grad_out, total, weight, rstd, grad_sum=None, out=None, stream=None):
+        """tapout_head_norm_grad at the sum (`total`) and rstd that norm returned.  Returns / fills a dict: grad_x [B, K, dim], by x and by
+        the residual alike, and grad_weight [dim], of the head's type."""
+        B, K, _ = grad_out.shape
+        if out is None:
+            out = dict(grad_x=_empty((B, K, self.dim), self.dtype, self.device, stream), grad_weight=_empty((self.dim,), self.dtype, self.device, stream))
+        st = _fast.head_norm_grad(self._addr, self.dim, self.cfg.dtype, self.cfg.device, grad_out, total, weight, rstd, grad_sum, out["grad_x"],
+                                  out["grad_weight"], _handle(stream))
+        if st == 0:
+            return out
+        refs = []
+        for t, n in ((grad_out, "grad_out"), (total, "total"), (grad_sum, "grad_sum"), (out["grad_x"], "grad_x")):
+            if t is not None and tuple(t.shape) != tuple(grad_out.shape):
+                raise ValueError(f"{n}: expected shape {tuple(grad_out.shape)}, got {tuple(t.shape)}")
+            refs.append(None if t is None else C.byref(self._hidden(t, n)))
+        _on(rstd, self.device, "rstd")
+        self._check(st if st is not None else self._lib.tapout_head_norm_grad(
+            self._head, refs[0], refs[1], self._vector(weight, "weight"), _ptr(rstd, torch.float32, (B, K), "rstd"), refs[2], B, K, refs[3],
+            self._vector(out["grad_weight"], "grad_weight"), self._on_stream(stream)))
+        return out
+
+    # -- distillation ----------------------------------------------------------
+    def distill(self, hidden, weight, top_ids, top_logits, teacher_lse=None, out=None, stream=None):
+        """tapout_head_distill: divergence from a teacher's top_logits [B, K, T] float32 at the tokens top_ids [B, K, T] int32.  Returns / fills
+        a dict: loss, lse [B, K], top [B, K, T] float32 (the head's logits at those tokens), flags [B] int32."""
+        (B, K, _), T = hidden.shape, top_ids.shape[-1]
+        f32, i32 = torch.float32, torch.int32
+        if out is None:
+            out = dict(loss=_empty((B, K), f32, self.device, stream), lse=_empty((B, K), f32, self.device, stream),
+                       top=_empty((B, K, T), f32, self.device, stream), flags=_empty((B,), i32, self.device, stream))
+        st = _fast.head_distill(self._addr, self.dim, self.cfg.dtype, self.cfg.device, hidden, weight, top_ids, top_logits, teacher_lse, out, _handle(stream))
+        if st == 0:
+            return out
+        hd, w = self._hidden(hidden, "hidden"), self._weight(weight, "weight")
+        for t, n in ((top_ids, "top_ids"), (top_logits, "top_logits"), (teacher_lse, "teacher_lse"), (out["loss"], "loss"), (out["lse"], "lse"),
+                     (out["top"], "top"), (out.get("flags"), "flags")):
+            _on(t, self.device, n)
+        self._check(st if st is not None else self._lib.tapout_head_distill(
+            self._head, C.byref(hd), C.byref(w), B, K, weight.shape[0], _ptr(top_ids, i32, (B, K, T), "top_ids"),
+            _ptr(top_logits, f32, (B, K, T), "top_logits"), T, _ptr(teacher_lse, f32, (B, K), "teacher_lse"), _ptr(out["loss"], f32, (B, K), "loss"),
+            _ptr(out["lse"], f32, (B, K), "lse"), _ptr(out["top"], f32, (B, K, T), "top"), _ptr(out.get("flags"), i32, (B,), "flags"),
+            self._on_stream(stream)))
+        return out
+
+    def distill_grad(self, hidden, weight, top_ids, top_logits, lse, top, teacher_lse=None, row_weight=None, scale=None, out=None, stream=None):
+        """tapout_head_distill_grad at the lse and top that distill returned.  Returns / fills a dict: grad_hidden [B, K, dim], grad_weight
+        [V, dim], of the head's type."""
+        (B, K, _), T = hidden.shape, top_ids.shape[-1]
+        f32, i32 = torch.float32, torch.int32
+        if out is None:
+            out = dict(grad_hidden=_empty((B, K, self.dim), self.dtype, self.device, stream),
+                       grad_weight=_empty((weight.shape[0], self.dim), self.dtype, self.device, stream))
+        st = _fast.head_distill_grad(self._addr, self.dim, self.cfg.dtype, self.cfg.device, hidden, weight, top_ids, top_logits, teacher_lse, lse, top,
+                                     row_weight, scale, out["grad_hidden"], out["grad_weight"], _handle(stream))
+        if st == 0:
+            return out
+        hd, w = self._hidden(hidden, "hidden"), self._weight(weight, "weight")
+        gh, gw = self._hidden(out["grad_hidden"], "grad_hidden"), self._weight(out["grad_weight"], "grad_weight")
+        if tuple(out["grad_hidden"].shape) != tuple(hidden.shape) or out["grad_weight"].shape[0] != weight.shape[0]:
+            raise ValueError("grad_hidden and grad_weight must have the shapes of hidden and weight")
+        for t, n in ((top_ids, "top_ids"), (top_logits, "top_logits"), (teacher_lse, "teacher_lse"), (lse, "lse"), (top, "top"),
+                     (row_weight, "row_weight"), (scale, "scale")):
+            _on(t, self.device, n)
+        self._check(st if st is not None else self._lib.tapout_head_distill_grad(
+            self._head, C.byref(hd), C.byref(w), B, K, weight.shape[0], _ptr(top_ids, i32, (B, K, T), "top_ids"),
+            _ptr(top_logits, f32, (B, K, T), "top_logits"), T, _ptr(teacher_lse, f32, (B, K), "teacher_lse"), _ptr(lse, f32, (B, K), "lse"),
+            _ptr(top, f32, (B, K, T), "top"), _ptr(row_weight, f32, (B, K), "row_weight"), _ptr(scale, f32, (1,), "scale"),
             C.byref(gh), C.byref(gw), self._on_stream(stream)))
         return out

@@ -27,13 +27,20 @@ inline int up(int a, int b) { return (a + b - 1) / b; }
 struct LossArgs {
     Operand weight, hidden;      // I: vocabulary rows, J: tokens
     int32_t N, V, D, rows_per_seq, B;
-    const int32_t *target;       // [N]
+    const int32_t *target;       // [N]; NULL: the rows have lists
     float2 *part;                // [N, blocks]: maximum and sum of exp(z - maximum) over a wavefront's vocabulary rows
     int64_t part_cap;            // elements it has room for; a launch that needs more is refused
     float *target_logit;         // [N]
     float *loss, *lse;           // [N]
     uint32_t *flags;             // [B] or NULL
+    // rows with lists of tokens in a target's place
+    int32_t T;
+    const int32_t *ids;          // [N, T] or NULL
+    const float *logits, *teacher_lse;          // the teacher's: [N, T]; [N] or NULL
+    float *top;                  // [N, T]
 };
+hipError_t launch_listed_logits(const LossArgs &a, int dtype, hipStream_t st);      // top
+hipError_t launch_listed_join(const LossArgs &a, int blocks, hipStream_t st);       // the rest of it
 hipError_t launch_head_loss(const LossArgs &a, int dtype, hipStream_t st);
 
 // One piece of the vocabulary, rows [v0, v0 + n): its gradient by the logits, both ways round.
@@ -42,12 +49,24 @@ struct GradArgs {
     int32_t N, V, D, v0, n;
     const int32_t *target;
     const float *lse, *row_weight;
+    int32_t listed;              // 1: no target's term, which launch_listed_grad puts in its place
     void *g;                     // [N, n_pad]   n_pad = n rounded up to 64, zeros behind n
     int64_t g_stride;            // elements
     void *gt;                    // [n, N_pad]   N_pad = N rounded up to 32, zeros behind N
     int64_t gt_stride;
 };
 hipError_t launch_head_grad(const GradArgs &a, int dtype, hipStream_t st);
+
+// Gradients by the listed tokens' logits.  Rows first: which count (state 0, else -1) and what their softmax is multiplied by; then, a piece at a
+// time, the elements that lie in it, over what launch_head_grad wrote there.
+struct ListedArgs {
+    int32_t N, V, T;
+    const int32_t *ids;
+    const float *logits, *teacher_lse, *lse, *top, *row_weight;
+    int32_t *state; float *factor;
+};
+hipError_t launch_listed_rows(const ListedArgs &a, hipStream_t st);
+hipError_t launch_listed_grad(const ListedArgs &a, const GradArgs &piece, int dtype, hipStream_t st);
 
 // dst [cols, rows_pad] = src [rows, cols]^T, zeros behind `rows`; with `target` given, rows that do not count are zeros.
 struct TransposeArgs {
@@ -104,6 +123,42 @@ struct DequantArgs {
     void *out; int64_t stride;                       // elements
 };
 hipError_t launch_mx4_dequantize(const DequantArgs &a, int dtype, hipStream_t st);
+
+// ---- 8-bit blocks -------------------------------------------------------------------------------------
+constexpr int kFp8Block = 128;       // elements of a row that share a scale; rows of codes are padded to whole blocks
+struct Fp8QuantArgs {
+    const void *src; int64_t stride_b, stride_k;     // elements; row r lies at (r / K) * stride_b + (r % K) * stride_k
+    int32_t rows, K, cols;
+    uint8_t *codes; float *scales;                   // [rows, pad], [rows / block_rows, pad / 128]
+};
+hipError_t launch_fp8_quantize(const Fp8QuantArgs &a, int block_rows, int dtype, hipStream_t st);
+struct Fp8DequantArgs {
+    const uint8_t *codes; const float *scales;
+    int32_t rows, cols, block_rows;
+    void *out; int64_t stride;                       // elements
+};
+hipError_t launch_fp8_dequantize(const Fp8DequantArgs &a, int dtype, hipStream_t st);
+
+// ---- norm ---------------------------------------------------------------------------------------------
+struct Rows { const void *p; int64_t stride_b, stride_k; };       // row r at (r / K) * stride_b + (r % K) * stride_k, elements; p NULL: none
+struct NormArgs {
+    Rows x, residual, sum, out;
+    const void *weight;              // [D]
+    float eps;
+    int32_t N, K, D;
+    uint8_t *codes; float *scales;   // [N, pad], [N, pad / 128], or both NULL
+    float *rstd;                     // [N] or NULL
+};
+hipError_t launch_head_norm(const NormArgs &a, int dtype, hipStream_t st);
+struct NormGradArgs {
+    Rows grad_out, sum, grad_sum, grad_x;
+    const void *weight;
+    const float *rstd;
+    int32_t N, K, D;
+    float *part; int64_t part_cap;   // partial sums of grad_weight: room in floats
+    void *grad_weight;               // [D]
+};
+hipError_t launch_head_norm_grad(const NormGradArgs &a, int dtype, hipStream_t st);
 
 struct LogitsArgs {
     Operand weight, hidden;

@@ -26,18 +26,20 @@ enum TileKind {
     kTileF32x3,  // both binary32, multiplied as sums of three bfloat16 each (see split3)
     kTileBf16,   // both bfloat16
     kTileMx4,    // both 4-bit codes with a scale byte for 32 of them
-    kTileMx4W    // I: 4-bit codes with scales; J: bfloat16
+    kTileMx4W,   // I: 4-bit codes with scales; J: bfloat16
+    kTileF8,     // both 8-bit codes, with a binary32 scale for 128 of a row of J and for 128 x 128 of I
+    kTileF8x     // the same, multiplied as bfloat16, whose products are summed in binary32
 };
 
 // Bytes of an operand's row in a stage, elements of k in a stage, and matrix steps: a step takes 64 bytes of each of 16 I rows
 // (16 a lane).
 template <int KIND> struct Kind {
-    static constexpr int elems = KIND == kTileF32 || KIND == kTileF32x3 ? 32 : KIND == kTileBf16 ? 64 : KIND == kTileMx4 ? 256 : 128;
+    static constexpr int elems = KIND == kTileF32 || KIND == kTileF32x3 ? 32 : KIND == kTileBf16 ? 64 : KIND == kTileMx4 ? 256 : 128;          // kTileF8: what shares a scale
     static constexpr int row_i = KIND == kTileMx4W ? 64 : 128;
     static constexpr int row_j = KIND == kTileMx4W ? 256 : 128;
     static constexpr int steps = row_i / 64;
     static constexpr int scale_i = KIND == kTileMx4 || KIND == kTileMx4W ? elems / 32 : 0;     // scale bytes of a row in a stage
-    static constexpr int scale_j = KIND == kTileMx4 ? elems / 32 : 0;
+    static constexpr int scale_j = KIND == kTileMx4 ? elems / 32 : KIND == kTileF8 || KIND == kTileF8x ? 4 : 0;
 };
 
 struct Operand {
@@ -45,8 +47,8 @@ struct Operand {
     int64_t stride;         // bytes from row to row, a multiple of 16; 256 of them within 2^31 (checked on the host)
     int32_t rows;
     int32_t row_bytes;      // bytes of a row, a multiple of 16: what lies behind counts as zeros
-    const uint8_t *scales;  // kTileMx4, and I of kTileMx4W
-    int32_t scale_stride;   // bytes of a row's scales, a multiple of 4
+    const uint8_t *scales;  // kTileMx4, kTileF8, and I of kTileMx4W
+    int32_t scale_stride;   // bytes of a row's scales (I of kTileF8: of 128 rows'), a multiple of 4
 };
 
 // Exchange of a row's 16-byte chunks.  A 16-byte LDS read serves its 64 lanes sixteen at a time, lanes 0-3, 12-15 and 20-27, then
@@ -181,6 +183,29 @@ __device__ __forceinline__ f32x4 mma_mx4(u32x4 a, uint32_t sa, u32x4 b, uint32_t
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)sa, 0, (int)sb);
 }
 
+__device__ __forceinline__ f32x4 mma_f8(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1)
+{
+    // scales of 1: the blocks' own are binary32 and meet the sum
+    const i32x8 x = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
+    const i32x8 y = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+}
+
+// Sixteen codes as bfloat16, which holds E4M3's four bits and their exponents exactly.
+struct Bf16Pair { u32x4 lo, hi; };
+__device__ __forceinline__ Bf16Pair codes8_to_bf16(u32x4 w)
+{
+    Bf16Pair r;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const uint32_t a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[n], 1.f, false));
+        const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[n], 1.f, true));
+        (n < 2 ? r.lo : r.hi)[n % 2 * 2] = a;
+        (n < 2 ? r.lo : r.hi)[n % 2 * 2 + 1] = b;
+    }
+    return r;
+}
+
 // A scale byte as the conversions take it: they read the exponent field alone, 0 as 2^-127 and 255 as NaN.
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
 
@@ -269,14 +294,14 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
     static_assert(!TURNED || KIND == kTileF32 || KIND == kTileF32x3 || KIND == kTileBf16, "");
     static constexpr int esz = KIND == kTileF32 || KIND == kTileF32x3 ? 4 : 2;
     static constexpr bool split = KIND == kTileF32x3;
-    static constexpr bool turned = TURNED;
+    static constexpr bool turned = TURNED, f8 = KIND == kTileF8 || KIND == kTileF8x;
     static constexpr int kind = KIND, TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, NW = WI * WJ, threads = NW * 64;
     static constexpr int MI = TI / WI / 16, NJ = TJ / WJ / 16;
     static_assert(MI % 2 == 0, "rows of I are ordered by pairs of blocks");
     static constexpr int up256(int n) { return (n + 255) & ~255; }
     static constexpr int oSI = TI * K::row_i, bytes_i = oSI + up256(TI * K::scale_i);
     static constexpr int oSJ = TJ * K::row_j, bytes_j = oSJ + up256(TJ * K::scale_j);
-    static constexpr int ring_i = KIND == kTileMx4 || KIND == kTileF32x3 ? 2 : 3, ring_j = 2, ring_bytes = ring_i * bytes_i + ring_j * bytes_j;
+    static constexpr int ring_i = KIND == kTileMx4 || KIND == kTileF32x3 || KIND == kTileF8 || KIND == kTileF8x ? 2 : 3, ring_j = 2, ring_bytes = ring_i * bytes_i + ring_j * bytes_j;
     static constexpr int per_cu = 163840 / ring_bytes < 1 ? 1 : 163840 / ring_bytes > 2048 / threads ? 2048 / threads : 163840 / ring_bytes;
     // wavefronts that have to fit a SIMD: where a tile is multiplied a second time (below) the compiler takes more registers than leave room
     // for a unit's second workgroup (gradient of 1000 x 32000 x 1024 by the logits: 556 us instead of 413)
@@ -297,9 +322,11 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
     }
     static __device__ __forceinline__ int j_of(int nj) { return wave() % WJ * (NJ * 16) + (lane() & 15) * NJ + nj; }
 
-    // What a wavefront multiplies: blocks of I (those of the next step replace them one by one), and of J for two steps.
+    // What a wavefront multiplies: blocks of I (those of the next step replace them one by one), and of J for two steps.  kTileF8: both halves of
+    // a stage's rows, of up to four blocks of I at a time.
+    static constexpr int held = f8 && MI > 4 ? 4 : MI;
     struct Frags {
-        u32x4 a[KIND == kTileMx4W || split ? 2 : 1][MI], b[2][NJ];
+        u32x4 a[KIND == kTileMx4W || split || f8 ? 2 : 1][held], b[2][NJ];
         uint32_t sa[KIND == kTileMx4W ? 2 : 1][K::scale_i ? MI : 1], sb[2][K::scale_j ? NJ : 1];
     };
     // Where this lane reads: its row of the first block, and the chunk of step 0; steps exchange bits of the chunk.
@@ -317,7 +344,7 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
             }
             b = rb * K::row_j + ((KIND == kTileMx4W ? g * 4 : g) ^ chunk_swap<K::row_j>(r16)) * 16;
             sa = oSI + ra * K::scale_i + g;
-            sb = oSJ + rb * K::scale_j + g;
+            sb = oSJ + rb * K::scale_j + (f8 ? 0 : g);
         }
     };
     static __device__ __forceinline__ void read_a(int set, int m, const char *pi, int s, const Places &at, Frags &f)
@@ -344,7 +371,19 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
     static __device__ __forceinline__ void read_b(int set, int n, const char *pj, int s, const Places &at, Frags &f)
     {
         f.b[set][n] = *(const u32x4 *)(pj + (at.b ^ (s * (KIND == kTileMx4W ? 16 : 64))) + n * 16 * K::row_j);
-        if constexpr (K::scale_j > 0) f.sb[set][n] = *(const uint8_t *)(pj + at.sb + s * 4 + n * 16 * K::scale_j);
+        if constexpr (f8) f.sb[set][n] = *(const uint32_t *)(pj + at.sb + n * 16 * K::scale_j);
+        else if constexpr (K::scale_j > 0) f.sb[set][n] = *(const uint8_t *)(pj + at.sb + s * 4 + n * 16 * K::scale_j);
+    }
+    // kTileF8: block m of I, both halves, into its place among those held; a block of J with its scale.
+    static __device__ __forceinline__ void read_a8(int m, const char *pi, const Places &at, Frags &f)
+    {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) f.a[s][m % held] = *(const u32x4 *)(pi + (at.a ^ (s * 64)) + m * 16 * K::row_i);
+    }
+    static __device__ __forceinline__ void read_b8(int n, const char *pj, const Places &at, Frags &f)
+    {
+        f.b[1][n] = *(const u32x4 *)(pj + (at.b ^ 64) + n * 16 * K::row_j);
+        read_b(0, n, pj, 0, at, f);
     }
     // Row mi of blocks times the J blocks of `set`.  kTileMx4W: a lane holds the 32 codes of block l / 16 of its row; matrix
     // instruction t of four takes codes 8 t .. + 7 of every lane, and the same k of J.
@@ -363,6 +402,12 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
 #pragma unroll
             for (int nj = 0; nj < NJ; ++nj) asm volatile("" : "+v"(acc[mi][nj]));
         }
+    }
+
+    static __device__ __forceinline__ void add_scaled(f32x4 &sum, const f32x4 &p, float factor)
+    {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[r] = fmaf(p[r], factor, sum[r]);
     }
 
     // The tile of `w` once more, as binary32 products, each lane's operands straight from memory.  Parts of an infinity are no number, nor is
@@ -484,16 +529,30 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
         advance();
         wait_loads_and_barrier<li + lj>();
         Frags f;
+        if constexpr (f8) {
 #pragma unroll
-        for (int x = 0; x < NJ; ++x) read_b(0, x, j0p, 0, places, f);
+            for (int x = 0; x < NJ; ++x) read_b8(x, j0p, places, f);
 #pragma unroll
-        for (int x = 0; x < MI; ++x) read_a(0, x, i0p, 0, places, f);
+            for (int x = 0; x < held; ++x) read_a8(x, i0p, places, f);
+        } else {
+#pragma unroll
+            for (int x = 0; x < NJ; ++x) read_b(0, x, j0p, 0, places, f);
+#pragma unroll
+            for (int x = 0; x < MI; ++x) read_a(0, x, i0p, 0, places, f);
+        }
         if constexpr (split) {
 #pragma unroll
             for (int x = 0; x < NJ; ++x) read_b(1, x, j0p, 1, places, f);
 #pragma unroll
             for (int x = 0; x < MI; ++x) read_a(1, x, i0p, 1, places, f);
         }
+        // kTileF8: the scale of this wavefront's rows of I, which lie within 128, in stage s of a tile (rows behind the last: any)
+        auto scale_of_i = [&](const Work &v, int s) {
+            static_assert(!f8 || (TI % 128 == 0 && 128 % (MI * 16) == 0), "a wavefront's rows share their scales");
+            const int row = min(v.i0 + wave / WJ * (MI * 16), I.rows - 1) / 128;
+            return *(const __attribute__((address_space(4))) float *)(uintptr_t)(I.scales + (int64_t)row * I.scale_stride + (v.first + s) * 4);
+        };
+        float i_scale = 0.f;
         int stores = 0;                                          // 1: STORES stores are younger than the loads that are waited for next
         constexpr int steps = KIND == kTileMx4W ? 4 : K::steps, last = steps - 1;
         constexpr int hold = KIND == kTileMx4W || MI < 4 ? 0 : 1;          // the row of blocks behind which a stage is handed on
@@ -599,8 +658,71 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
                     p = j0p; j0p = j1p; j1p = p;
                 }
             };
+            // 8-bit products: a stage has one scale, so every block's products of a stage leave the matrix unit by themselves and are added with their
+            // factor by the vector unit, while the next ones are under way.  The barrier that hands both places on comes where the last of a stage's
+            // blocks have been read.
+            auto f8_stage = [&](int s) {
+                if constexpr (f8) {
+                    constexpr bool wide = KIND == kTileF8x;
+                    constexpr int hold = MI - held, behind = wide ? 1 : 2;
+                    float factor[NJ];
+                    const float own = i_scale;
+                    if (s + 1 < w.n) i_scale = scale_of_i(w, s + 1);
+#pragma unroll
+                    for (int n = 0; n < NJ; ++n) factor[n] = __uint_as_float(f.sb[0][n]) * own;
+                    Bf16Pair b[wide ? 2 : 1][NJ];
+                    if constexpr (wide) {
+#pragma unroll
+                        for (int n = 0; n < NJ; ++n) { b[0][n] = codes8_to_bf16(f.b[0][n]); b[1][n] = codes8_to_bf16(f.b[1][n]); }
+                    }
+                    f32x4 p[behind + 1];
+                    // here and not at the end of the stage, to which the compiler would put them off, with every block's products held in registers until then
+                    auto add = [&](int t) {
+                        add_scaled(acc[t / NJ][t % NJ], p[t % (behind + 1)], factor[t % NJ]);
+                        asm volatile("" : "+v"(acc[t / NJ][t % NJ]));
+                    };
+#pragma unroll
+                    for (int mi = 0; mi < MI; ++mi) {
+                        if (mi == hold) hand_on();
+                        Bf16Pair a[2];
+                        if constexpr (wide) { a[0] = codes8_to_bf16(f.a[0][mi % held]); a[1] = codes8_to_bf16(f.a[1][mi % held]); }
+#pragma unroll
+                        for (int n = 0; n < NJ; ++n) {
+                            const int t = mi * NJ + n;
+                            if constexpr (wide) {
+                                f32x4 q = {0.f, 0.f, 0.f, 0.f};
+                                q = mma_bf16(a[0].lo, b[0][n].lo, q);
+                                q = mma_bf16(a[0].hi, b[0][n].hi, q);
+                                q = mma_bf16(a[1].lo, b[1][n].lo, q);
+                                p[t % (behind + 1)] = mma_bf16(a[1].hi, b[1][n].hi, q);
+                            } else {
+                                p[t % (behind + 1)] = mma_f8(f.a[0][mi % held], f.a[1][mi % held], f.b[0][n], f.b[1][n]);
+                            }
+                            if (t >= behind) add(t - behind);
+                            if (mi == MI - 1) read_b8(n, j1p, places, f);
+                        }
+                        if (mi >= hold) {
+#pragma unroll
+                            for (int x = (mi - hold) * lj / held; x < (mi - hold + 1) * lj / held; ++x) load_j(x, j0p);
+#pragma unroll
+                            for (int x = (mi - hold) * li / held; x < (mi - hold + 1) * li / held; ++x) load_i(x, i0p);
+                            read_a8(mi - hold, i1p, places, f);
+                        } else {
+                            read_a8(mi + held, i0p, places, f);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int t = MI * NJ > behind ? MI * NJ - behind : 0; t < MI * NJ; ++t) add(t);
+                    advance();
+                    char *q = i0p; i0p = i1p; i1p = q; i2p = q;
+                    q = j0p; j0p = j1p; j1p = q;
+                }
+            };
+            if constexpr (f8) i_scale = scale_of_i(w, 0);
             for (int s = 0; s < w.n; ++s) {
-                if constexpr (split) split_stage();
+                if constexpr (f8) f8_stage(s);
+                else if constexpr (split) split_stage();
                 else {
                     early_steps();
                     last_step();

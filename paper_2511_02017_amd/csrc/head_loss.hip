@@ -6,26 +6,16 @@
 // The logits are never kept: the forward pass leaves a maximum and a sum for each tile of the vocabulary, and the backward
 // pass forms the logits of one piece of the vocabulary again, turns them into g in the matrix instructions' accumulators and
 // writes g, rounded to the operands' type, in both orientations, so that both products that follow read their operands along k.
-#include "head.h"
+#include "head_loss_device.h"
 
 namespace tapout {
 namespace {
-
-template <int DT> struct ElemOf { using T = float; };
-template <> struct ElemOf<TAPOUT_BF16> { using T = __bf16; };
 
 // Eight neighbouring results.
 __device__ __forceinline__ void store8(float *to, f32x4 a, f32x4 b) { ((f32x4 *)to)[0] = a; ((f32x4 *)to)[1] = b; }
 __device__ __forceinline__ void store8(__bf16 *to, f32x4 a, f32x4 b)
 {
     *(bf16x8 *)to = bf16x8{(__bf16)a[0], (__bf16)a[1], (__bf16)a[2], (__bf16)a[3], (__bf16)b[0], (__bf16)b[1], (__bf16)b[2], (__bf16)b[3]};
-}
-
-__device__ __forceinline__ bool row_counts(int t, int V, const float *lse, const float *row_weight, int n)
-{
-    if (counted_target(t, V) < 0) return false;
-    const float l = lse[n];
-    return fabsf(l) < INFINITY && (!row_weight || row_weight[n] != 0.f);
 }
 
 // ---- forward -----------------------------------------------------------------------------------------
@@ -46,7 +36,7 @@ __global__ __launch_bounds__(T::threads, T::per_simd) void head_loss_kernel(Loss
 #pragma unroll
             for (int n = 0; n < T::NJ; ++n) {
                 const int j = w.j0 + T::j_of(n);
-                target[n] = j < a.N ? a.target[j] : -1;
+                target[n] = j < a.N && a.target ? a.target[j] : -1;
             }
         },
         [&](const Work &w, typename T::Acc &acc) {
@@ -91,38 +81,14 @@ __global__ __launch_bounds__(T::threads, T::per_simd) void head_loss_kernel(Loss
         });
 }
 
-// A workgroup a row: the blocks' maxima and sums to lse, in double (bound by memory: 8192 rows of 1002 blocks 21 us, 3.1 TB/s).
+// A workgroup a row (bound by memory: 8192 rows of 1002 blocks 21 us, 3.1 TB/s).
 __global__ __launch_bounds__(256) void head_loss_join_kernel(LossArgs a, int blocks)
 {
     __shared__ float maxima[4];
     __shared__ double sums[4];
-    const int n = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float2 *p = a.part + (int64_t)n * blocks;
-    float m = -INFINITY;
-    double s = 0.0;
-    for (int x = threadIdx.x; x < blocks; x += 1024) {
-        float2 q[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) q[k] = x + k * 256 < blocks ? p[x + k * 256] : float2{-INFINITY, 0.f};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float top = fmaxf(m, q[k].x), ref = top == -INFINITY ? 0.f : top;
-            s = s * (double)__builtin_amdgcn_exp2f((fmaxf(m, -3.4e38f) - ref) * kLog2e) + (double)q[k].y * (double)__builtin_amdgcn_exp2f((fmaxf(q[k].x, -3.4e38f) - ref) * kLog2e);
-            m = top;
-        }
-    }
-    const float own = m;
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    if (lane == 0) maxima[wave] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
-    const float ref = m == -INFINITY ? 0.f : m;
-    s *= (double)__builtin_amdgcn_exp2f((fmaxf(own, -3.4e38f) - ref) * kLog2e);
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    if (lane == 0) sums[wave] = s;
-    __syncthreads();
+    const int n = blockIdx.x;
+    const double lse = join_lse(a.part + (int64_t)n * blocks, blocks, maxima, sums);
     if (threadIdx.x) return;
-    const double lse = (double)ref + log(((sums[0] + sums[1]) + sums[2]) + sums[3]);
     const int t = counted_target(a.target[n], a.V);
     const bool bad = !(fabs(lse) < (double)INFINITY);
     const float nan = __uint_as_float(0x7fc00000u);
@@ -159,7 +125,7 @@ __global__ __launch_bounds__(T::threads, T::per_simd) void head_grad_kernel(Grad
             for (int n = 0; n < T::NJ; ++n) {
                 const int j = w.j0 + T::j_of(n);
                 const bool live = counted_target(target[n], a.V) >= 0 && fabsf(lse[n]) < INFINITY && weight[n] != 0.f;
-                const int hot = target[n] - a.v0 - w.i0, end = live ? a.n - w.i0 : 0;
+                const int hot = a.listed ? -1 : target[n] - a.v0 - w.i0, end = live ? a.n - w.i0 : 0;
 #pragma unroll
                 for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
@@ -317,6 +283,7 @@ template <class T> hipError_t loss_with(const LossArgs &a, hipStream_t st)
         head_loss_kernel<T><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
     });
     if (e != hipSuccess) return e;
+    if (a.ids) return launch_listed_join(a, ni * T::WI, st);
     head_loss_join_kernel<<<a.N, 256, 0, st>>>(a, ni * T::WI);
     return hipGetLastError();
 }

@@ -156,6 +156,13 @@ template <class E> hipError_t logits_of(const LogitsArgs &a, int kind, hipStream
         return a.N <= 16 ? logits_with<Tile<kTileMx4, 128, 16, 4, 1>, E>(a, st) : a.N <= 32 ? logits_with<Tile<kTileMx4, 128, 32, 4, 1>, E>(a, st)
              : a.N <= 64 ? logits_with<Tile<kTileMx4, 128, 64, 4, 1>, E>(a, st) : a.N <= 128 ? logits_with<Tile<kTileMx4, 256, 128, 4, 2>, E>(a, st)
              : logits_with<Tile<kTileMx4, 256, 256, 2, 4>, E>(a, st);
+    if (kind == kTileF8)
+        return a.N <= 16 ? logits_with<Tile<kTileF8, 128, 16, 4, 1>, E>(a, st) : a.N <= 32 ? logits_with<Tile<kTileF8, 128, 32, 4, 1>, E>(a, st)
+             : a.N <= 64 ? logits_with<Tile<kTileF8, 128, 64, 4, 1>, E>(a, st) : a.N <= 128 ? logits_with<Tile<kTileF8, 256, 128, 4, 2>, E>(a, st)
+             : logits_with<Tile<kTileF8, 256, 256, 2, 4>, E>(a, st);
+    if (kind == kTileF8x)
+        return a.N <= 16 ? logits_with<Tile<kTileF8x, 128, 16, 4, 1>, E>(a, st) : a.N <= 32 ? logits_with<Tile<kTileF8x, 128, 32, 4, 1>, E>(a, st)
+             : a.N <= 64 ? logits_with<Tile<kTileF8x, 128, 64, 4, 1>, E>(a, st) : logits_with<Tile<kTileF8x, 128, 128, 2, 2>, E>(a, st);
     // hidden states of 16 bits: they pass through LDS with the weights, four times their bytes for a row each, so tiles are long in I; V = 128256,
     // dim = 2048, us with tiles of 128 x 16 / 256 x 32 / 256 x 64 / 256 x 128: 1 row 27 / 28 / 36 / 55, 32 rows 45 / 30 / 36 / 52, 64 rows
     // 81 / 51 / 39 / 55, 128 rows 150 / 93 / 68 / 59, 512 rows 572 / 354 / 272 / 217 (128 x 128: 304)
@@ -192,6 +199,7 @@ hipError_t launch_mx4_dequantize(const DequantArgs &a, int dtype, hipStream_t st
 
 hipError_t launch_head_logits(const LogitsArgs &a, int kind, int dtype_out, hipStream_t st)
 {
+    if (kind == kTileF8) return dtype_out == TAPOUT_F32 ? logits_of<float>(a, kTileF8x, st) : logits_of<__bf16>(a, kTileF8, st);
     return dtype_out == TAPOUT_F32 ? logits_of<float>(a, kind, st) : logits_of<__bf16>(a, kind, st);
 }
 

@@ -31,6 +31,13 @@ struct Library {
     decltype(&tapout_head_logits_mx4) head_logits;
     decltype(&tapout_head_loss) head_loss;
     decltype(&tapout_head_loss_grad) head_loss_grad;
+    decltype(&tapout_fp8_quantize) fp8_quantize;
+    decltype(&tapout_fp8_dequantize) fp8_dequantize;
+    decltype(&tapout_head_logits_fp8) head_logits_fp8;
+    decltype(&tapout_head_norm) head_norm;
+    decltype(&tapout_head_norm_grad) head_norm_grad;
+    decltype(&tapout_head_distill) head_distill;
+    decltype(&tapout_head_distill_grad) head_distill_grad;
 } g_lib = {};
 
 constexpr auto kF32 = at::kFloat, kF64 = at::kDouble, kI32 = at::kInt, kU8 = at::kByte;
@@ -490,6 +497,178 @@ PyObject *head_loss_grad(PyObject *const *p)
     return call(a, [&] { return g_lib.head_loss_grad(h, &x, &w, (int32_t)B, (int32_t)K, (int32_t)V, target, lse, rw, scale, &gh, &gw, st); });
 }
 
+int64_t block_count(int64_t rows, int64_t block) { return block < 1 ? -1 : (rows + block - 1) / block; }
+
+// (x, block_rows, codes, scales, stream)
+PyObject *fp8_quantize(PyObject *const *p)
+{
+    Args a;
+    int64_t rows = 0, cols = 0;
+    const tapout_matrix x = a.matrix(p[0], &rows, &cols);
+    const int32_t block = a.i32(p[1]);
+    a.device(c10::hip::current_device(), {p[0], p[2], p[3]});
+    const int64_t P = codes_cols(cols);
+    uint8_t *codes = a.required<uint8_t>(p[2], kU8, {rows, P});
+    float *scales = a.required<float>(p[3], kF32, {block_count(rows, block), P / 128});
+    void *st = a.stream(p[4]);
+    if (!g_lib.fp8_quantize) a.ok = false;
+    return call(a, [&] { return g_lib.fp8_quantize(&x, (int32_t)rows, (int32_t)cols, block, codes, scales, st); });
+}
+
+// (codes, scales, cols, block_rows, out, stream)
+PyObject *fp8_dequantize(PyObject *const *p)
+{
+    Args a;
+    int64_t rows = 0, cols = 0;
+    const tapout_matrix out = a.matrix(p[4], &rows, &cols);
+    a.device(c10::hip::current_device(), {p[0], p[1], p[4]});
+    if (cols != a.i32(p[2])) a.ok = false;
+    const int32_t block = a.i32(p[3]);
+    const int64_t P = codes_cols(cols);
+    uint8_t *codes = a.required<uint8_t>(p[0], kU8, {rows, P});
+    float *scales = a.required<float>(p[1], kF32, {block_count(rows, block), P / 128});
+    void *st = a.stream(p[5]);
+    if (!g_lib.fp8_dequantize) a.ok = false;
+    return call(a, [&] { return g_lib.fp8_dequantize(codes, scales, (int32_t)rows, (int32_t)cols, block, &out, st); });
+}
+
+// (head, dim, dtype, device, hidden or its codes, act_scales, codes, scales, k_len, out, stream)
+PyObject *head_logits_fp8(PyObject *const *p)
+{
+    Args a;
+    tapout_head *h = (tapout_head *)a.ctx(p[0]);
+    const int64_t dim = a.i32(p[1]), dtype = a.i32(p[2]), dev = a.i32(p[3]);
+    a.device(dev, {p[4], p[5], p[6], p[7], p[8], p[9]});
+    int64_t B = 0, K = 0, Bo = 0, Ko = 0, V = 0;
+    const tapout_logits out = a.logits(p[9], &Bo, &Ko, &V);
+    const int64_t P = codes_cols(dim);
+    tapout_logits x = {};
+    const uint8_t *act = nullptr;
+    const float *act_scales = nullptr;
+    const bool coded = p[5] != Py_None;
+    if (coded) {
+        act = a.required<uint8_t>(p[4], kU8, {Bo, Ko, P});
+        act_scales = a.required<float>(p[5], kF32, {Bo, Ko, P / 128});
+    } else {
+        x = a.hidden(p[4], dim, dtype, &B, &K);
+        if (Bo != B || Ko != K) a.ok = false;
+    }
+    const uint8_t *codes = a.required<uint8_t>(p[6], kU8, {V, P});
+    const float *scales = a.required<float>(p[7], kF32, {block_count(V, 128), P / 128});
+    const int32_t *k_len = a.ptr<int32_t>(p[8], kI32, {Bo});
+    void *st = a.stream_on(dev, p[10]);
+    if (!g_lib.head_logits_fp8) a.ok = false;
+    return call(a, [&] { return g_lib.head_logits_fp8(h, coded ? nullptr : &x, act, act_scales, codes, scales, (int32_t)Bo, (int32_t)Ko, (int32_t)V, k_len, &out, st); });
+}
+
+// (head, dim, dtype, device, x, residual, weight, eps, sum, out, stream)
+PyObject *head_norm(PyObject *const *p)
+{
+    Args a;
+    tapout_head *h = (tapout_head *)a.ctx(p[0]);
+    const int64_t dim = a.i32(p[1]), dtype = a.i32(p[2]), dev = a.i32(p[3]);
+    int64_t B = 0, K = 0;
+    const tapout_logits x = a.hidden(p[4], dim, dtype, &B, &K);
+    PyObject *out = a.dict(p[9]);
+    if (!a.ok || !PyFloat_CheckExact(p[7])) Py_RETURN_NONE;
+    auto rows = [&](PyObject *o, tapout_logits *l) -> const tapout_logits * {
+        if (!o || o == Py_None) return nullptr;
+        int64_t Br = 0, Kr = 0;
+        *l = a.hidden(o, dim, dtype, &Br, &Kr);
+        if (Br != B || Kr != K) a.ok = false;
+        return l;
+    };
+    tapout_logits lr = {}, ls = {}, lo = {};
+    PyObject *o = PyDict_GetItemString(out, "out");
+    const tapout_logits *res = rows(p[5], &lr), *sum = rows(p[8], &ls), *y = rows(o, &lo);
+    const at::ScalarType type = dtype == TAPOUT_F32 ? kF32 : at::kBFloat16;
+    const void *w = a.required(p[6], type, {dim});
+    const int64_t P = codes_cols(dim);
+    uint8_t *codes = a.out<uint8_t>(out, "codes", kU8, {B, K, P});
+    float *scales = a.out<float>(out, "scales", kF32, {B, K, P / 128}), *rstd = a.out<float>(out, "rstd", kF32, {B, K});
+    a.device(dev, {p[4], p[5], p[6], p[8], o, PyDict_GetItemString(out, "codes"), PyDict_GetItemString(out, "scales"), PyDict_GetItemString(out, "rstd")});
+    void *st = a.stream_on(dev, p[10]);
+    if (!g_lib.head_norm) a.ok = false;
+    return call(a, [&] { return g_lib.head_norm(h, &x, res, w, (float)PyFloat_AS_DOUBLE(p[7]), (int32_t)B, (int32_t)K, sum, y, codes, scales, rstd, st); });
+}
+
+// (head, dim, dtype, device, grad_out, sum, weight, rstd, grad_sum, grad_x, grad_weight, stream)
+PyObject *head_norm_grad(PyObject *const *p)
+{
+    Args a;
+    tapout_head *h = (tapout_head *)a.ctx(p[0]);
+    const int64_t dim = a.i32(p[1]), dtype = a.i32(p[2]), dev = a.i32(p[3]);
+    a.device(dev, {p[4], p[5], p[6], p[7], p[8], p[9], p[10]});
+    int64_t B = 0, K = 0, Bs = 0, Ks = 0, Bx = 0, Kx = 0, Bm = 0, Km = 0;
+    const tapout_logits g = a.hidden(p[4], dim, dtype, &B, &K), s = a.hidden(p[5], dim, dtype, &Bs, &Ks), x = a.hidden(p[9], dim, dtype, &Bx, &Kx);
+    tapout_logits more = {};
+    const bool has = p[8] != Py_None;
+    if (has) {
+        more = a.hidden(p[8], dim, dtype, &Bm, &Km);
+        if (Bm != B || Km != K) a.ok = false;
+    }
+    if (Bs != B || Ks != K || Bx != B || Kx != K) a.ok = false;
+    const at::ScalarType type = dtype == TAPOUT_F32 ? kF32 : at::kBFloat16;
+    const void *w = a.required(p[6], type, {dim});
+    void *gw = a.required(p[10], type, {dim});
+    const float *rstd = a.required<float>(p[7], kF32, {B, K});
+    void *st = a.stream_on(dev, p[11]);
+    if (!g_lib.head_norm_grad) a.ok = false;
+    return call(a, [&] { return g_lib.head_norm_grad(h, &g, &s, w, rstd, has ? &more : nullptr, (int32_t)B, (int32_t)K, &x, gw, st); });
+}
+
+// The teacher's lists [B, K, T]: T, or 0 where they are not in order.
+int64_t list_length(Args &a, PyObject *ids)
+{
+    const at::Tensor *t = a.tensor(ids);
+    if (!t || t->dim() != 3 || t->size(2) > INT32_MAX) { a.ok = false; return 0; }
+    return t->size(2);
+}
+
+// (head, dim, dtype, device, hidden, weight, top_ids, top_logits, teacher_lse, out, stream)
+PyObject *head_distill(PyObject *const *p)
+{
+    Args a;
+    tapout_head *h = (tapout_head *)a.ctx(p[0]);
+    const int64_t dim = a.i32(p[1]), dtype = a.i32(p[2]), dev = a.i32(p[3]);
+    int64_t B = 0, K = 0, V = 0, D = 0;
+    const tapout_logits x = a.hidden(p[4], dim, dtype, &B, &K);
+    const tapout_matrix w = a.matrix(p[5], &V, &D);
+    if (D != dim || w.dtype != dtype) a.ok = false;
+    const int64_t T = list_length(a, p[6]);
+    const int32_t *ids = a.required<int32_t>(p[6], kI32, {B, K, T});
+    const float *logits = a.required<float>(p[7], kF32, {B, K, T}), *given = a.ptr<float>(p[8], kF32, {B, K});
+    PyObject *out = a.dict(p[9]);
+    if (!a.ok) Py_RETURN_NONE;
+    float *loss = a.need<float>(out, "loss", kF32, {B, K}), *lse = a.need<float>(out, "lse", kF32, {B, K}), *top = a.need<float>(out, "top", kF32, {B, K, T});
+    uint32_t *flags = a.out<uint32_t>(out, "flags", kI32, {B});
+    a.device(dev, {p[4], p[5], p[6], p[7], p[8], PyDict_GetItemString(out, "loss"), PyDict_GetItemString(out, "lse"), PyDict_GetItemString(out, "top"),
+                   PyDict_GetItemString(out, "flags")});
+    void *st = a.stream_on(dev, p[10]);
+    if (!g_lib.head_distill) a.ok = false;
+    return call(a, [&] { return g_lib.head_distill(h, &x, &w, (int32_t)B, (int32_t)K, (int32_t)V, ids, logits, (int32_t)T, given, loss, lse, top, flags, st); });
+}
+
+// (head, dim, dtype, device, hidden, weight, top_ids, top_logits, teacher_lse, lse, top, row_weight, scale, grad_hidden, grad_weight, stream)
+PyObject *head_distill_grad(PyObject *const *p)
+{
+    Args a;
+    tapout_head *h = (tapout_head *)a.ctx(p[0]);
+    const int64_t dim = a.i32(p[1]), dtype = a.i32(p[2]), dev = a.i32(p[3]);
+    a.device(dev, {p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13], p[14]});
+    int64_t B = 0, K = 0, V = 0, D = 0, Bg = 0, Kg = 0, Vg = 0, Dg = 0;
+    const tapout_logits x = a.hidden(p[4], dim, dtype, &B, &K), gh = a.hidden(p[13], dim, dtype, &Bg, &Kg);
+    const tapout_matrix w = a.matrix(p[5], &V, &D), gw = a.matrix(p[14], &Vg, &Dg);
+    if (D != dim || w.dtype != dtype || Dg != dim || gw.dtype != dtype || Bg != B || Kg != K || Vg != V) a.ok = false;
+    const int64_t T = list_length(a, p[6]);
+    const int32_t *ids = a.required<int32_t>(p[6], kI32, {B, K, T});
+    const float *logits = a.required<float>(p[7], kF32, {B, K, T}), *given = a.ptr<float>(p[8], kF32, {B, K}), *lse = a.required<float>(p[9], kF32, {B, K}),
+                *top = a.required<float>(p[10], kF32, {B, K, T}), *rw = a.ptr<float>(p[11], kF32, {B, K}), *scale = a.ptr<float>(p[12], kF32, {1});
+    void *st = a.stream_on(dev, p[15]);
+    if (!g_lib.head_distill_grad) a.ok = false;
+    return call(a, [&] { return g_lib.head_distill_grad(h, &x, &w, (int32_t)B, (int32_t)K, (int32_t)V, ids, logits, (int32_t)T, given, lse, top, rw, scale, &gh, &gw, st); });
+}
+
 // load(path): the entry points of this build of the library
 PyObject *load(PyObject *, PyObject *arg)
 {
@@ -511,6 +690,9 @@ PyObject *load(PyObject *, PyObject *arg)
     if (!ok) { PyErr_Format(PyExc_ImportError, "%s lacks an entry point", path); return nullptr; }
     get(l.mx4_quantize, "tapout_mx4_quantize"); get(l.mx4_dequantize, "tapout_mx4_dequantize"); get(l.head_logits, "tapout_head_logits_mx4");
     get(l.head_loss, "tapout_head_loss"); get(l.head_loss_grad, "tapout_head_loss_grad");
+    get(l.fp8_quantize, "tapout_fp8_quantize"); get(l.fp8_dequantize, "tapout_fp8_dequantize"); get(l.head_logits_fp8, "tapout_head_logits_fp8");
+    get(l.head_norm, "tapout_head_norm"); get(l.head_norm_grad, "tapout_head_norm_grad");
+    get(l.head_distill, "tapout_head_distill"); get(l.head_distill_grad, "tapout_head_distill_grad");
     g_lib = l;
     Py_RETURN_NONE;
 }
@@ -532,6 +714,8 @@ PyMethodDef g_methods[] = {
     ENTRY(bandit_select, 8), ENTRY(draft_stats, 9), ENTRY(verify, 12), ENTRY(bandit_update, 9), ENTRY(bandit_update_select, 13),
     ENTRY(shard_stats, 8), ENTRY(draft_stats_sharded, 11), ENTRY(verify_accept_sharded, 13), ENTRY(shard_final_sums, 6), ENTRY(shard_final_token, 14),
     ENTRY(mx4_quantize, 4), ENTRY(mx4_dequantize, 5), ENTRY(head_logits, 11), ENTRY(head_loss, 9), ENTRY(head_loss_grad, 13),
+    ENTRY(fp8_quantize, 5), ENTRY(fp8_dequantize, 6), ENTRY(head_logits_fp8, 11), ENTRY(head_norm, 11), ENTRY(head_norm_grad, 12),
+    ENTRY(head_distill, 11), ENTRY(head_distill_grad, 16),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
