@@ -248,6 +248,44 @@ TAPOUT_API tapout_status tapout_draft_stats(tapout_ctx *ctx, const tapout_logits
                                  int32_t *n_stop, uint8_t *stop_fired, uint32_t *flags, void *stream);
 
 /*
+ * Tokens under a temperature and filters, and the filtered logits.  The filtered
+ * rows are logits like any other: tapout_draft_stats and tapout_verify on the
+ * filtered draft and target rows make a round of speculative sampling that emits
+ * tokens of the filtered target distribution.
+ *   For every row x, with T = temperature[b]:
+ *     d_j = (x_j - max x) / T,  w_j = exp(d_j)
+ *     order: larger x first, equal ones by index (-infinity: masked, never kept)
+ *     top_k[b] in [1, V): the first top_k of the order; else no limit
+ *     top_p[b] < 1: the shortest run from its start whose mass is at least top_p of
+ *       the mass that top_k left (its first always); else no limit
+ *     min_p[b] > 0: those with w_j >= min_p (the largest always); else no limit
+ *     kept = d_j where all three keep j, else -infinity
+ *     token = smallest j whose inclusive sum of the kept w exceeds u * Z, Z their
+ *       sum;  logq = d_token - ln Z
+ *   T <= 0: greedy, the argmax (smallest index) alone is kept (kept 0, logq 0);
+ *   T = +infinity: all weights are 1.
+ *   Weights are computed in double and summed as whole multiples of 2^-s of the
+ *   largest, s = min(50, 62 - ceil(log2 V)): results do not depend on how the work
+ *   is divided.
+ * logits   [B,K,V], K up to max_k + 1 (target rows);  V at most 2^24
+ * k_len    [B] i32 or NULL: rows k >= k_len[b] are not read, their outputs untouched
+ * temperature, top_p, min_p [B] f32, top_k [B] i32, each or NULL (1, 1, 0, 0)
+ * u        [B,K] f32 in [0,1), or NULL: no tokens are drawn
+ * token    [B,K] i32, with u;  logq [B,K] f32 or NULL
+ * n_kept   [B,K] i32 or NULL: tokens that are kept
+ * kept     [B,K,V] logits, binary32 or bfloat16 at any element-aligned address and
+ *          strides, or NULL
+ * flags    [B] u32 or NULL (overwritten): BAD_ROW, a row that holds a NaN or has no
+ *          finite maximum, or whose temperature is NaN: token -1, logq NaN, nothing
+ *          kept
+ */
+TAPOUT_API tapout_status tapout_sample(tapout_ctx *ctx, const tapout_logits *logits,
+                            int32_t B, int32_t K, int32_t V, const int32_t *k_len,
+                            const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                            const float *u, int32_t *token, float *logq, int32_t *n_kept,
+                            const tapout_logits *kept, uint32_t *flags, void *stream);
+
+/*
  * Verification of the drafted tokens and the final token (Algorithm 1 lines
  * 10-11, with "verify" meaning speculative sampling as in the works the
  * paper's introduction cites).  n = n_draft[b] tokens were drafted; target

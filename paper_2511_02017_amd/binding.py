@@ -31,7 +31,7 @@ FLAG_BAD_ROW, FLAG_BAD_TOKEN, FLAG_BAD_NDRAFT, FLAG_SAMPLER_EXHAUSTED = 1, 2, 4,
 STATUS = {0: "TAPOUT_OK", 1: "TAPOUT_EINVAL", 2: "TAPOUT_EUNSUPPORTED", 3: "TAPOUT_ENOMEM", 4: "TAPOUT_EHIP"}
 
 EXPORTS = ("tapout_default_config", "tapout_create", "tapout_destroy", "tapout_last_error",
-           "tapout_bandit_select", "tapout_draft_stats", "tapout_draft_stats_static", "tapout_verify", "tapout_bandit_update",
+           "tapout_bandit_select", "tapout_draft_stats", "tapout_draft_stats_static", "tapout_sample", "tapout_verify", "tapout_bandit_update",
            "tapout_bandit_update_select", "tapout_round", "tapout_bandit_get_state", "tapout_bandit_set_state", "tapout_rule_state_get", "tapout_rule_state_set",
            "tapout_shard_stats", "tapout_draft_stats_sharded", "tapout_verify_accept_sharded",
            "tapout_shard_final_sums", "tapout_shard_final_token",
@@ -131,6 +131,7 @@ def load_library(path: str = None):
         lib.tapout_verify_accept_sharded.argtypes = [vp, vp, i32, i32, i32, i32] + [vp] * 15
         lib.tapout_shard_final_sums.argtypes = [vp, C.POINTER(TapoutLogits), C.POINTER(TapoutLogits), i32, i32, i32, vp, vp, vp]
         lib.tapout_shard_final_token.argtypes = [vp, C.POINTER(TapoutLogits), C.POINTER(TapoutLogits), i32, i32, i32, i32, i32, i32] + [vp] * 8
+        lib.tapout_sample.argtypes = [vp, C.POINTER(TapoutLogits), i32, i32, i32] + [vp] * 9 + [C.POINTER(TapoutLogits), vp, vp]
         lib.tapout_verify.argtypes = [vp, C.POINTER(TapoutLogits), C.POINTER(TapoutLogits), i32, i32, i32] + [vp] * 15
         lib.tapout_bandit_update.argtypes = [vp, i32] + [vp] * 6
         lib.tapout_bandit_update_select.argtypes = [vp, i32] + [vp] * 9
@@ -535,6 +536,41 @@ class Tapout:
                     n_stop=torch.zeros(B, dtype=torch.int32, device=d),
                     stop_fired=torch.zeros((B, K), dtype=torch.uint8, device=d),
                     flags=torch.zeros(B, dtype=torch.int32, device=d))
+
+    # -- tapout_sample -------------------------------------------------------
+    def sample(self, logits, u=None, temperature=None, top_k=None, top_p=None, min_p=None, k_len=None, kept=None, out=None, stream=None):
+        """tapout_sample: filters logits [B, K, V] by temperature, top_k, top_p, min_p (each [B] or None) and, with u [B, K], draws a token a
+        row.  Returns / fills a dict: n_kept [B, K] int32, flags [B] int32, with u token [B, K] int32 and logq [B, K] float32, and with
+        `kept` (a dtype) the filtered logits kept [B, K, V]."""
+        B, K, V = logits.shape
+        f32, i32 = torch.float32, torch.int32
+        if out is None:
+            e = lambda shape, dt: _empty(shape, dt, self.device, stream)                                   # noqa: E731
+            out = dict(n_kept=e((B, K), i32), flags=e((B,), i32))
+            if u is not None:
+                out.update(token=e((B, K), i32), logq=e((B, K), f32))
+            if kept is not None:
+                out["kept"] = e((B, K, V), kept)
+        st = _fast.sample(self._addr, self.cfg.device, logits, u, temperature, top_k, top_p, min_p, k_len, out, _handle(stream))
+        if st == 0:
+            return out
+        lg, y = _logits(logits, "sampled"), out.get("kept")
+        if y is not None and tuple(y.shape) != (B, K, V):
+            raise ValueError(f"kept: expected shape {(B, K, V)}, got {tuple(y.shape)}")
+        kl = None if y is None else C.byref(_logits(y, "kept"))
+        for t, n in ((logits, "logits"), (u, "u"), (temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p"),
+                     (k_len, "k_len"), *((out.get(n), n) for n in ("token", "logq", "n_kept", "kept", "flags"))):
+            _on(t, self.device, n)
+        self._check(st if st is not None else self._lib.tapout_sample(
+            self._ctx, C.byref(lg), B, K, V, _ptr(k_len, i32, (B,), "k_len"), _ptr(temperature, f32, (B,), "temperature"),
+            _ptr(top_k, i32, (B,), "top_k"), _ptr(top_p, f32, (B,), "top_p"), _ptr(min_p, f32, (B,), "min_p"), _ptr(u, f32, (B, K), "u"),
+            _ptr(out.get("token"), i32, (B, K), "token"), _ptr(out.get("logq"), f32, (B, K), "logq"), _ptr(out.get("n_kept"), i32, (B, K), "n_kept"),
+            kl, _ptr(out.get("flags"), i32, (B,), "flags"), self._on_stream(stream)))
+        return out
+
+    def _on_stream(self, stream):
+        """The stream given, or the current one of the context's device."""
+        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream.cuda_stream
 
     # -- tapout_verify -------------------------------------------------------
     def verify(self, target, draft, draft_lse, logq_tok, draft_tok, n_draft, u_accept, u_sample,

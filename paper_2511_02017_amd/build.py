@@ -19,7 +19,7 @@ OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(PKG, "libtapout.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 LIB_STAMPS = os.path.join(PKG, "libtapout_stamps.so")
-SOURCES = ["row_reduce.hip", "finalize.hip", "verify.hip", "bandit.hip", "api.hip", "head_loss.hip", "head_mx4.hip", "head_fp8.hip",
+SOURCES = ["row_reduce.hip", "finalize.hip", "verify.hip", "bandit.hip", "sample.hip", "api.hip", "head_loss.hip", "head_mx4.hip", "head_fp8.hip",
            "head_norm.hip", "head_distill.hip", "head_api.hip"]
 
 FLAGS = [

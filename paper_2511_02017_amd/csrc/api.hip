@@ -244,6 +244,16 @@ const char *check_logits(const tapout_logits *l, const char *name, int V, int ro
     return nullptr;
 }
 
+constexpr int kMaxFilterVocab = 1 << 24;
+
+// Whether two of the B x K rows of `len` elements share memory.
+bool rows_overlap(const tapout_logits *x, int B, int K, int len)
+{
+    const int64_t b = x->stride_b, k = x->stride_k;
+    if (B == 1 || K == 1) return (K > 1 && k < len) || (B > 1 && b < len);
+    return !(k >= len && b >= (K - 1) * k + len) && !(b >= len && k >= (B - 1) * b + len);
+}
+
 // Enqueue one kernel; when timing of `kind` is on, hand the launcher an event pair that the
 // runtime stamps with the begin and end of the kernel's execution.
 template <class F>
@@ -489,6 +499,35 @@ tapout_status tapout_bandit_select(tapout_ctx *ctx, int32_t B, const float *u_ts
     hipStream_t st = (hipStream_t)stream;
     hipError_t e = timed(ctx, TAPOUT_PROFILE_SELECT, [&](Timing tm) { return launch_bandit_select(a, u_ts, arm_out, flags, st, tm); });
     return e == hipSuccess ? TAPOUT_OK : hip_fail(ctx, e, "bandit_select launch");
+}
+
+tapout_status tapout_sample(tapout_ctx *ctx, const tapout_logits *logits, int32_t B, int32_t K, int32_t V, const int32_t *k_len,
+                            const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, const float *u,
+                            int32_t *token, float *logq, int32_t *n_kept, const tapout_logits *kept, uint32_t *flags, void *stream)
+{
+    if (!ctx) return fail(nullptr, TAPOUT_EINVAL, "ctx is NULL");
+    if (B < 0 || B > ctx->cfg.max_batch) return fail(ctx, TAPOUT_EINVAL, "B = %d outside [0, max_batch = %d]", B, ctx->cfg.max_batch);
+    if (K < 1 || K > ctx->cfg.max_k + 1) return fail(ctx, TAPOUT_EINVAL, "K = %d outside [1, max_k + 1 = %d]", K, ctx->cfg.max_k + 1);
+    if (V < 1 || V > ctx->cfg.vocab) return fail(ctx, TAPOUT_EINVAL, "V = %d outside [1, vocab = %d]", V, ctx->cfg.vocab);
+    if (V > kMaxFilterVocab) return fail(ctx, TAPOUT_EUNSUPPORTED, "V = %d beyond 2^24", V);
+    if (B == 0) return TAPOUT_OK;
+    char buf[128];
+    if (const char *e = check_logits(logits, "sampled", V, K, buf)) return fail(ctx, TAPOUT_EINVAL, "%s", e);
+    if (kept)
+        if (const char *e = check_logits(kept, "kept", V, K, buf)) return fail(ctx, TAPOUT_EINVAL, "%s", e);
+    if (u && !token) return fail(ctx, TAPOUT_EINVAL, "token is NULL");
+    if (!u && (token || logq)) return fail(ctx, TAPOUT_EINVAL, "token and logq need u");
+    if (!u && !kept && !n_kept) return fail(ctx, TAPOUT_EINVAL, "nothing to be written: neither u nor kept nor n_kept is given");
+    if (kept && rows_overlap(kept, B, K, V)) return fail(ctx, TAPOUT_EINVAL, "kept: rows overlap");
+    DeviceGuard guard(ctx->cfg.device);
+    FilterArgs a{};
+    a.base = logits->ptr; a.stride_b = logits->stride_b; a.stride_k = logits->stride_k;
+    a.B = B; a.K = K; a.V = V; a.k_len = k_len;
+    a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u;
+    a.token = token; a.n_kept = n_kept; a.logq = logq; a.flags = flags; a.exp_table = ctx->exp_table;
+    if (kept) { a.kept = (void *)kept->ptr; a.kept_dtype = kept->dtype; a.kept_stride_b = kept->stride_b; a.kept_stride_k = kept->stride_k; }
+    const hipError_t e = launch_filtered_sample(a, logits->dtype, (hipStream_t)stream);
+    return e == hipSuccess ? TAPOUT_OK : hip_fail(ctx, e, "sample");
 }
 
 tapout_status tapout_bandit_update(tapout_ctx *ctx, int32_t B, const int32_t *arm,

@@ -325,6 +325,21 @@ struct ShardFinalArgs {
 hipError_t launch_shard_final_sums(const ShardFinalArgs &a, hipStream_t st);
 hipError_t launch_shard_final_token(const ShardFinalArgs &a, hipStream_t st);
 
+// Tokens under a temperature and filters (sample.hip).
+struct FilterArgs {
+    const void *base; int64_t stride_b, stride_k;
+    int32_t B, K, V;
+    const int32_t *k_len;
+    const float *temperature; const int32_t *top_k; const float *top_p, *min_p;      // [B] each, or NULL
+    const float *u;               // [B, K], or NULL: no token is drawn
+    int32_t *token, *n_kept; float *logq;
+    void *kept; int32_t kept_dtype; int64_t kept_stride_b, kept_stride_k;
+    uint32_t *flags;
+    const double *exp_table;
+    int32_t shift;                // set by the launch
+};
+hipError_t launch_filtered_sample(FilterArgs a, int dtype, hipStream_t st);
+
 constexpr int kSampleSlice = 2048;   // elements per slice of the final-token passes
 
 hipError_t launch_bandit_select(const BanditArgs &a, const float *u_ts, int32_t *arm_out, uint32_t *flags, hipStream_t st, Timing tm);

@@ -31,6 +31,7 @@ struct Library {
     decltype(&tapout_head_logits_mx4) head_logits;
     decltype(&tapout_head_loss) head_loss;
     decltype(&tapout_head_loss_grad) head_loss_grad;
+    decltype(&tapout_sample) sample;
     decltype(&tapout_fp8_quantize) fp8_quantize;
     decltype(&tapout_fp8_dequantize) fp8_dequantize;
     decltype(&tapout_head_logits_fp8) head_logits_fp8;
@@ -408,6 +409,37 @@ PyObject *shard_final_token(PyObject *const *p)
     return call(a, [&] { return g_lib.shard_final_token(c, &t, &d, (int32_t)B, (int32_t)(K1 - 1), (int32_t)V, off, (int32_t)G, g, jobs, sums, exact, u, tok, mass, need, st); });
 }
 
+// (ctx, device, logits, u, temperature, top_k, top_p, min_p, k_len, out, stream)
+PyObject *sample(PyObject *const *p)
+{
+    Args a;
+    tapout_ctx *c = a.ctx(p[0]);
+    const int64_t dev = a.i32(p[1]);
+    int64_t B = 0, K = 0, V = 0, Bk = 0, Kk = 0, Vk = 0;
+    const tapout_logits x = a.logits(p[2], &B, &K, &V);
+    const float *u = a.ptr<float>(p[3], kF32, {B, K}), *temperature = a.ptr<float>(p[4], kF32, {B}), *top_p = a.ptr<float>(p[6], kF32, {B}),
+                *min_p = a.ptr<float>(p[7], kF32, {B});
+    const int32_t *top_k = a.ptr<int32_t>(p[5], kI32, {B}), *k_len = a.ptr<int32_t>(p[8], kI32, {B});
+    PyObject *out = a.dict(p[9]);
+    if (!a.ok) Py_RETURN_NONE;
+    int32_t *token = a.out<int32_t>(out, "token", kI32, {B, K}), *n_kept = a.out<int32_t>(out, "n_kept", kI32, {B, K});
+    float *logq = a.out<float>(out, "logq", kF32, {B, K});
+    uint32_t *flags = a.out<uint32_t>(out, "flags", kI32, {B});
+    PyObject *y = PyDict_GetItemString(out, "kept");
+    tapout_logits kept = {};
+    const bool has = y && y != Py_None;
+    if (has) {
+        kept = a.logits(y, &Bk, &Kk, &Vk);
+        if (Bk != B || Kk != K || Vk != V) a.ok = false;
+    }
+    a.device(dev, {p[2], p[3], p[4], p[5], p[6], p[7], p[8], y, PyDict_GetItemString(out, "token"), PyDict_GetItemString(out, "n_kept"),
+                   PyDict_GetItemString(out, "logq"), PyDict_GetItemString(out, "flags")});
+    void *st = a.stream_on(dev, p[10]);
+    if (!g_lib.sample) a.ok = false;
+    return call(a, [&] { return g_lib.sample(c, &x, (int32_t)B, (int32_t)K, (int32_t)V, k_len, temperature, top_k, top_p, min_p, u, token, logq, n_kept,
+                                             has ? &kept : nullptr, flags, st); });
+}
+
 int64_t codes_cols(int64_t cols) { return (cols + 127) / 128 * 128; }
 
 // (x, codes, scales, stream)
@@ -690,7 +722,7 @@ PyObject *load(PyObject *, PyObject *arg)
     if (!ok) { PyErr_Format(PyExc_ImportError, "%s lacks an entry point", path); return nullptr; }
     get(l.mx4_quantize, "tapout_mx4_quantize"); get(l.mx4_dequantize, "tapout_mx4_dequantize"); get(l.head_logits, "tapout_head_logits_mx4");
     get(l.head_loss, "tapout_head_loss"); get(l.head_loss_grad, "tapout_head_loss_grad");
-    get(l.fp8_quantize, "tapout_fp8_quantize"); get(l.fp8_dequantize, "tapout_fp8_dequantize"); get(l.head_logits_fp8, "tapout_head_logits_fp8");
+    get(l.sample, "tapout_sample"); get(l.fp8_quantize, "tapout_fp8_quantize"); get(l.fp8_dequantize, "tapout_fp8_dequantize"); get(l.head_logits_fp8, "tapout_head_logits_fp8");
     get(l.head_norm, "tapout_head_norm"); get(l.head_norm_grad, "tapout_head_norm_grad");
     get(l.head_distill, "tapout_head_distill"); get(l.head_distill_grad, "tapout_head_distill_grad");
     g_lib = l;
@@ -714,7 +746,7 @@ PyMethodDef g_methods[] = {
     ENTRY(bandit_select, 8), ENTRY(draft_stats, 9), ENTRY(verify, 12), ENTRY(bandit_update, 9), ENTRY(bandit_update_select, 13),
     ENTRY(shard_stats, 8), ENTRY(draft_stats_sharded, 11), ENTRY(verify_accept_sharded, 13), ENTRY(shard_final_sums, 6), ENTRY(shard_final_token, 14),
     ENTRY(mx4_quantize, 4), ENTRY(mx4_dequantize, 5), ENTRY(head_logits, 11), ENTRY(head_loss, 9), ENTRY(head_loss_grad, 13),
-    ENTRY(fp8_quantize, 5), ENTRY(fp8_dequantize, 6), ENTRY(head_logits_fp8, 11), ENTRY(head_norm, 11), ENTRY(head_norm_grad, 12),
+    ENTRY(sample, 11), ENTRY(fp8_quantize, 5), ENTRY(fp8_dequantize, 6), ENTRY(head_logits_fp8, 11), ENTRY(head_norm, 11), ENTRY(head_norm_grad, 12),
     ENTRY(head_distill, 11), ENTRY(head_distill_grad, 16),
     {nullptr, nullptr, 0, nullptr},
 };
