@@ -336,8 +336,13 @@ struct FilterArgs {
     void *kept; int32_t kept_dtype; int64_t kept_stride_b, kept_stride_k;
     uint32_t *flags;
     const double *exp_table;
+    struct FilterRow *rows;       // [B * K]: what each keeps
+    struct FilterSlice *slices;   // [B * K, filter_slices(V)]
     int32_t shift;                // set by the launch
 };
+constexpr int kFilterRowBytes = 40;
+struct FilterSlice { uint64_t units; int32_t kept, pad; };      // of a row's slice: the kept weights, and how many
+int filter_slices(int V, int dtype);
 hipError_t launch_filtered_sample(FilterArgs a, int dtype, hipStream_t st);
 
 constexpr int kSampleSlice = 2048;   // elements per slice of the final-token passes

@@ -4,69 +4,119 @@
 //   top-k: the first k;  top-p: the shortest run from the start whose mass reaches p of the top-k's;  min-p: w_j >= min_p
 //   token: smallest j whose sum of kept weights up to and with j exceeds u Z;  log q = d_token - ln Z
 //
-// All three filters keep a run from the start of the order, so what a row keeps is said by its last element: a key (the logit's bits, mapped to
-// integers that order alike) and the index up to which elements of that key are kept.  The row is not sorted: a histogram over the distance from
-// the maximum names the bin in which the run ends, and the few elements of that bin are ranked among each other (a bin with many is cut again, by
-// keys, down to a single key).
+// All three filters keep a run from the start of the order, so what a row keeps is said by the value of its last element and the index up to
+// which elements of that value are kept (Bound).  The row is not sorted.  Its elements are counted by the upper sixteen bits of their values: for
+// bfloat16 rows these are the values, so counts times weights are the masses and the counts alone say where every run ends; for binary32 rows they
+// name the place in which a run ends, whose few elements are ranked among each other (a place with many is divided again, down to one value).
 //
 // Weights are summed as whole numbers of 2^-S of the largest, S = 62 - log2 V (45 at V = 128256): sums of them do not depend on their order, so
 // any division of the work gives the same bits, and each is off by half a unit, so that a sum is off by about 1e-12 of the largest weight, far
 // less than the gaps between neighbouring sums that a decision could fall into.
+#include <type_traits>
+
 #include "exp_device.h"
 
 namespace tapout {
 namespace {
 
-constexpr int kThreads = 1024, kBins = 2048, kList = 1024, kLoads = 4;
-constexpr float kTopKBins = 256.f;             // bins of a unit of logits where elements are counted
+constexpr int kThreads = 1024, kWaves = kThreads / kWave, kLoads = 4;
+constexpr int kList = 1024, kBins = 2048;
 
-__device__ __forceinline__ uint32_t key_of(float x)             // -0 and 0 are one value
+// ---- values by their upper sixteen bits ----------------------------------------------------------------------
+// Entry 2 e + sign: e = 0 magnitudes below 2^-16, e = 1 .. kRegular those up to 2^7, kRegular + 1 beyond.  Places are entries in falling order of
+// their values; both signs of e = 0 share one.
+constexpr uint32_t kLow = (127 - 16) << 7;
+constexpr int kRegular = 23 * 128, kEntries = 2 * (kRegular + 2), kPlaces = kEntries, kTinyPlace = kRegular + 1;
+constexpr int kPer = (kPlaces + kThreads - 1) / kThreads;                  // places of a thread
+__device__ __forceinline__ int entry_at(int place) { return place <= kTinyPlace ? 2 * (kTinyPlace - place) : 2 * (place - kTinyPlace - 1) + 1; }
+__device__ __forceinline__ int entry_of(float x)
+{
+    const uint32_t u = __float_as_uint(x), m = (u >> 16) & 0x7fffu;
+    const int e = min(max((int)m - (int)(kLow - 1), 0), kRegular + 1);
+    return 2 * e + (int)(u >> 31);
+}
+__device__ __forceinline__ int place_of(float x)
+{
+    const int entry = entry_of(x), e = entry >> 1;
+    return (entry & 1) && e ? kTinyPlace + 1 + e : kTinyPlace - e;
+}
+// The value of a regular place (bfloat16), 0 for the place of the smallest.
+__device__ __forceinline__ float value_at(int place)
+{
+    const int entry = entry_at(place), e = entry >> 1;
+    return e ? __uint_as_float(((uint32_t)(entry & 1) << 31) | ((kLow - 1 + (uint32_t)e) << 16)) : 0.f;
+}
+// Two bfloat16 as they lie in a word to their entries, both at once: six instructions with the addresses.  Of values that are not regular the sign
+// is lost: 0 or 1 for small ones, the last two for large ones.
+__device__ __forceinline__ u16x2 entries_of(uint32_t w)
+{
+    const u16x2 v = __builtin_bit_cast(u16x2, w), sign = v >> (u16x2)(unsigned short)15;
+    u16x2 d;
+    asm("v_pk_mad_u16 %0, %1, 2, %2 op_sel_hi:[1,0,1]" : "=v"(d) : "v"(v), "v"(sign));
+    d = __builtin_elementwise_sub_sat(d, (u16x2)(unsigned short)(2 * (kLow - 1)));
+    return __builtin_elementwise_min(d, (u16x2)(unsigned short)(kEntries - 1));
+}
+
+__device__ __forceinline__ uint32_t key_of(float x)             // ordered like the values; -0 and 0 are one
 {
     const uint32_t u = __float_as_uint(x + 0.f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu)); }
-constexpr uint32_t kMasked = 0x007fffffu;      // the key of -infinity: only larger ones are ever kept
 
-// Last element of a run: keys above, and equal ones up to the index, are in it.
+// Last element of a run: larger values, and equal ones up to the index, are in it.
 struct Bound {
-    uint32_t key; int32_t index;
-    __device__ __forceinline__ bool holds(uint32_t k, int32_t j) const { return k > key || (k == key && j <= index); }
+    float x; int32_t index;
+    __device__ __forceinline__ bool holds(float y, int32_t j) const { return y > x || (y == x && j <= index); }
 };
-__device__ __forceinline__ Bound shorter(Bound a, Bound b) { return a.key > b.key || (a.key == b.key && a.index < b.index) ? a : b; }
+__device__ __forceinline__ float below(float x) { return value_of(key_of(x) - 1); }        // the next smaller value; of 0 a negative one
+constexpr int kAll = 0x7fffffff, kNone = (int)0x80000000u;       // of a value's elements (indices before a row are negative)
+__device__ __forceinline__ Bound shorter(Bound a, Bound b) { return a.x > b.x || (a.x == b.x && a.index < b.index) ? a : b; }
 
 struct Shared {
     double table[256];                         // 2^(k / 256)
-    uint64_t bins[kBins];
-    uint64_t list_w[kList];
-    uint32_t list_key[kList];
-    int32_t list_index[kList];
-    uint64_t waves[kThreads / kWave];
-    float waves_f[kThreads / kWave];
+    union {
+        uint32_t counts[kEntries];
+        uint64_t list[2 * kList];              // a place's elements, and their weights
+    };
+    union {
+        uint64_t units[kEntries];              // measures by entry
+        uint64_t bins[kBins];
+    };
+    uint64_t waves[2][kWaves];
+    uint32_t turn[2][kLoads * kWaves];
+    float waves_f[kWaves];
+    float tiny[64];                            // values that are not 0 in the place of the smallest
     uint32_t lo, hi;
-    int32_t count, found, nan;
+    int32_t count, found, tinies, bad, irregular;
     uint64_t sum;
     Bound bound;
 };
 
 // A row's weights.
 struct Weight {
-    double max, c; int shift;                  // c = 256 / (T ln 2);  shift: log2 of the units of the largest weight
-    // (x - max) / T in units of ln2 / 256, from 0 down to where weights are no unit any more
-    __device__ __forceinline__ double steps(float x) const { return fmax(((double)x - max) * c, -256.0 * 64.0); }
-    __device__ __forceinline__ uint64_t units(double t, int &ni, const double *table) const
+    double max, c; int shift;                  // c = 256 / (T ln 2);  shift: log2 of the units of the largest weight, at most 50
+    __device__ __forceinline__ uint64_t of(float x, const double *table) const
     {
-        const double tm = t + kMagic;
-        ni = __double2loint(tm);
+        // (x - max) / T in units of ln2 / 256, down to where weights are no unit any more
+        const double t = fmax(((double)x - max) * c, -256.0 * 64.0), tm = t + kMagic;
+        const int ni = __double2loint(tm);
         const double r = t - (tm - kMagic), tk = table[ni & 255];
         const double q = r * fma(r, fma(r, fma(r, kExpC1 * kExpC1 * kExpC1 * kExpC1 / 24.0, kExpC3), kExpC2), kExpC1);
-        const double e = ldexp(fma(tk, q, tk), (ni >> 8) + shift);
-        return (uint64_t)(__double_as_longlong(e + 4503599627370496.0) & 0xfffffffffffffll);          // to nearest: e is at most 2^50
+        const double e = fma(tk, q, tk);       // in [1, 2): scaled through the exponent field
+        const double s = __hiloint2double(__double2hiint(e) + ((ni >> 8) + shift) * 0x100000, __double2loint(e)) + 4503599627370496.0;
+        return ((uint64_t)(__double2hiint(s) & 0xfffff) << 32) | (uint32_t)__double2loint(s);          // to nearest: below 2^52
     }
-    __device__ __forceinline__ uint64_t of(float x, const double *table) const { int ni; return units(steps(x), ni, table); }
 };
 
-// Sixteen bytes of a row, as values; what lies outside it is -infinity.
+// What all threads of a workgroup hold alike, in scalar registers: branches on it are the wavefront's own.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uniform(float v) { return __int_as_float(uniform(__float_as_int(v))); }
+__device__ __forceinline__ double uniform(double v) { return __hiloint2double(uniform(__double2hiint(v)), uniform(__double2loint(v))); }
+__device__ __forceinline__ uint64_t uniform(uint64_t v) { return ((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v); }
+__device__ __forceinline__ Bound uniform(Bound b) { return Bound{uniform(b.x), uniform(b.index)}; }
+
+// ---- a row's vectors -----------------------------------------------------------------------------------------
 template <int DT> struct RowReader {
     static constexpr int n = Elem<DT>::vec;
     const char *base;                          // the row's start rounded down to 16 bytes
@@ -79,227 +129,296 @@ template <int DT> struct RowReader {
     }
     __device__ __forceinline__ int first(int v) const { return v * n - before; }        // index of a vector's first element
     __device__ __forceinline__ bool whole(int v) const { return first(v) >= 0 && first(v) + n <= V; }
-    __device__ __forceinline__ void load(int v, float (&x)[n]) const
+    // what lies outside the row is -infinity, and is not read
+    __device__ __forceinline__ u32x4 load(int v) const
     {
-        if (v < vecs && whole(v)) {
-            unpack<DT>(*(const u32x4 *)(base + (int64_t)v * 16), x);
-        } else {
-#pragma unroll
-            for (int e = 0; e < n; ++e) {
-                const int j = first(v) + e;
-                x[e] = j >= 0 && j < V ? load_elem<DT>(base, (int64_t)v * n + e) : -INFINITY;
-            }
+        if (whole(v)) return *(const u32x4 *)(base + (int64_t)v * 16);
+        u32x4 w = u32x4{1, 1, 1, 1} * (n == 4 ? 0xff800000u : 0xff80ff80u);
+        if (v >= vecs) return w;
+#pragma unroll 1
+        for (int e = n - 1; e >= 0; --e) {                                              // from the last on, which is shifted to its place
+            const int j = first(v) + e;
+            const uint32_t u = __float_as_uint(j >= 0 && j < V ? load_elem<DT>(base, (int64_t)j + before) : -INFINITY);
+            if constexpr (n == 4) w = u32x4{u, w[0], w[1], w[2]};
+            else w = u32x4{__builtin_amdgcn_alignbit(w[0], u, 16), __builtin_amdgcn_alignbit(w[1], w[0], 16), __builtin_amdgcn_alignbit(w[2], w[1], 16),
+                           __builtin_amdgcn_alignbit(w[3], w[2], 16)};
         }
+        return w;
     }
 };
 
-// f(vector, values) for the row's vectors, a turn of kThreads at a time, several turns' loads under way.  Every thread takes part in every turn: behind
-// the row it has values of -infinity.
-template <int DT, class F>
+// f(vector, words) for the row's vectors, a turn of kThreads at a time, LOADS turns' loads under way while as many are worked on: where f stores, a wait
+// for loads that are younger than its stores would wait for these too.  Every thread takes part in every turn: behind the row it has values of
+// -infinity.  A kernel runs through its code once, so code that is not there is what makes it short: the code of f is there LOADS + 1 times, and
+// what is done for a few of a row's elements is a loop.
+template <int DT, int LOADS, class F>
 __device__ __forceinline__ void each_vector(const RowReader<DT> &row, F f)
 {
-    constexpr int n = RowReader<DT>::n;
-    for (int base = 0; base < row.vecs; base += kThreads * kLoads) {
-        if ((base > 0 || row.before == 0) && base + kThreads * kLoads < row.vecs) {
-            u32x4 w[kLoads];
+    constexpr int step = kThreads * LOADS;
+    const int from = row.before ? step : 0;                            // the first vector may be one in part
+    u32x4 w[LOADS], next[LOADS];
+    auto load = [&](int base, u32x4 (&to)[LOADS]) {
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) w[u] = *(const u32x4 *)(row.base + (int64_t)(base + u * kThreads + threadIdx.x) * 16);
+        for (int u = 0; u < LOADS; ++u) to[u] = *(const u32x4 *)(row.base + (int64_t)(base + u * kThreads + threadIdx.x) * 16);
+    };
+    auto whole = [&](int base) { return base >= from && base + step < row.vecs; };
+    if (whole(0)) load(0, w);
+#pragma unroll 1
+    for (int base = 0; base < row.vecs; base += step) {
+        if (whole(base + step)) load(base + step, next);
+        if (whole(base)) {
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                float x[n];
-                unpack<DT>(w[u], x);
-                f(base + u * kThreads + (int)threadIdx.x, x);
-            }
+            for (int u = 0; u < LOADS; ++u) f(base + u * kThreads + (int)threadIdx.x, w[u]);
         } else {
-            for (int u = 0; u < kLoads && base + u * kThreads < row.vecs; ++u) {
-                float x[n];
-                row.load(base + u * kThreads + threadIdx.x, x);
-                f(base + u * kThreads + (int)threadIdx.x, x);
-            }
+#pragma unroll 1
+            for (int t = base; t < min(base + step, row.vecs); t += kThreads) f(t + (int)threadIdx.x, row.load(t + (int)threadIdx.x));
         }
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) w[u] = next[u];
+    }
+}
+// f(value, index) for its elements.
+template <int DT, int LOADS, class F>
+__device__ __forceinline__ void each_element(const RowReader<DT> &row, F f)
+{
+    each_vector<DT, LOADS>(row, [&](int v, const u32x4 &w) {
+        float x[RowReader<DT>::n];
+        unpack<DT>(w, x);
+#pragma unroll
+        for (int e = 0; e < RowReader<DT>::n; ++e) f(x[e], row.first(v) + e);
+    });
+}
+// f(value, index) for the elements of a vector whose bits are set, a lane's one after the other: as many turns as the lane with the most has.  The words
+// are shifted to the element, so that no register is chosen by number.
+template <int DT, class F> __device__ __forceinline__ void each_chosen(u32x4 w, uint32_t bits, int first, F f)
+{
+    const uint64_t front = ((uint64_t)w[1] << 32) | w[0], back = ((uint64_t)w[3] << 32) | w[2];
+#pragma unroll 1
+    while (bits) {
+        const int e = __ffs((int)bits) - 1;
+        bits &= bits - 1;
+        constexpr int half = Elem<DT>::vec / 2, size = Elem<DT>::size * 8;
+        const uint32_t u = (uint32_t)((e < half ? front : back) >> (e % half * size));
+        f(__uint_as_float(size == 32 ? u : u << 16), first + e);
     }
 }
 
-__device__ __forceinline__ uint64_t wave_sum_u(uint64_t v)
+// ---- sums over the workgroup -----------------------------------------------------------------------------------
+template <int CTRL> __device__ __forceinline__ uint64_t dpp_u(uint64_t v)         // lanes without a source: 0
 {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) v += (uint64_t)__shfl_xor((unsigned long long)v, d);
+    return ((uint64_t)(uint32_t)dpp_mov<CTRL>((int)(v >> 32)) << 32) | (uint32_t)dpp_mov<CTRL>((int)(uint32_t)v);
+}
+__device__ __forceinline__ uint64_t lane_u(uint64_t v, int lane)
+{
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+// Sum over the lanes up to this one; *all: over the wavefront.
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v, uint64_t *all)
+{
+    v += dpp_u<0x111>(v); v += dpp_u<0x112>(v); v += dpp_u<0x114>(v); v += dpp_u<0x118>(v);          // within sixteen lanes
+    const uint64_t t0 = lane_u(v, 15), t1 = lane_u(v, 31), t2 = lane_u(v, 47), t3 = lane_u(v, 63);
+    const int group = (threadIdx.x & 63) >> 4;
+    v += group == 0 ? 0 : group == 1 ? t0 : group == 2 ? t0 + t1 : t0 + t1 + t2;
+    *all = t0 + t1 + t2 + t3;
     return v;
 }
-// Sum over the workgroup, in every thread.
-__device__ __forceinline__ uint64_t block_sum(uint64_t v, Shared &sh)
+// Sum over the threads before this one, and over all.  which: 0 and 1 in turn, so that one barrier is enough between two calls.
+__device__ __forceinline__ uint64_t block_before(uint64_t v, uint64_t &all, Shared &sh, int which)
 {
-    v = wave_sum_u(v);
+    uint64_t wave;
+    uint64_t before = wave_scan(v, &wave) - v;
+    if ((threadIdx.x & 63) == 0) sh.waves[which][threadIdx.x >> 6] = wave;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.waves[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0;
-#pragma unroll
-    for (int k = 0; k < kThreads / kWave; ++k) v += sh.waves[k];
-    return v;
-}
-// Sum over the threads before this one, and over all.
-__device__ __forceinline__ uint64_t block_before(uint64_t v, uint64_t &all, Shared &sh)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint64_t s = v;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const uint64_t o = (uint64_t)__shfl_up((unsigned long long)s, d);
-        if (lane >= d) s += o;
-    }
-    __syncthreads();
-    if (lane == 63) sh.waves[wave] = s;
-    __syncthreads();
-    uint64_t before = s - v;
     all = 0;
 #pragma unroll
-    for (int k = 0; k < kThreads / kWave; ++k) {
-        if (k < wave) before += sh.waves[k];
-        all += sh.waves[k];
+    for (int k = 0; k < kWaves; ++k) {
+        const uint64_t q = sh.waves[which][k];
+        if (k < (int)(threadIdx.x >> 6)) before += q;
+        all += q;
     }
     return before;
 }
 
-// The first bin with which the bins' sum from `above` on reaches `target`, and the sum before it; -1 if none does.
-__device__ __forceinline__ int find_bin(uint64_t target, uint64_t &above, Shared &sh)
-{
-    constexpr int per = kBins / kThreads;
-    uint64_t own = 0, all;
-#pragma unroll
-    for (int k = 0; k < per; ++k) own += sh.bins[threadIdx.x * per + k];
-    uint64_t before = above + block_before(own, all, sh);
-    if (threadIdx.x == 0) sh.found = -1;
-    __syncthreads();
-    if (before < target && before + own >= target) {           // one thread
-#pragma unroll
-        for (int k = 0; k < per; ++k) {
-            const uint64_t next = before + sh.bins[threadIdx.x * per + k];
-            if (next >= target) { sh.found = threadIdx.x * per + k; sh.sum = before; break; }
-            before = next;
-        }
-    }
-    __syncthreads();
-    const int b = sh.found;
-    if (b >= 0) above = sh.sum;
-    __syncthreads();
-    return b;
-}
-
-__device__ __forceinline__ void clear_bins(Shared &sh)
-{
-    __syncthreads();
-    for (int k = threadIdx.x; k < kBins; k += kThreads) sh.bins[k] = 0;
-    __syncthreads();
-}
-
-// The last element of the shortest run of `within` whose measure (a count, or units of weight) reaches `target`; `within` itself if none does.
-// first_bin(x): bin from the front for a first division, kBins - 1 for all that lie far behind.  measure(x): of an element.
-template <int DT, class Bin, class Measure>
-__device__ __forceinline__ Bound reach(const RowReader<DT> &row, Bound within, uint64_t target, Bin first_bin, Measure measure, Shared &sh)
+// ---- the end of a run --------------------------------------------------------------------------------------------
+// Index of the r-th element (from 1) that equals x; r of them are there.
+template <int DT>
+__device__ __forceinline__ int nth_equal(const RowReader<DT> &row, float x, uint32_t r, Shared &sh)
 {
     constexpr int n = RowReader<DT>::n;
-    clear_bins(sh);
-    each_vector<DT>(row, [&](int v, const float (&x)[n]) {
+    static_assert(kLoads * kWaves == kWave, "a lane for each wavefront's part of a turn");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t seen = 0;
+    int flip = 0;
+    for (int base = 0; base < row.vecs; base += kThreads * kLoads, flip ^= 1) {
+        uint32_t equal = 0;                                    // a byte for each of the turns
 #pragma unroll
-        for (int e = 0; e < n; ++e) {
-            const uint32_t k = key_of(x[e]);
-            if (k > kMasked && within.holds(k, row.first(v) + e)) atomicAdd((unsigned long long *)&sh.bins[first_bin(x[e])], (unsigned long long)measure(x[e]));
+        for (int u = 0; u < kLoads; ++u) {
+            const int v = base + u * kThreads + (int)threadIdx.x;
+            float y[n];
+            unpack<DT>(row.load(v), y);
+            uint32_t of_wave = 0;
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                equal |= (y[e] == x ? 1u : 0u) << (u * 8 + e);
+                of_wave += (uint32_t)__popcll(__ballot(y[e] == x));
+            }
+            if (lane == 0) sh.turn[flip][u * kWaves + wave] = of_wave;
         }
-    });
+        __syncthreads();
+        uint64_t batch;
+        const uint32_t part = sh.turn[flip][lane], before_part = (uint32_t)wave_scan(part, &batch) - part;
+        if (seen + batch >= r) {
+#pragma unroll 1
+            for (int u = 0; u < kLoads; ++u) {
+                uint64_t all;
+                const uint32_t bits = equal >> (u * 8) & 0xffu, own = (uint32_t)__popc(bits);
+                uint32_t at = seen + (uint32_t)__builtin_amdgcn_readlane((int)before_part, u * kWaves + wave) + (uint32_t)wave_scan(own, &all) - own;
+                if (at < r && at + own >= r)
+#pragma unroll 1
+                    for (int e = 0; e < n; ++e)
+                        if ((bits >> e & 1) && ++at == r) sh.found = row.first(base + u * kThreads + (int)threadIdx.x) + e;
+            }
+            break;
+        }
+        seen += (uint32_t)batch;
+    }
     __syncthreads();
-    uint64_t above = 0;
-    int b = find_bin(target, above, sh);
-    if (b < 0) return within;
+    const int j = uniform(sh.found);
+    __syncthreads();
+    return j;
+}
+
+// The sum of get(p) over this thread's places, and the first place with which the sum over all before it, from `above` on, reaches `target`: in sh.found,
+// with the sum before it in sh.sum, behind the next barrier; untouched if none does.  `before`: the sum over the threads before.
+template <class Get>
+__device__ __forceinline__ uint64_t sum_places(int per, Get get)
+{
+    uint64_t own = 0;
+#pragma unroll 1
+    for (int k = 0; k < per; ++k) own += get(threadIdx.x * per + k);
+    return own;
+}
+template <class Get>
+__device__ __forceinline__ void mark_place(int per, uint64_t target, uint64_t before, uint64_t own, Get get, Shared &sh)
+{
+    if (before >= target || before + own < target) return;
+#pragma unroll 1
+    for (int k = 0; k < per; ++k) {                            // one thread
+        const uint64_t v = get(threadIdx.x * per + k);
+        if (before < target && before + v >= target) { sh.found = threadIdx.x * per + k; sh.sum = before; }
+        before += v;
+    }
+}
+// Both: the place, with the sum before it in `above`; -1 if none does.
+template <class Get>
+__device__ __forceinline__ int find_place(int per, uint64_t target, uint64_t &above, Get get, Shared &sh)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) sh.found = -1;
+    uint64_t all;
+    const uint64_t own = sum_places(per, get), before = above + block_before(own, all, sh, 0);
+    mark_place(per, target, before, own, get, sh);
+    __syncthreads();
+    const int place = uniform(sh.found);
+    if (place >= 0) above = uniform(sh.sum);
+    __syncthreads();
+    return place;
+}
+
+// What a run is measured in: elements, or units of weight.
+struct Measure {
+    bool weights; Weight w;
+    __device__ __forceinline__ uint64_t of(float x, const double *table) const { return weights ? w.of(x, table) : 1; }
+};
+
+// The end of the shortest run of `within` whose measure reaches `target`, which ends in `place`, before which the measure is `above`.
+template <int DT>
+__device__ __forceinline__ Bound end_in(const RowReader<DT> &row, Bound within, uint64_t target, int place, uint64_t above, const Measure &m, Shared &sh)
+{
+    constexpr int n = RowReader<DT>::n;
     uint32_t lo = 0, hi = 0;
     bool by_key = false;
     for (;;) {
-        // the elements of this bin
+        __syncthreads();
         if (threadIdx.x == 0) { sh.count = 0; sh.lo = 0xffffffffu; sh.hi = 0; }
         __syncthreads();
         uint32_t least = 0xffffffffu, most = 0;
-        each_vector<DT>(row, [&](int v, const float (&x)[n]) {
+        each_vector<DT, 4>(row, [&](int v, const u32x4 &w) {
+            float x[n];
+            unpack<DT>(w, x);
+            uint32_t in = 0;
 #pragma unroll
             for (int e = 0; e < n; ++e) {
                 const uint32_t k = key_of(x[e]);
-                const int j = row.first(v) + e;
-                if (k <= kMasked || (by_key ? k < lo || k > hi : first_bin(x[e]) != b) || !within.holds(k, j)) continue;
-                least = min(least, k);
-                most = max(most, k);
-                const int at = atomicAdd(&sh.count, 1);
-                if (at < kList) { sh.list_key[at] = k; sh.list_index[at] = j; }
+                in |= ((by_key ? k >= lo && k <= hi : place_of(x[e]) == place) ? 1u : 0u) << e;
             }
+            if (__any(in != 0))
+                each_chosen<DT>(w, in, row.first(v), [&](float y, int j) {
+                    if (!within.holds(y, j)) return;
+                    const uint32_t k = key_of(y);
+                    least = min(least, k);
+                    most = max(most, k);
+                    const int at = atomicAdd(&sh.count, 1);
+                    if (at < kList) sh.list[at] = ((uint64_t)k << 32) | (0xffffffffu - (uint32_t)j);
+                });
         });
         if (least <= most) { atomicMin(&sh.lo, least); atomicMax(&sh.hi, most); }
         __syncthreads();
-        const int count = sh.count;
-        lo = sh.lo; hi = sh.hi;
-        __syncthreads();
+        const int count = uniform(sh.count);
+        lo = (uint32_t)uniform((int)sh.lo); hi = (uint32_t)uniform((int)sh.hi);
         if (count <= kList) {
-            const int i = threadIdx.x;
-            uint32_t k = 0; int j = 0; uint64_t own = 0, before = above;
-            if (i < count) {
-                k = sh.list_key[i]; j = sh.list_index[i];
-                own = measure(value_of(k));
-                sh.list_w[i] = own;
+#pragma unroll 1
+            for (int i = threadIdx.x; i < count; i += kThreads) sh.list[kList + i] = m.of(value_of((uint32_t)(sh.list[i] >> 32)), sh.table);
+            __syncthreads();
+#pragma unroll 1
+            for (int i = threadIdx.x; i < count; i += kThreads) {
+                const uint64_t me = sh.list[i], own = sh.list[kList + i];
+                uint64_t before = above;
+#pragma unroll 4
+                for (int o = 0; o < count; ++o) before += sh.list[o] > me ? sh.list[kList + o] : 0;
+                if (before < target && before + own >= target) sh.bound = Bound{value_of((uint32_t)(me >> 32)), (int)(0xffffffffu - (uint32_t)me)};      // one thread
             }
             __syncthreads();
-            if (i < count) {
-                for (int o = 0; o < count; ++o) {
-                    const uint32_t ko = sh.list_key[o];
-                    if (ko > k || (ko == k && sh.list_index[o] < j)) before += sh.list_w[o];
-                }
-                if (before < target && before + own >= target) sh.bound = Bound{k, j};          // one thread
-            }
-            __syncthreads();
-            const Bound r = sh.bound;
+            const Bound r = uniform(sh.bound);
             __syncthreads();
             return r;
         }
         if (lo == hi) {
-            // equal elements: the run ends at the r-th of them by index
-            const uint64_t own = measure(value_of(lo)), r = own ? (target - above + own - 1) / own : 1;
-            uint64_t seen = 0;
-            for (int v0 = 0; v0 < row.vecs; v0 += kThreads) {
-                float x[n];
-                row.load(v0 + threadIdx.x, x);
-                uint32_t equal = 0;
-#pragma unroll
-                for (int e = 0; e < n; ++e)
-                    if (key_of(x[e]) == lo && within.holds(lo, row.first(v0 + threadIdx.x) + e)) equal |= 1u << e;
-                uint64_t all;
-                uint64_t before = seen + block_before(__popc(equal), all, sh);
-                if (before < r && before + __popc(equal) >= r) {
-#pragma unroll
-                    for (int e = 0; e < n; ++e)
-                        if (equal >> e & 1 && ++before == r) sh.bound = Bound{lo, row.first(v0 + threadIdx.x) + e};
-                }
-                seen += all;
-                if (seen >= r) break;
-            }
-            __syncthreads();
-            const Bound q = sh.bound;
-            __syncthreads();
-            return q;
+            const float x = value_of(lo);
+            const uint64_t own = m.of(x, sh.table);                         // not 0: the target is reached here
+            return shorter(Bound{x, nth_equal<DT>(row, x, (uint32_t)((target - above + own - 1) / own), sh)}, within);       // `within` may end among the same elements
         }
-        // too many: by keys
-        const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);           // (hi - lo) >> shift is below kBins
-        clear_bins(sh);
-        each_vector<DT>(row, [&](int v, const float (&x)[n]) {
-#pragma unroll
-            for (int e = 0; e < n; ++e) {
-                const uint32_t k = key_of(x[e]);
-                if (k >= lo && k <= hi && within.holds(k, row.first(v) + e)) atomicAdd((unsigned long long *)&sh.bins[(hi - k) >> shift], (unsigned long long)measure(x[e]));
-            }
-        });
+        // too many: a 2048th of their keys' range each
+        const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
         __syncthreads();
-        b = find_bin(target, above, sh);
-        if (b < 0) return within;                                            // not reached: the bin holds what was missing
+#pragma unroll 1
+        for (int k = threadIdx.x; k < kBins; k += kThreads) sh.bins[k] = 0;
+        __syncthreads();
+        each_element<DT, 1>(row, [&](float x, int j) {
+            const uint32_t k = key_of(x);
+            if (k >= lo && k <= hi && within.holds(x, j)) atomicAdd((unsigned long long *)&sh.bins[(hi - k) >> shift], (unsigned long long)m.of(x, sh.table));
+        });
+        const int b = find_place(kBins / kThreads, target, above, [&](int k) { return sh.bins[k]; }, sh);
         by_key = true;
         const uint32_t top = hi - ((uint32_t)b << shift);
         lo = max(lo, top - min(top, (1u << shift) - 1));
         hi = top;
     }
+}
+
+// The smallest value whose weight is at least min_p, found a 64th of the interval of keys at a time.
+__device__ __forceinline__ float least_value(float max, float T, float min_p)
+{
+    const int lane = threadIdx.x & 63;
+    const double least = log((double)fminf(min_p, 1.f)), inv = 1.0 / (double)T;
+    uint32_t lo = key_of(-INFINITY), hi = key_of(max);                                     // lo: not enough (or masked), hi: enough
+    while (hi - lo > 1) {
+        const uint32_t step = (hi - lo + 63) / 64, at = lo + min((uint32_t)(lane + 1) * step, hi - lo);
+        const int first = __ffsll((unsigned long long)__ballot(((double)value_of(at) - (double)max) * inv >= least)) - 1;       // the last lane's is hi
+        hi = lo + min((uint32_t)(first + 1) * step, hi - lo);
+        lo += (uint32_t)first * step;
+    }
+    return value_of(hi);
 }
 
 // A vector of results at any element-aligned address.
@@ -318,191 +437,515 @@ template <class E, int N> __device__ __forceinline__ void store_any(E *to, const
     }
 }
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void filtered_sample_kernel(FilterArgs a)
+// What a row asks for.
+struct Filters {
+    float T, top_p, min_p; int top_k; bool greedy;
+};
+
+// Counts of a bfloat16 row's values.  sh.bad: a NaN or +infinity; sh.irregular: values beyond the table, or too many that are smaller than it.
+__device__ __forceinline__ void count_values(const RowReader<TAPOUT_BF16> &row, Shared &sh)
 {
-    constexpr int n = RowReader<DT>::n;
+#pragma unroll 1
+    for (int k = threadIdx.x; k < kEntries; k += kThreads) sh.counts[k] = 0;
+    __syncthreads();
+    each_vector<TAPOUT_BF16, 4>(row, [&](int, const u32x4 &w) {
+        u16x2 d[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            d[q] = entries_of(w[q]);
+            atomicAdd(&sh.counts[d[q][0]], 1u);
+            atomicAdd(&sh.counts[d[q][1]], 1u);
+        }
+        const u16x2 top = __builtin_elementwise_max(__builtin_elementwise_max(d[0], d[1]), __builtin_elementwise_max(d[2], d[3]));
+        const u16x2 low = __builtin_elementwise_min(__builtin_elementwise_min(d[0], d[1]), __builtin_elementwise_min(d[2], d[3]));
+        if (max(top[0], top[1]) >= kEntries - 2 || min(low[0], low[1]) < 2) {
+            // what there is beside masked elements and zeros, two at a time: magnitudes less the infinity's bits wrap round below it
+            u16x2 large = {0, 0}, nan = {0xffff, 0xffff}, inf = nan, small = nan;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const u16x2 m = __builtin_bit_cast(u16x2, w[q] & 0x7fff7fffu), over = m - (u16x2)(unsigned short)0x7f80;
+                large = __builtin_elementwise_max(large, over);
+                nan = __builtin_elementwise_min(nan, over - (u16x2)(unsigned short)1);
+                inf = __builtin_elementwise_min(inf, __builtin_bit_cast(u16x2, w[q] ^ 0x7f807f80u));
+                small = __builtin_elementwise_min(small, m - (u16x2)(unsigned short)1);
+            }
+            if (max(large[0], large[1]) >= (unsigned short)(kLow + kRegular - 0x7f80)) sh.irregular = 1;
+            if (min(nan[0], nan[1]) < 0x7f || min(inf[0], inf[1]) == 0) sh.bad = 1;
+            if (min(small[0], small[1]) < kLow - 1)
+                each_chosen<TAPOUT_BF16>(w, 0xffu, 0, [&](float x, int) {
+                    if (x == 0.f || !(fabsf(x) < 0x1p-16f)) return;
+                    const int at = atomicAdd(&sh.tinies, 1);
+                    if (at < 64) sh.tiny[at] = x;
+                    else sh.irregular = 1;
+                });
+        }
+    });
+    __syncthreads();
+    if (threadIdx.x == 0) { sh.counts[0] += sh.counts[1]; sh.counts[1] = 0; sh.counts[kEntries - 1] = 0; }         // one place; the last are masked
+    __syncthreads();
+}
+
+// A bfloat16 row from its counts: its maximum, where its run ends and how many that keeps.  false: it was not decided here (not regular, without a
+// finite value (sh.bad), or its run ends among the small values).
+__device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, const Filters &f, int shift, float &peak, Weight &w, Bound &end, int &kept, Shared &sh)
+{
+    count_values(row, sh);
+    if (uniform(sh.bad | sh.irregular)) return false;
+    const int tinies = uniform(sh.tinies);
+    const int p0 = threadIdx.x * kPer;
+    uint32_t c[kPer];
+    uint64_t all, own = 0, before, units[kPer];
+    int first = kPlaces;
+#pragma unroll
+    for (int k = kPer - 1; k >= 0; --k) {
+        c[k] = p0 + k < kPlaces ? sh.counts[entry_at(p0 + k)] : 0;
+        own += c[k];
+        if (c[k]) first = p0 + k;
+    }
+    // the first place with an element, and the place of the k-th
+    if (threadIdx.x == 0) { sh.found = kPlaces; sh.count = 0; sh.lo = kPlaces; }
+    before = block_before(own, all, sh, 0);
+    if (uniform((int)(all >> 32) | (int)all) == 0) {
+        if (threadIdx.x == 0) sh.bad = 1;
+        __syncthreads();
+        return false;
+    }
+    kept = uniform((int)all);
+    const uint64_t counted = before, top_k = f.greedy ? 1 : f.top_k > 0 ? f.top_k : 1ull << 40;
+    if (own && before == 0) sh.hi = first;                                                 // one thread
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        if (before < top_k && before + c[k] >= top_k) { sh.found = p0 + k; sh.count = (int)(top_k - before); }
+        before += c[k];
+    }
+    __syncthreads();
+    int place = uniform(sh.found), n = uniform(sh.count);      // the run: all places before `place`, n elements of it
+    first = uniform((int)sh.hi);
+    if (first == kTinyPlace && tinies) return false;
+    peak = value_at(first);
+    w = Weight{(double)peak, f.greedy ? 0.0 : 256.0 / ((double)f.T * kLn2), shift};
+    // weights by value, masses of what top-k leaves, the first place whose elements are too light; small values one by one
+    const double least = !f.greedy && f.min_p > 0.f ? log((double)fminf(f.min_p, 1.f)) * (double)f.T : -INFINITY;          // of x - peak
+    bool light = false;
+    uint64_t mass[kPer];
+    own = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int p = p0 + k;
+        mass[k] = units[k] = 0;
+        if (!c[k]) continue;
+        const float x = value_at(p);
+        units[k] = w.of(x, sh.table);
+        mass[k] = (uint64_t)(p < place ? c[k] : p == place ? (uint32_t)n : 0u) * units[k];
+        if (!light && (double)x - (double)peak < least) {
+            atomicMin(&sh.lo, (uint32_t)p);
+            light = true;
+        }
+        if (p == kTinyPlace && tinies) {
+            if ((-0x1p-16 - (double)peak < least) != (0x1p-16 - (double)peak < least)) sh.irregular = 1;         // the border among the small values
+            if (p < place) {
+                mass[k] -= tinies * units[k];
+#pragma unroll 1
+                for (int q = 0; q < tinies; ++q) mass[k] += w.of(sh.tiny[q], sh.table);
+            }
+        }
+        own += mass[k];
+    }
+    if (!f.greedy && f.top_p < 1.f) {
+        before = block_before(own, all, sh, 1);
+        const double reached = (double)f.top_p * (double)all;
+        const uint64_t target = reached > 1.0 ? (uint64_t)ceil(reached) : 1;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            if (before < target && before + mass[k] >= target) {                           // one thread
+                const uint64_t one = units[k] ? units[k] : 1, need = (target - before + one - 1) / one;
+                const uint32_t most = p0 + k == place ? (uint32_t)n : c[k];
+                sh.found = p0 + k;
+                sh.count = need < most ? (int)need : (int)most;
+            }
+            before += mass[k];
+        }
+        __syncthreads();
+        place = uniform(sh.found);
+        n = uniform(sh.count);
+    } else {
+        __syncthreads();
+    }
+    if (uniform(sh.irregular)) return false;
+    if (const int lo = uniform((int)sh.lo); place >= lo) { place = lo; n = 0; }
+    if (place == kTinyPlace && n && tinies) return false;
+    if (place == kPlaces) {
+        end = Bound{-INFINITY, kNone};
+        return true;
+    }
+    // how many that keeps
+    if (place >= p0 && place < p0 + kPer) {                                                // one thread
+        uint64_t ahead = counted;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) ahead += p0 + k < place ? c[k] : 0;
+        sh.sum = ahead;
+    }
+    __syncthreads();
+    kept = uniform((int)sh.sum) + n;
+    const uint32_t here = (uint32_t)uniform((int)sh.counts[entry_at(place)]);
+    if (n == 0) end = Bound{place == kTinyPlace ? __uint_as_float((kLow - 1) << 16) : value_at(place), kNone};
+    else if ((uint32_t)n >= here) end = Bound{value_at(place), kAll};
+    else end = Bound{value_at(place), nth_equal<TAPOUT_BF16>(row, value_at(place), (uint32_t)n, sh)};
+    return true;
+}
+
+// Any row.
+template <int DT>
+__device__ __forceinline__ void by_places(const RowReader<DT> &row, const Filters &f, int shift, float &peak, Weight &w, Bound &end, Shared &sh)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) sh.bad = 0;
+    float m = -INFINITY;
+    bool nan = false;
+    each_element<DT, 4>(row, [&](float x, int) {
+        m = fmaxf(m, x);
+        nan |= x != x;
+    });
+    m = lanes_max(m, 0, 6);
+    if ((threadIdx.x & 63) == 0) sh.waves_f[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (nan) sh.bad = 1;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) m = fmaxf(m, sh.waves_f[k]);
+    __syncthreads();
+    peak = m;
+    end = Bound{-INFINITY, kNone};
+    m = uniform(m);
+    const bool bad = uniform(sh.bad) || !(fabsf(m) < INFINITY);
+    __syncthreads();
+    if (bad) {
+        if (threadIdx.x == 0) sh.bad = 1;
+        __syncthreads();
+        return;
+    }
+    w = Weight{(double)m, f.greedy ? 0.0 : 256.0 / ((double)f.T * kLn2), shift};
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {                     // top-k (greedy: the first one), then top-p of what that leaves
+        if (turn == 0 ? !f.greedy && (f.top_k <= 0 || f.top_k >= row.V) : f.greedy || !(f.top_p < 1.f)) continue;
+        const Measure measure{turn == 1, w};
+        const Bound within = end;
+        __syncthreads();
+#pragma unroll 1
+        for (int k = threadIdx.x; k < kEntries; k += kThreads) sh.units[k] = 0;
+        __syncthreads();
+        each_element<DT, 1>(row, [&](float x, int j) {
+            if (within.holds(x, j)) atomicAdd((unsigned long long *)&sh.units[entry_of(x)], (unsigned long long)measure.of(x, sh.table));
+        });
+        __syncthreads();
+        if (threadIdx.x == 0) { sh.units[0] += sh.units[1]; sh.units[1] = 0; }
+        __syncthreads();
+        auto at = [&](int p) { return p < kPlaces ? sh.units[entry_at(p)] : 0; };
+        uint64_t target = f.greedy ? 1 : f.top_k, all, above = 0;
+        if (turn == 1) {
+            (void)block_before(sum_places(kPer, at), all, sh, 1);
+            const double reached = (double)f.top_p * (double)all;
+            target = reached > 1.0 ? (uint64_t)ceil(reached) : 1;
+        }
+        const int place = find_place(kPer, target, above, at, sh);
+        if (place >= 0) end = end_in<DT>(row, within, target, place, above, measure, sh);
+    }
+    if (!f.greedy && f.min_p > 0.f) end = shorter(end, Bound{least_value(m, f.T, f.min_p), kAll});
+}
+
+// What by_places decides about a bfloat16 row, out of the way of those that are decided by their counts.
+struct Decision { float peak; Weight w; Bound end; };
+__device__ __attribute__((noinline)) Decision any_bf16_row(const void *p, int V, Filters f, int shift, Shared *sh)
+{
+    Decision d{0.f, {0.0, 0.0, shift}, {INFINITY, kNone}};
+    by_places<TAPOUT_BF16>(RowReader<TAPOUT_BF16>(p, V), f, shift, d.peak, d.w, d.end, *sh);
+    return d;
+}
+
+// ---- kernels -----------------------------------------------------------------------------------------------------
+}  // namespace
+
+// What every row keeps.  Elements are kept that are larger than one of two values: up to the index `last` than `from`, behind it than `above`, which
+// differ where equal elements are kept in part.
+struct FilterRow {
+    float max, inv, above, from;
+    int32_t last, kept;                        // kept: -1 where it was not counted
+    int32_t bad, pad;
+    double c;                                  // see Weight
+};
+static_assert(sizeof(FilterRow) == kFilterRowBytes, "the context makes room for it");
+
+namespace {
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a)
+{
     __shared__ Shared sh;
     const int r = blockIdx.x, b = r / a.K, k = r - b * a.K;
     if (a.k_len && k >= a.k_len[b]) return;
     const RowReader<DT> row(row_address(a.base, DT, a.stride_b, a.stride_k, b, k), a.V);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float T = a.temperature ? a.temperature[b] : 1.f, top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
-    const int top_k = a.top_k ? a.top_k[b] : 0;
+    Filters f{a.temperature ? a.temperature[b] : 1.f, a.top_p ? a.top_p[b] : 1.f, a.min_p ? a.min_p[b] : 0.f, a.top_k ? a.top_k[b] : 0, false};
+    f.greedy = !(f.T > 0.f);
     if (threadIdx.x < 256) sh.table[threadIdx.x] = a.exp_table[threadIdx.x];
-    if (threadIdx.x == 0) sh.nan = 0;
-    // the maximum
-    float m = -INFINITY;
-    bool nan = false;
-    each_vector<DT>(row, [&](int, const float (&x)[n]) {
-#pragma unroll
-        for (int e = 0; e < n; ++e) { m = fmaxf(m, x[e]); nan |= x[e] != x[e]; }
-    });
-    m = lanes_max(m, 0, 6);
-    if (lane == 0) sh.waves_f[wave] = m;
+    if (threadIdx.x == 0) { sh.bad = f.T != f.T; sh.irregular = 0; sh.tinies = 0; sh.found = 0; }
     __syncthreads();
-    if (nan) sh.nan = 1;
-    m = sh.waves_f[0];
-#pragma unroll
-    for (int w = 1; w < kThreads / kWave; ++w) m = fmaxf(m, sh.waves_f[w]);
-    __syncthreads();
-    const bool bad = sh.nan || !(fabsf(m) < INFINITY) || T != T, greedy = !(T > 0.f);
-    if (a.flags && threadIdx.x == 0) {
-        if (a.K == 1) a.flags[b] = bad ? TAPOUT_FLAG_BAD_ROW : 0u;
-        else if (bad) atomicOr(&a.flags[b], TAPOUT_FLAG_BAD_ROW);
-    }
-    // what the row keeps; a bad row nothing
-    Bound end{kMasked, -1};                                    // -1: no element of this key
-    Weight w{(double)m, greedy || bad ? 0.0 : 256.0 / ((double)T * kLn2), a.shift};
-    if (bad) end = Bound{0xffffffffu, -1};
-    else {
-        if (greedy || (top_k > 0 && top_k < a.V)) {
-            const float mf = m;
-            end = reach<DT>(row, end, greedy ? 1 : top_k, [=](float x) { return (int)fminf((mf - x) * kTopKBins, (float)(kBins - 1)); }, [](float) { return (uint64_t)1; }, sh);
-        }
-        if (!greedy && top_p < 1.f) {
-            uint64_t mine = 0;
-            const Bound within = end;
-            each_vector<DT>(row, [&](int v, const float (&x)[n]) {
-#pragma unroll
-                for (int e = 0; e < n; ++e) {
-                    const uint32_t key = key_of(x[e]);
-                    if (key > kMasked && within.holds(key, row.first(v) + e)) mine += w.of(x[e], sh.table);
-                }
-            });
-            const uint64_t Z = block_sum(mine, sh);
-            const double reached = (double)top_p * (double)Z;
-            const uint64_t target = reached > 1.0 ? (uint64_t)ceil(reached) : 1;
-            end = reach<DT>(row, within, target, [=](float x) { return min(kBins - 1, (int)(-w.steps(x)) >> 3); }, [&](float x) { return w.of(x, sh.table); }, sh);
-        }
-        if (!greedy && min_p > 0.f) {
-            // the smallest key whose weight is large enough: a 64th of the interval at a time
-            const double least = log((double)fminf(min_p, 1.f)), inv = 1.0 / (double)T;
-            uint32_t lo = kMasked, hi = key_of(m);                                         // lo: not enough, hi: enough
-            while (hi - lo > 1) {
-                const uint32_t step = (hi - lo + 63) / 64, at = lo + min((uint32_t)(lane + 1) * step, hi - lo);
-                const uint64_t enough = __ballot(((double)value_of(at) - (double)m) * inv >= least);
-                const int first = __ffsll((unsigned long long)enough) - 1;                   // the last lane's is hi
-                hi = lo + min((uint32_t)(first + 1) * step, hi - lo);
-                lo = first ? lo + (uint32_t)first * step : lo;
+    float max = 0.f;
+    Weight w{0.0, 0.0, a.shift};
+    Bound end{INFINITY, kNone};
+    int kept = -1;
+    if (f.T == f.T) {
+        bool done = false;
+        if constexpr (DT == TAPOUT_BF16) done = by_counts(row, f, a.shift, max, w, end, kept, sh);
+        if (!done && !uniform(sh.bad)) {
+            kept = -1;
+            if constexpr (DT == TAPOUT_BF16) {
+                const Decision d = any_bf16_row(row.base + row.before * Elem<DT>::size, a.V, f, a.shift, &sh);
+                max = d.peak; w = d.w; end = d.end;
+            } else {
+                by_places<DT>(row, f, a.shift, max, w, end, sh);
             }
-            end = shorter(end, Bound{hi, 0x7fffffff});
         }
     }
-    // what is kept, and its weights by chunks of the row
+    __syncthreads();
+    if (threadIdx.x) return;
+    const bool bad = sh.bad;
+    FilterRow q{max, f.greedy ? 0.f : fminf(1.f / f.T, 3.402823466e38f), end.x, end.x, kNone, kept, bad, 0, w.c};      // inv is finite: 0 times it stays 0
+    if (bad) q = FilterRow{0.f, 0.f, INFINITY, INFINITY, kNone, 0, 1, 0, 0.0};
+    else if (end.index == kAll) q.above = q.from = below(end.x);
+    else if (end.index != kNone) { q.from = below(end.x); q.last = end.index; }
+    a.rows[r] = q;
+}
+
+// The vectors of a slice, and which of their elements are kept.
+constexpr int kSliceThreads = 256, kSliceTurns = 4, kSliceVecs = kSliceThreads * kSliceTurns;
+template <int N> __device__ __forceinline__ void kept_of(const FilterRow &q, const float (&x)[N], int j0, bool (&in)[N])
+{
+    const float than = j0 + N - 1 <= q.last ? q.from : q.above;
+#pragma unroll
+    for (int e = 0; e < N; ++e) in[e] = x[e] > than;
+    if (j0 <= q.last && q.last < j0 + N - 1) {                 // one vector of the row
+#pragma unroll
+        for (int e = 0; e < N; ++e) in[e] = x[e] > (j0 + e <= q.last ? q.from : q.above);
+    }
+}
+__device__ __forceinline__ FilterRow row_record(const FilterArgs &a, int r)
+{
+    FilterRow q = a.rows[r];
+    q.max = uniform(q.max); q.inv = uniform(q.inv); q.above = uniform(q.above); q.from = uniform(q.from);
+    q.last = uniform(q.last); q.kept = uniform(q.kept); q.bad = uniform(q.bad); q.c = uniform(q.c);
+    return q;
+}
+// Units of a vector's kept elements: all of its elements in turn where most lanes keep some, else those that are kept.
+template <int DT> __device__ __forceinline__ uint64_t kept_units(const Weight &w, const u32x4 &words, uint32_t keeps, int j0, const double *table)
+{
+    uint64_t sum = 0;
+    const int lanes = __popcll(__ballot(keeps != 0));
+    if (lanes > 40) {
+        float x[Elem<DT>::vec];
+        unpack<DT>(words, x);
+#pragma unroll
+        for (int e = 0; e < Elem<DT>::vec; ++e) {
+            const uint64_t one = w.of(x[e], table);
+            sum += keeps >> e & 1 ? one : 0;
+        }
+    } else if (lanes) {
+        each_chosen<DT>(words, keeps, j0, [&](float x, int) { sum += w.of(x, table); });
+    }
+    return sum;
+}
+
+// The filtered logits, and a slice's kept elements and weights: a workgroup a slice, all of its loads requested first.
+template <int DT>
+__global__ __launch_bounds__(kSliceThreads) void filter_slices_kernel(FilterArgs a, int slices)
+{
+    constexpr int n = RowReader<DT>::n;
+    __shared__ double table[256];
+    __shared__ uint64_t sums[kSliceThreads / kWave];
+    __shared__ int counts[kSliceThreads / kWave];
+    const int r = blockIdx.x / slices, s = blockIdx.x - r * slices, b = r / a.K, k = r - b * a.K;
+    if (a.k_len && k >= a.k_len[b]) return;
+    const RowReader<DT> row(row_address(a.base, DT, a.stride_b, a.stride_k, b, k), a.V);
+    const int v0 = s * kSliceVecs;
+    if (v0 >= row.vecs) {                                      // a row without a part of a vector before it may have no vector here
+        if (threadIdx.x == 0) a.slices[blockIdx.x] = FilterSlice{0, 0, 0};
+        return;
+    }
     const bool draw = a.u != nullptr;
-    const int turn = kThreads, turns = (row.vecs + turn - 1) / turn, per = (turns + kBins - 1) / kBins;      // vectors of a turn; turns of a chunk
-    const double inv = greedy || bad ? 0.0 : 1.0 / (double)T;
-    clear_bins(sh);
-    int kept = 0;
-    char *out = a.kept ? (char *)row_address(a.kept, a.kept_dtype, a.kept_stride_b, a.kept_stride_k, b, k) : nullptr;
-    each_vector<DT>(row, [&](int v, const float (&x)[n]) {
-        float y[n];
-        uint64_t mine = 0;
-        const int j0 = row.first(v);
+    if (draw) table[threadIdx.x] = a.exp_table[threadIdx.x];
+    u32x4 words[kSliceTurns];
+    if ((v0 > 0 || row.before == 0) && v0 + kSliceVecs < row.vecs) {
 #pragma unroll
-        for (int e = 0; e < n; ++e) {
-            const uint32_t key = key_of(x[e]);
-            y[e] = -INFINITY;
-            if (key > kMasked && end.holds(key, j0 + e)) {
-                ++kept;
-                y[e] = (float)(((double)x[e] - (double)m) * inv);
-                if (draw) mine += w.of(x[e], sh.table);
-            }
-        }
-        if (draw && __any(mine != 0)) {
-            mine = wave_sum_u(mine);
-            if (lane == 0) atomicAdd((unsigned long long *)&sh.bins[v / turn / per], (unsigned long long)mine);
-        }
-        if (!out) return;
-        if (row.whole(v)) {
-            if (a.kept_dtype == TAPOUT_F32) store_any<float, n>((float *)out + j0, y);
-            else store_any<__bf16, n>((__bf16 *)out + j0, y);
-        } else {
+        for (int t = 0; t < kSliceTurns; ++t) words[t] = *(const u32x4 *)(row.base + (int64_t)(v0 + t * kSliceThreads + threadIdx.x) * 16);
+    } else {
 #pragma unroll
-            for (int e = 0; e < n; ++e) {
-                if (j0 + e < 0 || j0 + e >= a.V) continue;
-                if (a.kept_dtype == TAPOUT_F32) ((float *)out)[j0 + e] = y[e];
-                else ((__bf16 *)out)[j0 + e] = (__bf16)y[e];
-            }
-        }
-    });
-    if (a.n_kept) {
-        const uint64_t all = block_sum((uint64_t)kept, sh);
-        if (threadIdx.x == 0) a.n_kept[r] = (int32_t)all;
+        for (int t = 0; t < kSliceTurns; ++t) words[t] = row.load(v0 + t * kSliceThreads + (int)threadIdx.x);
     }
-    if (!draw) return;
-    if (bad) {
+    const FilterRow q = row_record(a, r);
+    const Weight w{(double)q.max, q.c, a.shift};
+    char *out = a.kept ? (char *)row_address(a.kept, a.kept_dtype, a.kept_stride_b, a.kept_stride_k, b, k) : nullptr;
+    uint64_t mine = 0;
+    int count = 0;
+    if (draw) __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kSliceTurns; ++t) {
+        const int v = v0 + t * kSliceThreads + (int)threadIdx.x, j0 = row.first(v);
+        float x[n], y[n];
+        bool in[n];
+        unpack<DT>(words[t], x);
+        kept_of(q, x, j0, in);
+        uint32_t keeps = 0;
+#pragma unroll
+        for (int e = 0; e < n; ++e) keeps |= (in[e] ? 1u : 0u) << e;
+        count += __popc(keeps);
+        if (draw) mine += kept_units<DT>(w, words[t], keeps, j0, table);
+        if (!out) continue;
+#pragma unroll
+        for (int e = 0; e < n; ++e) y[e] = in[e] ? (x[e] - q.max) * q.inv : -INFINITY;
+        if (!row.whole(v)) continue;
+        if (a.kept_dtype == TAPOUT_F32) store_any<float, n>((float *)out + j0, y);
+        else store_any<__bf16, n>((__bf16 *)out + j0, y);
+    }
+    if (out)
+#pragma unroll 1
+        for (int e = 0; e < 2; ++e) {                          // the row's first and last vector, where they are vectors in part
+            const int v = e ? row.vecs - 1 : 0;
+            if (row.whole(v) || (v - v0) % kSliceThreads != (int)threadIdx.x || v < v0 || v >= v0 + kSliceVecs || (e && v == 0)) continue;
+            each_chosen<DT>(row.load(v), (1u << n) - 1, row.first(v), [&](float x, int j) {
+                if (j < 0 || j >= a.V) return;
+                const float z = x > (j <= q.last ? q.from : q.above) ? (x - q.max) * q.inv : -INFINITY;
+                if (a.kept_dtype == TAPOUT_F32) ((float *)out)[j] = z;
+                else ((__bf16 *)out)[j] = (__bf16)z;
+            });
+        }
+    uint64_t all;
+    (void)wave_scan(mine, &all);
+    for (int d = 32; d; d >>= 1) count += __shfl_xor(count, d);
+    if ((threadIdx.x & 63) == 0) { sums[threadIdx.x >> 6] = all; counts[threadIdx.x >> 6] = count; }
+    __syncthreads();
+    if (threadIdx.x == 0) a.slices[blockIdx.x] = FilterSlice{sums[0] + sums[1] + sums[2] + sums[3], counts[0] + counts[1] + counts[2] + counts[3], 0};
+}
+
+// How many a row keeps, the flags of its sequence, and its token: the slice that holds it, then the vector, then the element.  A workgroup a row.
+template <int DT>
+__global__ __launch_bounds__(kSliceThreads) void filter_tokens_kernel(FilterArgs a, int slices)
+{
+    constexpr int n = RowReader<DT>::n, kW = kSliceThreads / kWave;
+    __shared__ double table[256];
+    __shared__ uint64_t sums[kW], parts[kSliceTurns * kW];
+    __shared__ int counts[kW], slice, found;
+    __shared__ uint64_t ahead;
+    const int r = blockIdx.x, b = r / a.K, k = r - b * a.K, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int live = a.k_len ? min(a.k_len[b], a.K) : a.K;
+    if (a.flags && k == 0 && threadIdx.x < kWave) {
+        bool bad = false;
+        for (int o = lane; o < live; o += kWave) bad |= a.rows[r + o].bad != 0;
+        const bool any = __any(bad);
+        if (lane == 0) a.flags[b] = any ? TAPOUT_FLAG_BAD_ROW : 0u;
+    }
+    if (k >= live) return;
+    const FilterRow q = row_record(a, r);
+    const FilterSlice *p = a.slices + (int64_t)r * slices;
+    table[threadIdx.x] = a.exp_table[threadIdx.x];
+    const float u = a.u ? a.u[r] : 0.f;
+    // every thread a run of slices
+    const int per = (slices + kSliceThreads - 1) / kSliceThreads, s0 = threadIdx.x * per, s1 = min(s0 + per, slices);
+    uint64_t own = 0, all;
+    int count = 0;
+    for (int s = s0; s < s1; ++s) { own += p[s].units; count += p[s].kept; }
+    uint64_t before = wave_scan(own, &all) - own;
+    for (int d = 32; d; d >>= 1) count += __shfl_xor(count, d);
+    if (lane == 0) { sums[wave] = all; counts[wave] = count; }
+    if (threadIdx.x == 0) { slice = 0; ahead = 0; found = 0x7fffffff; }
+    __syncthreads();
+    if (a.n_kept && threadIdx.x == 0) a.n_kept[r] = counts[0] + counts[1] + counts[2] + counts[3];
+    if (!a.u) return;
+    if (q.bad) {
         if (threadIdx.x == 0) {
             a.token[r] = -1;
             if (a.logq) a.logq[r] = __uint_as_float(0x7fc00000u);
         }
         return;
     }
-    // the token: its chunk, its turn, its thread
-    __syncthreads();
-    uint64_t own = 0, Z;
+    uint64_t Z = 0;
 #pragma unroll
-    for (int q = 0; q < kBins / kThreads; ++q) own += sh.bins[threadIdx.x * (kBins / kThreads) + q];
-    (void)block_before(own, Z, sh);
-    const float u = a.u[r];
+    for (int g = 0; g < kW; ++g) { if (g < wave) before += sums[g]; Z += sums[g]; }
     const double point = (double)u * (double)Z;
-    uint64_t target = point >= 0.0 ? (uint64_t)point + 1 : 1;         // the sum has to reach this: whole numbers above u Z
+    uint64_t target = point >= 0.0 ? (uint64_t)point + 1 : 1;                          // whole numbers above u Z reach this
     if (!(u < 1.f) || target > Z) target = Z;
-    uint64_t before = 0;
-    const int chunk = find_bin(target, before, sh);
-    if (threadIdx.x == 0) { sh.found = 0x7fffffff; sh.sum = 0; }
+    if (before < target && before + own >= target)                                     // one thread
+        for (int s = s0; s < s1; ++s) {
+            if (before < target && before + p[s].units >= target) { slice = s; ahead = before; }
+            before += p[s].units;
+        }
     __syncthreads();
+    const RowReader<DT> row(row_address(a.base, DT, a.stride_b, a.stride_k, b, k), a.V);
+    const Weight w{(double)q.max, q.c, a.shift};
     if (u == 0.f) {
-        // the first kept element of any weight at all, units or not
-        const double least = -745.13;
+        // the first kept element that has a weight at all, in units or not
         int first = 0x7fffffff;
-        each_vector<DT>(row, [&](int v, const float (&x)[n]) {
-#pragma unroll
-            for (int e = 0; e < n; ++e) {
-                const uint32_t key = key_of(x[e]);
-                if (key > kMasked && end.holds(key, row.first(v) + e) && ((double)x[e] - (double)m) * inv > least) first = min(first, row.first(v) + e);
-            }
-        });
-        atomicMin(&sh.found, first);
-    } else {
-        for (int t = chunk * per; t < min((chunk + 1) * per, turns); ++t) {
-            const int v = t * turn + threadIdx.x;
+#pragma unroll 1
+        for (int v = threadIdx.x; v < row.vecs; v += kSliceThreads) {
+            const u32x4 words = row.load(v);
             float x[n];
-            row.load(v, x);
-            uint64_t mine = 0, all;
-            uint64_t units[n];
+            unpack<DT>(words, x);
 #pragma unroll
-            for (int e = 0; e < n; ++e) {
-                const uint32_t key = key_of(x[e]);
-                units[e] = key > kMasked && end.holds(key, row.first(v) + e) ? w.of(x[e], sh.table) : 0;
-                mine += units[e];
+            for (int e = n - 1; e >= 0; --e) {
+                const int j = row.first(v) + e;
+                if (x[e] > (j <= q.last ? q.from : q.above) && (double)(x[e] - q.max) * (double)q.inv > -745.13) first = min(first, j);
             }
-            uint64_t sum = before + block_before(mine, all, sh);
-            if (sum < target && sum + mine >= target) {
+            if (first < 0x7fffffff) break;
+        }
+        atomicMin(&found, first);
+    } else {
+        const int v0 = uniform(slice) * kSliceVecs;
+        u32x4 words[kSliceTurns];
+        auto keeps_of = [&](const u32x4 &w4, int v) {
+            float x[n];
+            bool in[n];
+            unpack<DT>(w4, x);
+            kept_of(q, x, row.first(v), in);
+            uint32_t keeps = 0;
 #pragma unroll
-                for (int e = 0; e < n; ++e) {
-                    if (sum < target && sum + units[e] >= target) sh.found = row.first(v) + e;
-                    sum += units[e];
-                }
-            }
-            before += all;
-            if (before >= target) break;
+            for (int e = 0; e < n; ++e) keeps |= (in[e] ? 1u : 0u) << e;
+            return keeps;
+        };
+#pragma unroll
+        for (int t = 0; t < kSliceTurns; ++t) words[t] = row.load(v0 + t * kSliceThreads + (int)threadIdx.x);
+#pragma unroll
+        for (int t = 0; t < kSliceTurns; ++t) {
+            uint64_t of_wave;
+            const int v = v0 + t * kSliceThreads + (int)threadIdx.x;
+            (void)wave_scan(kept_units<DT>(w, words[t], keeps_of(words[t], v), row.first(v), table), &of_wave);
+            if (lane == 0) parts[t * kW + wave] = of_wave;
+        }
+        __syncthreads();
+        // the part that holds it, once more: every wavefront does, and the one whose part it is finds it
+        static_assert(kSliceTurns * kW <= kWave, "a lane a part");
+        uint64_t of_slice;
+        const uint64_t part = lane < kSliceTurns * kW ? parts[lane] : 0, upto = ahead + wave_scan(part, &of_slice);
+        const int hit = __ffsll((unsigned long long)__ballot(upto >= target && upto - part < target)) - 1;
+        if (hit >= 0 && hit % kW == wave) {
+            const int v = v0 + hit / kW * kSliceThreads + (int)threadIdx.x;
+            const u32x4 w4 = row.load(v);
+            uint64_t of_wave;
+            const uint32_t keeps = keeps_of(w4, v);
+            const uint64_t own = kept_units<DT>(w, w4, keeps, row.first(v), table);
+            uint64_t at = lane_u(upto - part, hit) + wave_scan(own, &of_wave) - own;
+            if (at < target && at + own >= target)             // one lane
+                each_chosen<DT>(w4, keeps, row.first(v), [&](float y, int j) {
+                    const uint64_t one = w.of(y, table);
+                    if (at < target && at + one >= target) found = j;
+                    at += one;
+                });
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        const int j = sh.found;
-        a.token[r] = j;
-        const float x = load_elem<DT>(row.base, (int64_t)j + row.before);
-        if (a.logq) a.logq[r] = (float)(((double)x - (double)m) * inv - log(ldexp((double)Z, -a.shift)));
+    if (threadIdx.x) return;
+    const int j = min(found, a.V - 1);
+    a.token[r] = j;
+    if (a.logq) {
+        const float x = load_elem<DT>(row.base, (int64_t)j + row.before), T = a.temperature ? a.temperature[b] : 1.f;
+        a.logq[r] = (float)((T > 0.f ? ((double)x - (double)q.max) / (double)T : 0.0) - log(ldexp((double)Z, -a.shift)));
     }
-}
-
-__global__ __launch_bounds__(256) void clear_flags_kernel(uint32_t *flags, int B)
-{
-    const int b = blockIdx.x * 256 + threadIdx.x;
-    if (b < B) flags[b] = 0;
 }
 
 }  // namespace
@@ -512,14 +955,24 @@ hipError_t launch_filtered_sample(FilterArgs a, int dtype, hipStream_t st)
     int log2_v = 0;
     while ((1ll << log2_v) < a.V) ++log2_v;
     a.shift = 62 - log2_v < 50 ? 62 - log2_v : 50;
-    if (a.flags && a.K > 1) {
-        clear_flags_kernel<<<(a.B + 255) / 256, 256, 0, st>>>(a.flags, a.B);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
     const int64_t rows = (int64_t)a.B * a.K;
-    if (dtype == TAPOUT_F32) filtered_sample_kernel<TAPOUT_F32><<<rows, kThreads, 0, st>>>(a);
-    else filtered_sample_kernel<TAPOUT_BF16><<<rows, kThreads, 0, st>>>(a);
+    const int slices = filter_slices(a.V, dtype);
+    const auto launch = [&](auto elem) {
+        constexpr int DT = decltype(elem)::value;
+        filter_rows_kernel<DT><<<rows, kThreads, 0, st>>>(a);
+        filter_slices_kernel<DT><<<rows * slices, kSliceThreads, 0, st>>>(a, slices);
+        if (a.u || a.n_kept || a.flags) filter_tokens_kernel<DT><<<rows, kSliceThreads, 0, st>>>(a, slices);
+    };
+    if (dtype == TAPOUT_F32) launch(std::integral_constant<int, TAPOUT_F32>{});
+    else launch(std::integral_constant<int, TAPOUT_BF16>{});
     return hipGetLastError();
+}
+
+// Slices of a row: it may begin anywhere in its first vector.
+int filter_slices(int V, int dtype)
+{
+    const int n = dtype == TAPOUT_F32 ? 4 : 8;
+    return (V + n - 1 + kSliceVecs * n - 1) / (kSliceVecs * n);
 }
 
 }  // namespace tapout
