@@ -262,7 +262,8 @@ TAPOUT_API tapout_status tapout_draft_stats(tapout_ctx *ctx, const tapout_logits
  *     kept = d_j where all three keep j, else -infinity
  *     token = smallest j whose inclusive sum of the kept w exceeds u * Z, Z their
  *       sum;  logq = d_token - ln Z
- *   T <= 0: greedy, the argmax (smallest index) alone is kept (kept 0, logq 0);
+ *   T below 2^-126, 0 and negative ones among them: greedy, the argmax (smallest
+ *   index) alone is kept (kept 0, logq 0);
  *   T = +infinity: all weights are 1.
  *   Weights are computed in double and summed as whole multiples of 2^-s of the
  *   largest, s = min(50, 62 - ceil(log2 V)): results do not depend on how the work

@@ -69,7 +69,11 @@ struct Bound {
     float x; int32_t index;
     __device__ __forceinline__ bool holds(float y, int32_t j) const { return y > x || (y == x && j <= index); }
 };
-__device__ __forceinline__ float below(float x) { return value_of(key_of(x) - 1); }        // the next smaller value; of 0 a negative one
+__device__ __forceinline__ float below(float x)                                            // the next smaller value; of 0 a negative one
+{
+    const uint32_t k = key_of(x) - 1;
+    return value_of(k == 0x7fffffffu ? k - 1 : k);              // that key is no value's: it would be -0
+}
 constexpr int kAll = 0x7fffffff, kNone = (int)0x80000000u;       // of a value's elements (indices before a row are negative)
 __device__ __forceinline__ Bound shorter(Bound a, Bound b) { return a.x > b.x || (a.x == b.x && a.index < b.index) ? a : b; }
 
@@ -437,7 +441,8 @@ template <class E, int N> __device__ __forceinline__ void store_any(E *to, const
     }
 }
 
-// What a row asks for.
+// What a row asks for.  Temperatures below the smallest normal number, whose inverse binary32 does not hold, are as good as 0.
+constexpr float kLeastT = 0x1p-126f;
 struct Filters {
     float T, top_p, min_p; int top_k; bool greedy;
 };
@@ -684,7 +689,7 @@ __global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a)
     if (a.k_len && k >= a.k_len[b]) return;
     const RowReader<DT> row(row_address(a.base, DT, a.stride_b, a.stride_k, b, k), a.V);
     Filters f{a.temperature ? a.temperature[b] : 1.f, a.top_p ? a.top_p[b] : 1.f, a.min_p ? a.min_p[b] : 0.f, a.top_k ? a.top_k[b] : 0, false};
-    f.greedy = !(f.T > 0.f);
+    f.greedy = !(f.T >= kLeastT);
     if (threadIdx.x < 256) sh.table[threadIdx.x] = a.exp_table[threadIdx.x];
     if (threadIdx.x == 0) { sh.bad = f.T != f.T; sh.irregular = 0; sh.tinies = 0; sh.found = 0; }
     __syncthreads();
@@ -708,7 +713,7 @@ __global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a)
     __syncthreads();
     if (threadIdx.x) return;
     const bool bad = sh.bad;
-    FilterRow q{max, f.greedy ? 0.f : fminf(1.f / f.T, 3.402823466e38f), end.x, end.x, kNone, kept, bad, 0, w.c};      // inv is finite: 0 times it stays 0
+    FilterRow q{max, f.greedy ? 0.f : 1.f / f.T, end.x, end.x, kNone, kept, bad, 0, w.c};
     if (bad) q = FilterRow{0.f, 0.f, INFINITY, INFINITY, kNone, 0, 1, 0, 0.0};
     else if (end.index == kAll) q.above = q.from = below(end.x);
     else if (end.index != kNone) { q.from = below(end.x); q.last = end.index; }
@@ -944,7 +949,7 @@ __global__ __launch_bounds__(kSliceThreads) void filter_tokens_kernel(FilterArgs
     a.token[r] = j;
     if (a.logq) {
         const float x = load_elem<DT>(row.base, (int64_t)j + row.before), T = a.temperature ? a.temperature[b] : 1.f;
-        a.logq[r] = (float)((T > 0.f ? ((double)x - (double)q.max) / (double)T : 0.0) - log(ldexp((double)Z, -a.shift)));
+        a.logq[r] = (float)((T >= kLeastT ? ((double)x - (double)q.max) / (double)T : 0.0) - log(ldexp((double)Z, -a.shift)));
     }
 }
 
