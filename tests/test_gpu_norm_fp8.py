@@ -1,0 +1,437 @@
+"""The norm in front of the head with its gradient, 8-bit blocks, and logits under them, against plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+from paper_2511_02017_amd import binding
+from tests import operators_util as ou
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+f32, bf16, i32, u8 = torch.float32, torch.bfloat16, torch.int32, torch.uint8
+EPS = 1e-5
+
+
+def rand(*shape, seed, scale=1.0, dtype=f32):
+    return (torch.randn(*shape, generator=torch.Generator().manual_seed(seed)) * scale).to(dtype)
+
+
+def within(got, want, bound):
+    got, want, bound = got.cpu().double(), want.double(), bound.double()
+    ok = ((got - want).abs() <= bound) | (torch.isnan(got) & torch.isnan(want))
+    assert ok.all(), (f"{int((~ok).sum())} of {ok.numel()} off, worst {float(((got - want).abs() / bound).nan_to_num(nan=float('inf')).max()):.3g} bounds; "
+                      f"first at {ok.logical_not().nonzero()[0].tolist()}")
+
+
+# ---- 8-bit blocks -----------------------------------------------------------------------------------------------
+def special_rows(cols, dtype):
+    x = rand(140, cols, seed=cols, dtype=dtype)
+    x[0] = 0
+    x[1] *= 2.0 ** -130                                  # below the smallest normal number
+    x[2] *= 2.0 ** 120
+    x[3, 0], x[4, cols // 2], x[5, cols - 1] = float("nan"), float("inf"), -float("inf")
+    x[6] = torch.arange(cols).remainder(97).sub(48).div(8).to(dtype)      # ties
+    x[7] = -0.0
+    x[8, 1:] = 0
+    x[9] *= torch.exp2(torch.arange(cols).remainder(40).float() - 20).to(dtype)
+    x[10] = 448.0
+    x[11] = torch.arange(cols).remainder(448).to(dtype)
+    return x
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("cols", [32, 96, 128, 160, 1120])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_codes_scales_and_values(cols, dtype, block_rows):
+    x = special_rows(cols, dtype)
+    if block_rows == 128:
+        x = torch.cat((x[12:], x, x[12:100], x[:2]))      # blocks with and without bad elements, the last one short
+    q, s = ou.fp8(x, block_rows)
+    c, got = binding.fp8_quantize(x.to(DEV), block_rows)
+    torch.cuda.synchronize()
+    assert torch.equal(got.cpu().nan_to_num(nan=-1.0), s.nan_to_num(nan=-1.0))
+    fine = ~torch.isnan(q)
+    assert torch.equal(ou.code_values(c)[fine], q[fine])
+    for out in (bf16, f32):
+        v = binding.fp8_dequantize(c, got, cols, block_rows, dtype=out).cpu()
+        want = (q * ou.spread(s, len(x), block_rows))[:, :cols].float().to(out)          # products of 4 and 24 bits: one rounding, then the type's
+        assert torch.equal(v.float().nan_to_num(nan=-1.0), want.float().nan_to_num(nan=-1.0))
+
+
+@pytest.mark.parametrize("rows", [0, 1, 2, 127, 129, 1025])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_rows_strides_and_given_outputs(rows, block_rows):
+    wide = rand(rows, 3, 160, seed=rows, dtype=bf16).to(DEV)
+    x = wide[:, 1]                                       # rows 480 elements apart
+    R = -(-rows // block_rows)
+    c = torch.full((rows + 1, 256), 0xAB, dtype=u8, device=DEV)
+    s = torch.full((R + 1, 2), 7.0, device=DEV)
+    binding.fp8_quantize(x, block_rows, out=(c[:rows], s[:R]))
+    out = torch.full((rows + 1, 192), 7.0, dtype=f32, device=DEV)
+    binding.fp8_dequantize(c[:rows], s[:R], 160, block_rows, out=out[:rows, :160])
+    torch.cuda.synchronize()
+    q, want = ou.fp8(x.cpu(), block_rows)
+    assert torch.equal(s[:R].cpu(), want) and torch.equal(ou.code_values(c[:rows]), q)
+    assert torch.equal(out[:rows, :160].cpu(), (q * ou.spread(want, rows, block_rows))[:, :160].float())
+    assert (out[:, 160:] == 7).all() and (out[rows] == 7).all() and (c[rows] == 0xAB).all() and (s[R] == 7).all() and (c[:rows, 160:] == 0).all()
+
+
+def test_blocks_beyond_32_bits_of_offsets():
+    rows, cols = 2 ** 16 + 300, 32768
+    x = torch.zeros(rows, cols, dtype=bf16, device=DEV)
+    x[-200:] = rand(200, cols, seed=1, dtype=bf16).to(DEV)
+    for block_rows in (1, 128):
+        c, s = binding.fp8_quantize(x, block_rows)
+        q, want = ou.fp8(x[-300:].cpu() if block_rows == 1 else x[2 ** 16:].cpu(), block_rows)
+        assert torch.equal(s[-len(want):].cpu(), want) and torch.equal(ou.code_values(c[-300:]), q[-300:])
+        assert int(c[:2 ** 16].count_nonzero()) == 0
+        v = binding.fp8_dequantize(c, s, cols, block_rows, out=x)
+        assert torch.equal(v[-300:].cpu().double(), (q * ou.spread(want, 300, block_rows)).float().to(bf16).double())
+
+
+# ---- logits ---------------------------------------------------------------------------------------------------------
+def weights(V, D, seed, block_rows=128):
+    w = rand(V, D, seed=seed, scale=2 / D ** 0.5)
+    w *= torch.exp(0.5 * torch.randn(V, 1, generator=torch.Generator().manual_seed(seed + 1)))
+    q, s = ou.fp8(w, block_rows)
+    return binding.fp8_quantize(w.to(DEV), 128), q, s
+
+
+def check_logits(B, K, V, D, dtype, out, seed=0):
+    (c, s), qw, sw = weights(V, D, seed)
+    h = rand(B, K, D, seed=seed + 2, dtype=dtype)
+    head = binding.DraftHead(B * K + 1, D, V + 3, dtype=dtype)
+    z = head.logits_fp8(h.to(DEV), c, s, dtype=out)
+    codes, scales = binding.fp8_quantize(h.to(DEV).view(B * K, D))
+    again = head.logits_fp8(codes.view(B, K, -1), c, s, act_scales=scales.view(B, K, -1), dtype=out)
+    torch.cuda.synchronize()
+    assert torch.equal(z, again)
+    qa, sa = ou.fp8(h.view(B * K, D))
+    want, bound = ou.logits_fp8(qa, sa, qw, sw, out)
+    within(z.reshape(B * K, V), want, bound)
+
+
+@pytest.mark.parametrize("out", [bf16, f32])
+@pytest.mark.parametrize("B,K,V,D", [(1, 1, 1, 32), (1, 1, 129, 128), (3, 5, 130, 96), (1, 16, 300, 160), (17, 1, 257, 288), (4, 8, 127, 32), (11, 3, 515, 64),
+                                     (64, 1, 128, 256), (5, 13, 400, 96), (16, 8, 385, 160), (43, 3, 300, 64), (3, 67, 513, 416), (1, 300, 260, 128)])
+def test_logits_sizes(B, K, V, D, out):
+    check_logits(B, K, V, D, bf16 if (B + V) % 2 else f32, out)
+
+
+@pytest.mark.parametrize("out", [bf16, f32])
+@pytest.mark.parametrize("N", [1, 16, 17, 33, 65, 129, 257])
+def test_logits_of_more_tiles_than_run_at_a_time(N, out):
+    """Over a vocabulary of hundreds of tiles: the plain form on a part of its rows, from every place where blocks of scales meet."""
+    V, D = 140_001 if N < 100 else 70_001, 96
+    g = torch.Generator(device=DEV).manual_seed(N)
+    w = torch.randn(V, D, generator=g, device=DEV) * 0.2
+    c, s = binding.fp8_quantize(w, 128)
+    h = rand(1, N, D, seed=N, dtype=bf16)
+    z = binding.DraftHead(N, D, V).logits_fp8(h.to(DEV), c, s, dtype=out)[0].cpu()
+    qa, sa = ou.fp8(h[0])
+    sw = s.cpu()
+    for v0 in list(range(0, V - 256, 256 * 37)) + [V - 256]:
+        at = v0 // 128 * 128
+        part = slice(at, min(at + 256, V))
+        want, bound = ou.logits_fp8(qa, sa, ou.code_values(c[part]), sw[at // 128:at // 128 + 2], out)
+        within(z[:, part], want, bound)
+
+
+@pytest.mark.parametrize("out", [bf16, f32])
+@pytest.mark.parametrize("B,K", [(3, 4), (9, 15)])
+def test_logits_strides_lengths_and_neighbours(B, K, out):
+    V, D = 333, 96
+    (c, s), qw, sw = weights(V, D, 5)
+    wide = rand(K, B, 2 * D, seed=8, dtype=bf16).to(DEV)
+    h = wide.transpose(0, 1)[..., D:]                                                 # sequences inside positions
+    lengths = torch.randint(0, K + 1, (B,), generator=torch.Generator().manual_seed(1), dtype=i32)
+    room = torch.full((B, K, V + 21), 7.0, dtype=out, device=DEV)
+    z = room[..., 5:5 + V]
+    binding.DraftHead(B * K, D, V).logits_fp8(h, c, s, k_len=lengths.to(DEV), out=z)
+    torch.cuda.synchronize()
+    qa, sa = ou.fp8(h.reshape(B * K, D).cpu())
+    want, bound = (t.view(B, K, V) for t in ou.logits_fp8(qa, sa, qw, sw, out))
+    live = torch.arange(K)[None] < lengths[:, None]
+    within(z.cpu()[live], want[live], bound[live])
+    assert (z.cpu()[~live] == 7).all() and (room[..., :5] == 7).all() and (room[..., 5 + V:] == 7).all()
+
+
+@pytest.mark.parametrize("out", [bf16, f32])
+@pytest.mark.parametrize("N", [3, 40, 300])
+def test_logits_of_extreme_blocks(N, out):
+    """A scale or code that is NaN, scales of 0, the smallest and large ones; a hidden state that holds a NaN or an infinity."""
+    V, D = 300, 256
+    (c, s), _, _ = weights(V, D, 3)
+    c[9] = 0
+    s[1, 0] = 0.0
+    s[1, 1] = 2.0 ** -126
+    s[2] = 2.0 ** 100
+    c[20, 3] = 0x7f
+    h = rand(1, N, D, seed=6, dtype=bf16).to(DEV)
+    h[0, 1, 5], h[0, 2, 200] = float("nan"), float("inf")
+    z = binding.DraftHead(N, D, V).logits_fp8(h, c, s, dtype=out)[0].cpu()
+    ok = torch.ones(N, dtype=torch.bool)
+    ok[1:3] = False
+    assert z[1:3].isnan().all() and z[:, 20].isnan().all()
+    assert (z[ok][:, 9] == 0).all() and (z[ok][:, 128:256].abs() < 1e-33).all()
+    assert torch.isfinite(z[ok][:, [v for v in range(256) if v != 20]]).all() and (z[ok][:, 256:].abs() > 1e24).any()
+    s[0] = float("nan")
+    z = binding.DraftHead(N, D, V).logits_fp8(h, c, s, dtype=out)[0].cpu()
+    assert z[ok][:, :128].isnan().all() and torch.isfinite(z[ok][:, 128:256]).all()
+
+
+def test_logits_beside_other_memory():
+    """Behind the last rows of weights, scales and hidden states lies what would show in the results."""
+    N, V, D = 33, 129, 160
+    (c, s), qw, sw = weights(V, D, 2)
+    codes, scales = torch.full((V + 300, 256), 0x7f, dtype=u8, device=DEV), torch.full((8, 2), math.nan, device=DEV)
+    codes[:V], scales[:2] = c, s
+    h = rand(1, N, D, seed=1, dtype=bf16)
+    a, sa = binding.fp8_quantize(h[0].to(DEV))
+    acts, act_s = torch.full((N + 300, 256), 0x7f, dtype=u8, device=DEV), torch.full((N + 300, 2), math.nan, device=DEV)
+    acts[:N], act_s[:N] = a, sa
+    z = binding.DraftHead(N, D, V).logits_fp8(acts[:N].view(1, N, -1), codes[:V], scales[:2], act_scales=act_s[:N].view(1, N, -1), dtype=f32)
+    qa, s64 = ou.fp8(h[0])
+    within(z[0], *ou.logits_fp8(qa, s64, qw, sw, f32))
+
+
+# ---- norm ------------------------------------------------------------------------------------------------------------
+# every way of dividing a row among threads, one more and one less than it holds
+DIMS = [32, 96, 256, 288, 512, 544, 1024, 1056, 1120, 2048, 2080, 4096, 4128, 8192, 8224, 16384, 16416, 32768, 32800, 65536]
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("D", DIMS)
+def test_norm_and_its_gradient(D, dtype):
+    for B, K in ((1, 1), (3, 7)) + (((2, 300),) if D <= 2080 else ()):
+        head = binding.DraftHead(B * K, D, 1, dtype=dtype, training=True)
+        x, res = rand(B, K, D, seed=1, dtype=dtype), rand(B, K, D, seed=2, scale=3, dtype=dtype)
+        w, g, more = 1 + rand(D, seed=3, scale=0.2, dtype=dtype), rand(B, K, D, seed=4, scale=0.1, dtype=dtype), rand(B, K, D, seed=5, scale=0.1, dtype=dtype)
+        d = lambda t: t.to(DEV)                                                      # noqa: E731
+        f = head.norm(d(x), d(w), residual=d(res), eps=EPS)
+        e = head.norm(d(x), d(w), residual=d(res), eps=EPS, fp8=True)
+        alone = head.norm(d(x), d(w), eps=EPS)
+        b = head.norm_grad(d(g), f["sum"], d(w), f["rstd"])
+        both = head.norm_grad(d(g), f["sum"], d(w), f["rstd"], grad_sum=d(more))
+        torch.cuda.synchronize()
+        total = (x.float() + res.float()).to(dtype)
+        assert torch.equal(f["sum"].cpu(), total) and torch.equal(e["sum"].cpu(), total) and alone["sum"].data_ptr() != f["sum"].data_ptr()
+        s, w64 = total.view(-1, D).double(), w.double()
+        y, r = ou.norm(s, w64, EPS)
+        within(f["out"].view(-1, D), y, ou.norm_bound(y, dtype))
+        within(f["rstd"].view(-1, 1), r, 2 * ou.U32 * r)
+        y1, _ = ou.norm(x.view(-1, D).double(), w64, EPS)
+        within(alone["out"].view(-1, D), y1, ou.norm_bound(y1, dtype))
+        # 8 bits: half a step of the value (2^-4), below 2^-6 of the scale's units half of 2^-9; the scale follows the largest value's roundings
+        v = binding.fp8_dequantize(e["codes"], e["scales"], D, dtype=f32).cpu().view(-1, D).double()
+        top = torch.zeros(len(y), -(-D // 128) * 128, dtype=torch.float64)
+        top[:, :D] = y.abs()
+        scale = top.view(len(y), -1, 128).amax(-1) / ou.TOP
+        within(e["scales"].view(len(y), -1), scale, 8 * ou.U32 * scale + 2.0 ** -149)
+        within(v, y, y.abs() * (2.0 ** -4 + 2.0 ** -18) + scale.repeat_interleave(128, 1)[:, :D] * 2.0 ** -10 * 1.001)
+        if D % 128:
+            assert (e["codes"].cpu()[..., D:] == 0).all()
+        for got, m in ((b, None), (both, more.view(-1, D).double())):
+            dx, dw, bx, bw = ou.norm_grad(g.view(-1, D).double(), s, w64, EPS, m, dtype)
+            within(got["grad_x"].view(-1, D), dx, bx)
+            within(got["grad_weight"], dw, bw)
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+def test_norm_gradient_over_many_rows(dtype):
+    """More rows than workgroups take at a time, held to 64 bits on the GPU."""
+    N, D = 20_011, 160
+    g = torch.Generator(device=DEV).manual_seed(3)
+    s, dy = (torch.randn(1, N, D, generator=g, device=DEV).to(dtype) for _ in range(2))
+    w = torch.ones(D, dtype=dtype, device=DEV)
+    head = binding.DraftHead(N, D, 1, dtype=dtype, training=True)
+    f = head.norm(s, w, eps=EPS)
+    got = head.norm_grad(dy, s, w, f["rstd"])
+    dx, dw, bx, bw = ou.norm_grad(dy[0].double(), s[0].double(), w.double(), EPS, None, dtype)
+    assert ((got["grad_x"][0].double() - dx).abs() <= bx).all() and ((got["grad_weight"].double() - dw).abs() <= bw).all()
+    # sums of this many terms stay far inside their bound
+    assert float((got["grad_weight"].double() - dw).norm() / dw.norm()) < (2.0 ** -8 if dtype == bf16 else 2.0 ** -20)
+
+
+def test_norm_gradient_is_the_slope():
+    B, K, D = 2, 3, 64
+    head = binding.DraftHead(B * K, D, 1, dtype=f32, training=True)
+    s, w, g = rand(B, K, D, seed=1).to(DEV), (1 + rand(D, seed=2, scale=0.3)).to(DEV), rand(B, K, D, seed=3).to(DEV)
+    f = head.norm(s, w, eps=EPS)
+    b = head.norm_grad(g, s, w, f["rstd"])
+    val = lambda a, c: float((head.norm(a, c, eps=EPS)["out"].double() * g.double()).sum())         # noqa: E731
+    eps = 2.0 ** -5
+    for seed in range(4):
+        for which in (0, 1):
+            d = rand(*(s.shape if which == 0 else w.shape), seed=20 + seed).to(DEV)
+            d /= d.norm()
+            lo, hi = (val(s + q * d, w) if which == 0 else val(s, w + q * d) for q in (-eps, eps))
+            slope = float(((b["grad_x"] if which == 0 else b["grad_weight"]).double() * d).sum())
+            # |g . y| is below |g| |y| < 20 * 28, its terms off by 4 u; the third derivative of a row's y along a unit step is below 15 |y| / |s|^3
+            # (|s| > 5 here), against |g| / row below 12
+            assert abs((hi - lo) / (2 * eps) - slope) < 4 * ou.U32 * 560 / eps + 15 * 12 * 12 / 125 * eps ** 2 / 6
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+def test_norm_in_place_strided_and_with_single_outputs(dtype):
+    B, K, D = 3, 5, 288
+    head = binding.DraftHead(B * K, D, 1, dtype=dtype, training=True)
+    x, res, w = rand(B, K, D, seed=1, dtype=dtype), rand(B, K, D, seed=2, dtype=dtype), rand(D, seed=3, dtype=dtype).to(DEV)
+    want = head.norm(x.to(DEV), w, residual=res.to(DEV), eps=EPS)
+    wide = torch.full((K, B, 3 * D), 7.0, dtype=dtype, device=DEV)
+    xs, rs, ys = (wide.transpose(0, 1)[..., i * D:(i + 1) * D] for i in range(3))         # sequences inside positions
+    for into in (rs, xs):                                                             # the sum in the place of either
+        xs.copy_(x), rs.copy_(res)
+        head.norm(xs, w, residual=rs, eps=EPS, out=dict(sum=into, out=ys))
+        assert torch.equal(into, want["sum"]) and torch.equal(ys, want["out"])
+        assert torch.equal(rs if into is xs else xs, (res if into is xs else x).to(DEV))
+    rstd = torch.zeros(B, K, device=DEV)
+    head.norm(x.to(DEV), w, residual=res.to(DEV), eps=EPS, out=dict(rstd=rstd))
+    assert torch.equal(rstd, want["rstd"])
+    g, more = rand(B, K, D, seed=5, dtype=dtype).to(DEV), rand(B, K, D, seed=6, dtype=dtype).to(DEV)
+    grads = head.norm_grad(g, want["sum"], w, rstd, grad_sum=more)
+    for into in ("g", "s", "more"):
+        t = dict(g=g.clone(), s=want["sum"].clone(), more=more.clone())
+        gw = torch.zeros(D, dtype=dtype, device=DEV)
+        head.norm_grad(t["g"], t["s"], w, rstd, grad_sum=t["more"], out=dict(grad_x=t[into], grad_weight=gw))
+        assert torch.equal(t[into], grads["grad_x"]) and torch.equal(gw, grads["grad_weight"])
+    # one row for all
+    one = x[:1, :1].to(DEV).expand(B, K, D)
+    assert torch.equal(head.norm(one, w, eps=EPS)["out"][2, 3], head.norm(x[:1, :1].to(DEV), w, eps=EPS)["out"][0, 0])
+
+
+def test_norm_of_extreme_rows():
+    D = 160
+    x = torch.zeros(1, 7, D)
+    x[0, 0] = 0
+    x[0, 1] = 2e19                                       # whose squares binary32 does not hold
+    x[0, 2] = 1e-30
+    x[0, 3, 5] = float("nan")
+    x[0, 4, 7] = float("inf")
+    x[0, 5] = 3e38
+    x[0, 6] = 1e-45
+    w = torch.ones(D, device=DEV)
+    head = binding.DraftHead(7, D, 1, dtype=f32)
+    f = head.norm(x.to(DEV), w, eps=0.0)
+    e = head.norm(x.to(DEV), w, eps=1e-6, fp8=True)
+    y = f["out"][0].cpu()
+    assert y[0].isnan().all() and (y[[1, 2, 5]] - 1).abs().max() <= 4 * ou.U32 and y[3].isnan().all()
+    assert torch.isfinite(head.norm(x.to(DEV), w, eps=1e-6)["out"][0, 0]).all()
+    s = e["scales"][0].cpu()
+    assert s[3].isnan().all() and s[4].isnan().any() and torch.isfinite(s[[0, 1, 2, 5, 6]]).all()
+    assert (e["codes"][0, 0].cpu() == 0).all()
+
+
+def test_no_rows():
+    head = binding.DraftHead(4, 64, 1, training=True)
+    e = torch.empty(0, 2, 64, dtype=bf16, device=DEV)
+    w = torch.ones(64, dtype=bf16, device=DEV)
+    f = head.norm(e, w, residual=e)
+    gw = torch.full((64,), 5.0, dtype=bf16, device=DEV)
+    head.norm_grad(e, f["sum"], w, f["rstd"], out=dict(grad_x=e, grad_weight=gw))
+    assert (gw == 0).all() and head.norm(e, w, fp8=True)["codes"].shape == (0, 2, 128)
+    c, s = binding.fp8_quantize(torch.ones(8, 64, device=DEV), 128)
+    assert binding.DraftHead(4, 64, 8).logits_fp8(e, c, s).shape == (0, 2, 8)
+
+
+# ---- together ----------------------------------------------------------------------------------------------------------
+def chain(head, tp, x, res, w, c, s, u, T, p, **kw):
+    """From the last layer's output to drawn tokens under an 8-bit head."""
+    f = head.norm(x, w, residual=res, fp8=True, **kw)
+    z = head.logits_fp8(f["codes"], c, s, act_scales=f["scales"], **kw)
+    r = tp.sample(z, u, temperature=T, top_p=p, kept=bf16, **kw)
+    return dict(f, z=z, **r)
+
+
+def same(a, b):
+    for k in a:
+        assert torch.equal(a[k].contiguous().view(u8), b[k].contiguous().view(u8)), k
+
+
+@pytest.mark.parametrize("B,K,V,D", [(2, 3, 500, 96), (24, 1, 3001, 288), (40, 8, 2000, 160)])
+def test_from_states_to_tokens_on_streams_and_in_a_replayed_graph(B, K, V, D):
+    head, tp = binding.DraftHead(B * K, D, V), binding.Tapout(B, K, V)
+    (c, s), qw, sw = weights(V, D, 7)
+    w = torch.ones(D, dtype=bf16, device=DEV)
+    T, p = torch.full((B,), 0.8, device=DEV), torch.full((B,), 0.9, device=DEV)
+    sets = [[rand(B, K, D, seed=10 * i + j, dtype=bf16).to(DEV) for j in range(2)] + [torch.rand(B, K, generator=torch.Generator().manual_seed(i)).to(DEV)]
+            for i in range(3)]
+    run = lambda q, **kw: chain(head, tp, q[0], q[1], w, c, s, q[2], T, p, **kw)       # noqa: E731
+    want = [run(q) for q in sets]
+    torch.cuda.synchronize()
+    # the tokens are those of the logits that were written
+    for b in range(min(B, 4)):
+        ref = ou.filtered(want[0]["z"][b, 0].cpu(), float(T[b]), 0, float(p[b]), 0.0, float(sets[0][2][b, 0]))
+        assert int(want[0]["token"][b, 0]) == ref["token"] and int(want[0]["n_kept"][b, 0]) == ref["n"]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = run(sets[1], stream=side)
+    side.synchronize()
+    same(got, want[1])
+    held = [t.clone() for t in sets[0]]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = run(held)
+    for i in (1, 0, 2, 1):
+        for a, b in zip(held, sets[i]):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        same(out, want[i])
+        same(run(sets[2]), want[2])
+        torch.cuda.synchronize()
+
+
+# ---- refusals ------------------------------------------------------------------------------------------------------------
+def test_refusals():
+    head = binding.DraftHead(8, 64, 100)
+    x, w = torch.zeros(2, 4, 64, dtype=bf16, device=DEV), torch.ones(64, dtype=bf16, device=DEV)
+    c, s = binding.fp8_quantize(torch.ones(100, 64, device=DEV), 128)
+    f = head.norm(x, w)
+    with pytest.raises(binding.TapoutError, match="training"):
+        head.norm_grad(x, f["sum"], w, f["rstd"])
+    with pytest.raises(binding.TapoutError, match="max_rows"):
+        head.norm(torch.cat([x, x]), w)
+    for eps in (-1e-6, math.nan, math.inf):
+        with pytest.raises(binding.TapoutError, match="eps"):
+            head.norm(x, w, eps=eps)
+    with pytest.raises(binding.TapoutError, match="overlap"):
+        head.norm(x, w, out=dict(out=torch.zeros(2, 1, 64, dtype=bf16, device=DEV).expand(2, 4, 64)))
+    with pytest.raises(binding.TapoutError, match="aligned"):
+        head.norm(x, torch.ones(65, dtype=bf16, device=DEV)[1:])
+    with pytest.raises(binding.TapoutError, match="NULL"):
+        head.norm(x, w, out=dict(codes=torch.zeros(2, 4, 128, dtype=u8, device=DEV)))
+    with pytest.raises(ValueError):
+        head.norm(x.float(), w)
+    with pytest.raises(ValueError):
+        head.norm(x, w.float())
+    with pytest.raises(ValueError):
+        head.norm(x, w, residual=x[:, :2])
+    with pytest.raises(ValueError, match="cpu"):
+        head.norm(x, w, residual=x.cpu())
+    with pytest.raises(binding.TapoutError, match="vocab"):
+        big = binding.fp8_quantize(torch.ones(200, 64, device=DEV), 128)
+        head.logits_fp8(x, *big)
+    with pytest.raises(binding.TapoutError, match="overlap"):
+        head.logits_fp8(x, c, s, out=torch.empty(2, 1, 100, dtype=bf16, device=DEV).expand(2, 4, 100))
+    with pytest.raises(ValueError):
+        head.logits_fp8(x, c[:50], s[:0])
+    with pytest.raises(ValueError):
+        head.logits_fp8(x, c, s.double())
+    with pytest.raises(ValueError):
+        head.logits_fp8(x, c, s, act_scales=torch.zeros(2, 4, 1, device=DEV))         # states that are not codes
+    with pytest.raises(ValueError):
+        head.logits_fp8(torch.zeros(2, 4, 64, dtype=u8, device=DEV), c, s, act_scales=torch.zeros(2, 4, 1, device=DEV))
+    with pytest.raises(binding.TapoutError, match="block_rows"):
+        binding.fp8_quantize(torch.ones(100, 64, device=DEV), 64)
+    with pytest.raises(binding.TapoutError, match="cols"):
+        binding.fp8_quantize(torch.ones(4, 40, device=DEV))
+    with pytest.raises(ValueError):
+        binding.fp8_dequantize(c, s, 64, 128, out=torch.empty(100, 32, device=DEV))
+    head.close()
+    with pytest.raises(binding.TapoutError, match="NULL"):
+        head.norm(x, w)
+    with pytest.raises(binding.TapoutError, match="NULL"):
+        head.logits_fp8(x, c, s)
