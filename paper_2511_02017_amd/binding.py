@@ -688,6 +688,7 @@ class Tapout:
 
 # ---- the draft model's output head ------------------------------------------------------------------------
 _DT = {torch.float32: F32, torch.bfloat16: BF16}
+_EMPTY = {torch.float32: 0, torch.bfloat16: 1, torch.int32: 2, torch.uint8: 3}              # types that _marshal.empty makes
 MX4_BLOCK, MX4_PAD = 32, 128
 
 
@@ -709,7 +710,8 @@ def _on(t, dev, name):
 def _empty(shape, dtype, device, stream):
     """An output of a call on `stream`: its memory belongs to that stream, so that it is not handed on while the call still works on it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        t = _fast.empty(tuple(shape), _EMPTY[dtype], device.index) if dtype in _EMPTY and device.type == "cuda" and device.index is not None else None
+        return torch.empty(shape, dtype=dtype, device=device) if t is None else t
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
@@ -783,14 +785,15 @@ def fp8_dequantize(codes, scales, cols: int, block_rows: int = 1, dtype=torch.bf
     """tapout_fp8_dequantize: the values [rows, cols] that codes and scales stand for; of codes [..., P] with scales [..., P / 128], as norm
     writes them, [..., cols]."""
     lib = _lib or load_library()
-    if codes.dim() > 2 and block_rows == 1 and scales.dim() == codes.dim() and (out is None or out.is_contiguous()):
-        flat = fp8_dequantize(codes.flatten(0, -2), scales.flatten(0, -2), cols, 1, dtype, None if out is None else out.flatten(0, -2), stream)
-        return flat.view(*codes.shape[:-1], cols) if out is None else out
-    rows, P, R = codes.shape[0], -(-cols // FP8_BLOCK) * FP8_BLOCK, -(-codes.shape[0] // max(int(block_rows), 1))
+    lead = codes.shape[:-1]
     if out is None:
-        out = _empty((rows, cols), dtype, codes.device, stream)
+        out = _empty((*lead, cols), dtype, codes.device, stream)
     st = _fast.fp8_dequantize(codes, scales, cols, int(block_rows), out, _handle(stream))
+    if st is None and codes.dim() > 2 and block_rows == 1 and scales.shape[:-1] == lead and out.shape[:-1] == lead and out.is_contiguous():
+        fp8_dequantize(codes.flatten(0, -2), scales.flatten(0, -2), cols, 1, dtype, out.flatten(0, -2), stream)
+        return out
     if st is None:
+        rows, P, R = codes.shape[0], -(-cols // FP8_BLOCK) * FP8_BLOCK, -(-codes.shape[0] // max(int(block_rows), 1))
         m = _matrix(out, "out")
         if tuple(out.shape) != (rows, cols):
             raise ValueError(f"out: expected shape {(rows, cols)}, got {tuple(out.shape)}")

@@ -5,6 +5,7 @@
 // code does and, if all of them are in order, calls the library and returns its status.  At anything unusual (another type,
 // a tensor subclass, a wrong shape or device, a missing output) it returns None before anything is called, and the Python
 // code, which describes errors, takes over.  No results, addresses or tensors are kept.
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -552,13 +553,32 @@ PyObject *fp8_dequantize(PyObject *const *p)
 {
     Args a;
     int64_t rows = 0, cols = 0;
-    const tapout_matrix out = a.matrix(p[4], &rows, &cols);
-    a.device(c10::hip::current_device(), {p[0], p[1], p[4]});
-    if (cols != a.i32(p[2])) a.ok = false;
     const int32_t block = a.i32(p[3]);
-    const int64_t P = codes_cols(cols);
-    uint8_t *codes = a.required<uint8_t>(p[0], kU8, {rows, P});
-    float *scales = a.required<float>(p[1], kF32, {block_count(rows, block), P / 128});
+    const at::Tensor *c = a.tensor(p[0]), *o = a.tensor(p[4]);
+    const uint8_t *codes = nullptr;
+    const float *scales = nullptr;
+    tapout_matrix out = {};
+    if (a.ok && c->dim() == 3 && block == 1) {                  // [B, K, P], as the norm writes them: rows behind each other
+        const int64_t B = c->size(0), K = c->size(1);
+        cols = a.i32(p[2]);
+        rows = B * K;
+        const int64_t P = codes_cols(cols);
+        codes = a.required<uint8_t>(p[0], kU8, {B, K, P});
+        scales = a.required<float>(p[1], kF32, {B, K, P / 128});
+        const bool f32 = o->scalar_type() == kF32;
+        if (!f32 && o->scalar_type() != at::kBFloat16) a.ok = false;
+        out.dtype = f32 ? TAPOUT_F32 : TAPOUT_BF16;
+        out.ptr = a.required(p[4], f32 ? kF32 : at::kBFloat16, {B, K, cols});
+        out.stride = cols;
+        if (rows > INT32_MAX) a.ok = false;
+    } else {
+        out = a.matrix(p[4], &rows, &cols);
+        if (cols != a.i32(p[2])) a.ok = false;
+        const int64_t P = codes_cols(cols);
+        codes = a.required<uint8_t>(p[0], kU8, {rows, P});
+        scales = a.required<float>(p[1], kF32, {block_count(rows, block), P / 128});
+    }
+    a.device(c10::hip::current_device(), {p[0], p[1], p[4]});
     void *st = a.stream(p[5]);
     if (!g_lib.fp8_dequantize) a.ok = false;
     return call(a, [&] { return g_lib.fp8_dequantize(codes, scales, (int32_t)rows, (int32_t)cols, block, &out, st); });
@@ -729,6 +749,27 @@ PyObject *load(PyObject *, PyObject *arg)
     Py_RETURN_NONE;
 }
 
+// empty(shape, dtype, device): an output, as torch.empty makes it; dtype 0 float32, 1 bfloat16, 2 int32, 3 uint8
+PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kInt, at::kByte};
+    int64_t shape[8];
+    if (n != 3 || !PyTuple_CheckExact(args[0]) || PyTuple_GET_SIZE(args[0]) > 8) Py_RETURN_NONE;
+    const Py_ssize_t dims = PyTuple_GET_SIZE(args[0]);
+    Args a;
+    for (Py_ssize_t k = 0; k < dims; ++k) {
+        shape[k] = a.integer(PyTuple_GET_ITEM(args[0], k));
+        if (shape[k] < 0) a.ok = false;
+    }
+    const int32_t type = a.i32(args[1]), dev = a.i32(args[2]);
+    if (!a.ok || type < 0 || type > 3 || dev < 0) Py_RETURN_NONE;
+    try {
+        return THPVariable_Wrap(at::empty(at::IntArrayRef(shape, dims), at::TensorOptions().dtype(types[type]).device(at::kCUDA, (c10::DeviceIndex)dev)));
+    } catch (const std::exception &) {                            // out of memory, say: torch.empty raises it in its own words
+        Py_RETURN_NONE;
+    }
+}
+
 // current_stream(): handle of the current stream of the current device
 PyObject *current_stream(PyObject *, PyObject *)
 {
@@ -742,7 +783,7 @@ PyObject *current_stream(PyObject *, PyObject *)
 
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
-    {"load", load, METH_O, nullptr}, {"current_stream", current_stream, METH_NOARGS, nullptr},
+    {"load", load, METH_O, nullptr}, {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, nullptr}, {"current_stream", current_stream, METH_NOARGS, nullptr},
     ENTRY(bandit_select, 8), ENTRY(draft_stats, 9), ENTRY(verify, 12), ENTRY(bandit_update, 9), ENTRY(bandit_update_select, 13),
     ENTRY(shard_stats, 8), ENTRY(draft_stats_sharded, 11), ENTRY(verify_accept_sharded, 13), ENTRY(shard_final_sums, 6), ENTRY(shard_final_token, 14),
     ENTRY(mx4_quantize, 4), ENTRY(mx4_dequantize, 5), ENTRY(head_logits, 11), ENTRY(head_loss, 9), ENTRY(head_loss_grad, 13),
