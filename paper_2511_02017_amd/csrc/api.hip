@@ -27,7 +27,8 @@ struct tapout_ctx {
     uint32_t *flags_ws = nullptr;
     int32_t *arm_played = nullptr;                             // [max_batch]: the arms a round was drafted under (see draft_stats_impl)
     double *exp_table = nullptr;                               // 2^(k/256), k = 0..255, for the final-token passes
-    FilterRow *filter_rows = nullptr; FilterSlice *filter_slices = nullptr;       // tapout_sample: rows (max_k + 1 of a sequence) and their slices
+    FilterRow *filter_rows = nullptr; FilterSlice *filter_slices = nullptr;       // tapout_sample: rows (max_k + 1 of a sequence) and their slices,
+    CountSlice *filter_counts = nullptr;                       // and the counts of the parts of few rows
     int nsl_max = 0;                                           // final-token slices per row at cfg.vocab
     double *sum_r = nullptr, *sum_r2 = nullptr; int64_t *count = nullptr;   // bandit state [n_bandits, n_arms]
     // state of the stateful stop rules (allocated only when an arm needs it)
@@ -404,6 +405,7 @@ tapout_status tapout_create(tapout_ctx **out, const tapout_config *cfg)
         table[256 + 2 * idx + 1] = neg;
     }
     const size_t filter_n = (size_t)cfg->max_batch * (cfg->max_k + 1);
+    const size_t count_n = std::min(filter_n, (size_t)kCountRows) * kCountParts;
     bool ok = hipMalloc(&c->part, c->part_cap * sizeof(Partial)) == hipSuccess
            && hipMalloc(&c->part_t, c->part_cap * sizeof(Partial)) == hipSuccess
            && hipMalloc(&c->part1, nsums * sizeof(double)) == hipSuccess
@@ -414,6 +416,7 @@ tapout_status tapout_create(tapout_ctx **out, const tapout_config *cfg)
            && hipMalloc(&c->jobs, (size_t)cfg->max_batch * sizeof(JobRecord)) == hipSuccess
            && hipMalloc(&c->flags_ws, (size_t)cfg->max_batch * sizeof(uint32_t)) == hipSuccess
            && hipMalloc(&c->filter_rows, filter_n * kFilterRowBytes) == hipSuccess
+           && hipMalloc(&c->filter_counts, count_n * kCountSliceBytes) == hipSuccess
            && hipMalloc(&c->filter_slices, filter_n * filter_slices(cfg->vocab, TAPOUT_F32) * sizeof(FilterSlice)) == hipSuccess
            && hipMalloc(&c->arm_played, (size_t)cfg->max_batch * sizeof(int32_t)) == hipSuccess
            && hipMalloc(&c->sum_r, nstate * sizeof(double)) == hipSuccess
@@ -453,7 +456,7 @@ tapout_status tapout_destroy(tapout_ctx *ctx)
     profile_release(ctx);
     (void)hipFree(ctx->part); (void)hipFree(ctx->part_t); (void)hipFree(ctx->part1); (void)hipFree(ctx->part2);
     (void)hipFree(ctx->jobs); (void)hipFree(ctx->flags_ws); (void)hipFree(ctx->arm_played);
-    (void)hipFree(ctx->exp_table); (void)hipFree(ctx->sampled_lse); (void)hipFree(ctx->filter_rows); (void)hipFree(ctx->filter_slices);
+    (void)hipFree(ctx->exp_table); (void)hipFree(ctx->sampled_lse); (void)hipFree(ctx->filter_rows); (void)hipFree(ctx->filter_counts); (void)hipFree(ctx->filter_slices);
     (void)hipFree(ctx->sum_r); (void)hipFree(ctx->sum_r2); (void)hipFree(ctx->count);
     (void)hipFree(ctx->prev_entropy); (void)hipFree(ctx->accept_rate); (void)hipFree(ctx->lambda); (void)hipFree(ctx->round_entropy);
     delete ctx;
@@ -529,7 +532,7 @@ tapout_status tapout_sample(tapout_ctx *ctx, const tapout_logits *logits, int32_
     a.B = B; a.K = K; a.V = V; a.k_len = k_len;
     a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u;
     a.token = token; a.n_kept = n_kept; a.logq = logq; a.flags = flags; a.exp_table = ctx->exp_table;
-    a.rows = ctx->filter_rows; a.slices = ctx->filter_slices;
+    a.rows = ctx->filter_rows; a.slices = ctx->filter_slices; a.counts = ctx->filter_counts;
     if ((int64_t)B * K * filter_slices(V, logits->dtype) > INT32_MAX) return fail(ctx, TAPOUT_EUNSUPPORTED, "B * K * V beyond 2^31 slices");
     if (kept) { a.kept = (void *)kept->ptr; a.kept_dtype = kept->dtype; a.kept_stride_b = kept->stride_b; a.kept_stride_k = kept->stride_k; }
     const hipError_t e = launch_filtered_sample(a, logits->dtype, (hipStream_t)stream);

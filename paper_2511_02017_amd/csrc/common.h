@@ -338,11 +338,14 @@ struct FilterArgs {
     const double *exp_table;
     struct FilterRow *rows;       // [B * K]: what each keeps
     struct FilterSlice *slices;   // [B * K, filter_slices(V)]
+    struct CountSlice *counts;    // [B * K, count_parts(B * K, V)]
     int32_t shift;                // set by the launch
 };
 constexpr int kFilterRowBytes = 40;
 struct FilterSlice { uint64_t units; int32_t kept, pad; };      // of a row's slice: the kept weights, and how many
 int filter_slices(int V, int dtype);
+constexpr int kCountRows = 256, kCountParts = 8, kCountSliceBytes = 12056;       // rows whose counting may be divided, parts of a row
+int count_parts(int64_t rows, int V);
 hipError_t launch_filtered_sample(FilterArgs a, int dtype, hipStream_t st);
 
 constexpr int kSampleSlice = 2048;   // elements per slice of the final-token passes

@@ -77,15 +77,15 @@ __device__ __forceinline__ float below(float x)                                 
 constexpr int kAll = 0x7fffffff, kNone = (int)0x80000000u;       // of a value's elements (indices before a row are negative)
 __device__ __forceinline__ Bound shorter(Bound a, Bound b) { return a.x > b.x || (a.x == b.x && a.index < b.index) ? a : b; }
 
+constexpr int kHalfPlaces = (kPlaces + 1) / 2;
+
 struct Shared {
     double table[256];                         // 2^(k / 256)
-    union {
-        uint32_t counts[kEntries];
+    union {                                    // in turn
+        uint32_t counts[kEntries];             // bfloat16: of every value
+        uint64_t measures[kHalfPlaces];        // of two neighbouring places each
         uint64_t list[2 * kList];              // a place's elements, and their weights
-    };
-    union {
-        uint64_t units[kEntries];              // measures by entry
-        uint64_t bins[kBins];
+        uint64_t bins[kBins];                  // of a range of keys
     };
     uint64_t waves[2][kWaves];
     uint32_t turn[2][kLoads * kWaves];
@@ -156,26 +156,30 @@ template <int DT> struct RowReader {
 // -infinity.  A kernel runs through its code once, so code that is not there is what makes it short: the code of f is there LOADS + 1 times, and
 // what is done for a few of a row's elements is a loop.
 template <int DT, int LOADS, class F>
-__device__ __forceinline__ void each_vector(const RowReader<DT> &row, F f)
+__device__ __forceinline__ void each_vector(const RowReader<DT> &row, F f, int begin = 0, int end = 0x7fffffff)       // of vectors [begin, end)
 {
     constexpr int step = kThreads * LOADS;
-    const int from = row.before ? step : 0;                            // the first vector may be one in part
+    end = min(end, row.vecs);
     u32x4 w[LOADS], next[LOADS];
     auto load = [&](int base, u32x4 (&to)[LOADS]) {
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) to[u] = *(const u32x4 *)(row.base + (int64_t)(base + u * kThreads + threadIdx.x) * 16);
     };
-    auto whole = [&](int base) { return base >= from && base + step < row.vecs; };
-    if (whole(0)) load(0, w);
+    auto whole = [&](int base) { return (base > 0 || !row.before) && base + step <= end && base + step < row.vecs; };      // the row's first and last vector may be such in part
+    if (whole(begin)) load(begin, w);
 #pragma unroll 1
-    for (int base = 0; base < row.vecs; base += step) {
+    for (int base = begin; base < end; base += step) {
         if (whole(base + step)) load(base + step, next);
         if (whole(base)) {
 #pragma unroll
             for (int u = 0; u < LOADS; ++u) f(base + u * kThreads + (int)threadIdx.x, w[u]);
         } else {
+            const u32x4 masked = u32x4{1, 1, 1, 1} * (RowReader<DT>::n == 4 ? 0xff800000u : 0xff80ff80u);
 #pragma unroll 1
-            for (int t = base; t < min(base + step, row.vecs); t += kThreads) f(t + (int)threadIdx.x, row.load(t + (int)threadIdx.x));
+            for (int t = base; t < min(base + step, end); t += kThreads) {
+                const int v = t + (int)threadIdx.x;
+                f(v, v < end ? row.load(v) : masked);
+            }
         }
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) w[u] = next[u];
@@ -244,16 +248,16 @@ __device__ __forceinline__ uint64_t block_before(uint64_t v, uint64_t &all, Shar
 }
 
 // ---- the end of a run --------------------------------------------------------------------------------------------
-// Index of the r-th element (from 1) that equals x; r of them are there.
+// Index of the r-th element (from 1) that equals x among those of the vectors from `begin` on; r of them are there.
 template <int DT>
-__device__ __forceinline__ int nth_equal(const RowReader<DT> &row, float x, uint32_t r, Shared &sh)
+__device__ __forceinline__ int nth_equal(const RowReader<DT> &row, float x, uint32_t r, Shared &sh, int begin = 0)
 {
     constexpr int n = RowReader<DT>::n;
     static_assert(kLoads * kWaves == kWave, "a lane for each wavefront's part of a turn");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t seen = 0;
     int flip = 0;
-    for (int base = 0; base < row.vecs; base += kThreads * kLoads, flip ^= 1) {
+    for (int base = begin; base < row.vecs; base += kThreads * kLoads, flip ^= 1) {
         uint32_t equal = 0;                                    // a byte for each of the turns
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
@@ -335,7 +339,7 @@ struct Measure {
     __device__ __forceinline__ uint64_t of(float x, const double *table) const { return weights ? w.of(x, table) : 1; }
 };
 
-// The end of the shortest run of `within` whose measure reaches `target`, which ends in `place`, before which the measure is `above`.
+// The end of the shortest run of `within` whose measure reaches `target`, which ends in the pair `place` of places, before which the measure is `above`.
 template <int DT>
 __device__ __forceinline__ Bound end_in(const RowReader<DT> &row, Bound within, uint64_t target, int place, uint64_t above, const Measure &m, Shared &sh)
 {
@@ -354,7 +358,7 @@ __device__ __forceinline__ Bound end_in(const RowReader<DT> &row, Bound within, 
 #pragma unroll
             for (int e = 0; e < n; ++e) {
                 const uint32_t k = key_of(x[e]);
-                in |= ((by_key ? k >= lo && k <= hi : place_of(x[e]) == place) ? 1u : 0u) << e;
+                in |= ((by_key ? k >= lo && k <= hi : place_of(x[e]) >> 1 == place) ? 1u : 0u) << e;
             }
             if (__any(in != 0))
                 each_chosen<DT>(w, in, row.first(v), [&](float y, int j) {
@@ -447,8 +451,9 @@ struct Filters {
     float T, top_p, min_p; int top_k; bool greedy;
 };
 
-// Counts of a bfloat16 row's values.  sh.bad: a NaN or +infinity; sh.irregular: values beyond the table, or too many that are smaller than it.
-__device__ __forceinline__ void count_values(const RowReader<TAPOUT_BF16> &row, Shared &sh)
+// Counts of the values of a bfloat16 row's vectors [begin, end).  sh.bad: a NaN or +infinity; sh.irregular: values beyond the table, or too many that
+// are smaller than it.
+__device__ __forceinline__ void count_values(const RowReader<TAPOUT_BF16> &row, Shared &sh, int begin = 0, int end = 0x7fffffff)
 {
 #pragma unroll 1
     for (int k = threadIdx.x; k < kEntries; k += kThreads) sh.counts[k] = 0;
@@ -484,17 +489,63 @@ __device__ __forceinline__ void count_values(const RowReader<TAPOUT_BF16> &row, 
                     else sh.irregular = 1;
                 });
         }
-    });
+    }, begin, end);
     __syncthreads();
     if (threadIdx.x == 0) { sh.counts[0] += sh.counts[1]; sh.counts[1] = 0; sh.counts[kEntries - 1] = 0; }         // one place; the last are masked
     __syncthreads();
 }
 
+}  // namespace
+
+// Where rows are few each is counted in parts, by workgroups of their own, and a part's counts go through memory, in sixteen bits: a part has less than
+// 2^16 elements.
+struct CountSlice {
+    uint16_t counts[kEntries];
+    int32_t bad, irregular, tinies, pad;
+    float tiny[64];
+};
+static_assert(sizeof(CountSlice) == kCountSliceBytes, "the context makes room for them");
+
+namespace {
+
+__device__ __host__ __forceinline__ int part_vecs(int vecs, int parts) { return ((vecs + parts - 1) / parts + 63) & ~63; }
+
+__device__ __forceinline__ void load_counts(const CountSlice *parts, int n_parts, Shared &sh)
+{
+#pragma unroll 1
+    for (int k = threadIdx.x; k < kEntries / 2; k += kThreads) {
+        uint32_t lo = 0, hi = 0;
+#pragma unroll 4
+        for (int s = 0; s < n_parts; ++s) {
+            const uint32_t both = ((const uint32_t *)parts[s].counts)[k];
+            lo += both & 0xffffu;
+            hi += both >> 16;
+        }
+        sh.counts[2 * k] = lo;
+        sh.counts[2 * k + 1] = hi;
+    }
+    if (threadIdx.x < 64) {
+        int to = 0, bad = 0, irregular = 0;
+#pragma unroll 1
+        for (int s = 0; s < n_parts; ++s) {
+            const int n = uniform(parts[s].tinies);
+            if ((int)threadIdx.x < n && to + (int)threadIdx.x < 64) sh.tiny[to + threadIdx.x] = parts[s].tiny[threadIdx.x];
+            to += n;
+            bad |= parts[s].bad;
+            irregular |= parts[s].irregular;
+        }
+        if (threadIdx.x == 0) { sh.tinies = to; sh.bad = bad; sh.irregular = irregular | (to > 64 ? 1 : 0); }
+    }
+    __syncthreads();
+}
+
 // A bfloat16 row from its counts: its maximum, where its run ends and how many that keeps.  false: it was not decided here (not regular, without a
 // finite value (sh.bad), or its run ends among the small values).
-__device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, const Filters &f, int shift, float &peak, Weight &w, Bound &end, int &kept, Shared &sh)
+__device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, const Filters &f, int shift, const CountSlice *parts, int n_parts, float &peak,
+                                          Weight &w, Bound &end, int &kept, Shared &sh)
 {
-    count_values(row, sh);
+    if (n_parts) load_counts(parts, n_parts, sh);
+    else count_values(row, sh);
     if (uniform(sh.bad | sh.irregular)) return false;
     const int tinies = uniform(sh.tinies);
     const int p0 = threadIdx.x * kPer;
@@ -595,7 +646,18 @@ __device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, con
     const uint32_t here = (uint32_t)uniform((int)sh.counts[entry_at(place)]);
     if (n == 0) end = Bound{place == kTinyPlace ? __uint_as_float((kLow - 1) << 16) : value_at(place), kNone};
     else if ((uint32_t)n >= here) end = Bound{value_at(place), kAll};
-    else end = Bound{value_at(place), nth_equal<TAPOUT_BF16>(row, value_at(place), (uint32_t)n, sh)};
+    else {
+        // among its equals: with the parts' counts the part that the last one lies in
+        int begin = 0;
+        uint32_t r = (uint32_t)n;
+        for (int s = 0; s < n_parts; ++s) {
+            const uint32_t of_part = parts[s].counts[entry_at(place)];
+            if (of_part >= r) break;
+            r -= of_part;
+            begin += part_vecs(row.vecs, n_parts);
+        }
+        end = Bound{value_at(place), nth_equal<TAPOUT_BF16>(row, value_at(place), (uint32_t)uniform((int)r), sh, uniform(begin))};
+    }
     return true;
 }
 
@@ -636,22 +698,21 @@ __device__ __forceinline__ void by_places(const RowReader<DT> &row, const Filter
         const Bound within = end;
         __syncthreads();
 #pragma unroll 1
-        for (int k = threadIdx.x; k < kEntries; k += kThreads) sh.units[k] = 0;
+        for (int k = threadIdx.x; k < kHalfPlaces; k += kThreads) sh.measures[k] = 0;
         __syncthreads();
         each_element<DT, 1>(row, [&](float x, int j) {
-            if (within.holds(x, j)) atomicAdd((unsigned long long *)&sh.units[entry_of(x)], (unsigned long long)measure.of(x, sh.table));
+            if (within.holds(x, j)) atomicAdd((unsigned long long *)&sh.measures[place_of(x) >> 1], (unsigned long long)measure.of(x, sh.table));
         });
         __syncthreads();
-        if (threadIdx.x == 0) { sh.units[0] += sh.units[1]; sh.units[1] = 0; }
-        __syncthreads();
-        auto at = [&](int p) { return p < kPlaces ? sh.units[entry_at(p)] : 0; };
+        constexpr int per = (kHalfPlaces + kThreads - 1) / kThreads;
+        auto at = [&](int p) { return p < kHalfPlaces ? sh.measures[p] : 0; };
         uint64_t target = f.greedy ? 1 : f.top_k, all, above = 0;
         if (turn == 1) {
-            (void)block_before(sum_places(kPer, at), all, sh, 1);
+            (void)block_before(sum_places(per, at), all, sh, 1);
             const double reached = (double)f.top_p * (double)all;
             target = reached > 1.0 ? (uint64_t)ceil(reached) : 1;
         }
-        const int place = find_place(kPer, target, above, at, sh);
+        const int place = find_place(per, target, above, at, sh);
         if (place >= 0) end = end_in<DT>(row, within, target, place, above, measure, sh);
     }
     if (!f.greedy && f.min_p > 0.f) end = shorter(end, Bound{least_value(m, f.T, f.min_p), kAll});
@@ -681,8 +742,26 @@ static_assert(sizeof(FilterRow) == kFilterRowBytes, "the context makes room for 
 
 namespace {
 
+// A part of a bfloat16 row's values, counted.  Bound by the LDS, which adds one element a lane at a time.
+__global__ __launch_bounds__(kThreads, 8) void filter_counts_kernel(FilterArgs a, int parts)
+{
+    __shared__ Shared sh;
+    const int r = blockIdx.x / parts, s = blockIdx.x - r * parts, b = r / a.K, k = r - b * a.K;
+    if (a.k_len && k >= a.k_len[b]) return;
+    const RowReader<TAPOUT_BF16> row(row_address(a.base, TAPOUT_BF16, a.stride_b, a.stride_k, b, k), a.V);
+    if (threadIdx.x == 0) { sh.bad = 0; sh.irregular = 0; sh.tinies = 0; }
+    const int per = part_vecs(row.vecs, parts);
+    count_values(row, sh, s * per, (s + 1) * per);
+    CountSlice &to = a.counts[blockIdx.x];
+#pragma unroll 1
+    for (int q = threadIdx.x; q < kEntries / 2; q += kThreads) ((uint32_t *)to.counts)[q] = sh.counts[2 * q] | sh.counts[2 * q + 1] << 16;
+    if (threadIdx.x < 64) to.tiny[threadIdx.x] = sh.tiny[threadIdx.x];
+    if (threadIdx.x == 0) { to.bad = sh.bad; to.irregular = sh.irregular; to.tinies = min(sh.tinies, 64); }
+}
+
+// What every row keeps: a workgroup a row.
 template <int DT>
-__global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a)
+__global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a, int parts)
 {
     __shared__ Shared sh;
     const int r = blockIdx.x, b = r / a.K, k = r - b * a.K;
@@ -699,7 +778,7 @@ __global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a)
     int kept = -1;
     if (f.T == f.T) {
         bool done = false;
-        if constexpr (DT == TAPOUT_BF16) done = by_counts(row, f, a.shift, max, w, end, kept, sh);
+        if constexpr (DT == TAPOUT_BF16) done = by_counts(row, f, a.shift, a.counts + (int64_t)r * parts, parts, max, w, end, kept, sh);
         if (!done && !uniform(sh.bad)) {
             kept = -1;
             if constexpr (DT == TAPOUT_BF16) {
@@ -964,13 +1043,30 @@ hipError_t launch_filtered_sample(FilterArgs a, int dtype, hipStream_t st)
     const int slices = filter_slices(a.V, dtype);
     const auto launch = [&](auto elem) {
         constexpr int DT = decltype(elem)::value;
-        filter_rows_kernel<DT><<<rows, kThreads, 0, st>>>(a);
+        const int parts = DT == TAPOUT_BF16 ? count_parts(rows, a.V) : 0;
+        if constexpr (DT == TAPOUT_BF16)
+            if (parts) filter_counts_kernel<<<rows * parts, kThreads, 0, st>>>(a, parts);
+        filter_rows_kernel<DT><<<rows, kThreads, 0, st>>>(a, parts);
         filter_slices_kernel<DT><<<rows * slices, kSliceThreads, 0, st>>>(a, slices);
         if (a.u || a.n_kept || a.flags) filter_tokens_kernel<DT><<<rows, kSliceThreads, 0, st>>>(a, slices);
     };
     if (dtype == TAPOUT_F32) launch(std::integral_constant<int, TAPOUT_F32>{});
     else launch(std::integral_constant<int, TAPOUT_BF16>{});
     return hipGetLastError();
+}
+
+// Parts that a bfloat16 row's counting is divided into, 0: not.  Few rows leave most compute units idle: 64 rows of 128256 take 9.2 us for the counts of 4
+// parts each and 17.1 for the rest, 31.4 in one kernel.  Above a row to a compute unit what a second kernel reads again costs more: 576 rows take 39.9
+// and 52.8 us with 3 parts, 85.5 without.
+int count_parts(int64_t rows, int V)
+{
+    if (rows > kCountRows) return 0;
+    int parts = rows > 128 ? 2 : rows > 32 ? 4 : 8;
+    const int most = V / 8192;
+    parts = parts < most ? parts : most;
+    const int vecs = V / 8 + 2;
+    while (parts > 0 && parts <= kCountParts && (int64_t)part_vecs(vecs, parts) * 8 >= 65536) ++parts;
+    return parts < 2 || parts > kCountParts ? 0 : parts;
 }
 
 // Slices of a row: it may begin anywhere in its first vector.

@@ -281,3 +281,29 @@ def test_refusals():
     tp.close()
     with pytest.raises(binding.TapoutError, match="NULL"):
         tp.sample(x, u)
+
+
+@pytest.mark.parametrize("V", [16391, 70001, 131075, 262153, 540009])
+@pytest.mark.parametrize("before", [0, 3])
+def test_few_rows_with_what_matters_far_apart(V, before):
+    """Equal elements at which the run ends, and small values among zeros, from a row's start to its end; one bad value in its last part."""
+    wide = torch.full((8, 1, V + 16), 9.0, dtype=bf16)
+    x = wide[:, :, before:before + V]
+    x.fill_(-2.0)
+    x[:, :, 5::11] = 1.5
+    x[1, :, -9:] = 3.0
+    x[2] = 0.0
+    x[2, :, 3::V // 40] = 2.0 ** -20
+    x[3] = -INF
+    x[3, :, 1::V // 70] = 2.0 ** -30                               # too many of them, in all parts together
+    x[4, 0, -1] = 7.0
+    x[5, 0, -2] = NAN
+    x[6, 0, -1] = 300.0                                            # beyond what is counted
+    x[7] = -INF
+    n = V // 11
+    T, k, p, m = columns([(1.0, n - 7, 1.0, 0.0), (1.0, 0, 0.6, 0.0), (0.3, n, 0.7, 0.0), (1.0, 33, 0.9, 0.0), (0.0, 0, 1.0, 0.0), (1.0, 5, 1.0, 0.0),
+                          (200.0, n // 2, 1.0, 0.0), (1.0, 0, 1.0, 0.0)])
+    u = torch.rand(8, 1, generator=torch.Generator().manual_seed(V))
+    tp = binding.Tapout(8, 1, V)
+    got = run(tp, wide.to(DEV)[:, :, before:before + V], T, k, p, m, u, bf16)
+    check(x, got, bf16, T, k, p, m, u)
