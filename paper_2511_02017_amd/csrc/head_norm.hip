@@ -255,16 +255,22 @@ template <class E, int TPR, int VPT> hipError_t grad_with(const NormGradArgs &a,
     return hipGetLastError();
 }
 
-// Threads and vectors for a row of so many: a wavefront a row while four vectors a lane hold it, more threads for long rows.
-template <template <class, int, int> class F, class E, class A> hipError_t by_length(const A &a, hipStream_t st)
+// Threads and vectors for a row of so many vectors: a wavefront a row while two vectors a lane hold it, above that all threads of a workgroup, as few vectors
+// each as hold it.  Four vectors a lane of one wavefront (MORE) only where the columns' sums are kept through many rows, which wavefronts of their own
+// do without a barrier.  us for rows of 256 vectors (2048 bfloat16), one wavefront / 256 threads: 64 rows 4.9 / 3.8, 1024 rows 7.1 / 6.1, 8192 rows
+// 24.8 / 23.4; the gradient's 7.2 / 6.2, 10.0 / 11.2, 24.5 / 27.8.  128 vectors: 8192 rows 12.6 / 15.3.  512 vectors, 256 threads x 2 / 1024 x 1:
+// 64 rows 4.3 / 4.5, 8192 rows 47.0 / 58.8.  1024 vectors, 256 x 4 / 1024 x 1: 64 rows 5.2 / 4.8, 1024 rows 13.5 / 14.2, 8192 rows 104 / 103.
+template <template <class, int, int> class F, bool MORE, class E, class A> hipError_t by_length(const A &a, hipStream_t st)
 {
     const int vecs = a.D / Vec<E>::n;
     if (vecs <= 64) return F<E, 64, 1>::launch(a, st);
     if (vecs <= 128) return F<E, 64, 2>::launch(a, st);
-    if (vecs <= 256) return F<E, 64, 4>::launch(a, st);
+    if (vecs <= 256) return F<E, MORE ? 64 : 256, MORE ? 4 : 1>::launch(a, st);
     if (vecs <= 512) return F<E, 256, 2>::launch(a, st);
     if (vecs <= 1024) return F<E, 256, 4>::launch(a, st);
-    if (vecs <= 4096) return F<E, 1024, 4>::launch(a, st);
+    if (vecs <= 2048) return F<E, 1024, 2>::launch(a, st);
+    if constexpr (!MORE || sizeof(E) == 4)                     // the gradient's bfloat16 rows do not fit the registers by four
+        if (vecs <= 4096) return F<E, 1024, 4>::launch(a, st);
     if constexpr (sizeof(E) == 2) return F<E, 1024, 8>::launch(a, st);          // a row has 65536 elements at most
     else return F<E, 1024, 16>::launch(a, st);
 }
@@ -275,11 +281,11 @@ template <class E, int TPR, int VPT> struct NormGrad { static hipError_t launch(
 
 hipError_t launch_head_norm(const NormArgs &a, int dtype, hipStream_t st)
 {
-    return dtype == TAPOUT_F32 ? by_length<Norm, float>(a, st) : by_length<Norm, __bf16>(a, st);
+    return dtype == TAPOUT_F32 ? by_length<Norm, false, float>(a, st) : by_length<Norm, false, __bf16>(a, st);
 }
 hipError_t launch_head_norm_grad(const NormGradArgs &a, int dtype, hipStream_t st)
 {
-    return dtype == TAPOUT_F32 ? by_length<NormGrad, float>(a, st) : by_length<NormGrad, __bf16>(a, st);
+    return dtype == TAPOUT_F32 ? by_length<NormGrad, true, float>(a, st) : by_length<NormGrad, true, __bf16>(a, st);
 }
 
 }  // namespace tapout

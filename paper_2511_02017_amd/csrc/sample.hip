@@ -800,7 +800,7 @@ __global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a, int
 }
 
 // The vectors of a slice, and which of their elements are kept.
-constexpr int kSliceThreads = 256, kSliceTurns = 4, kSliceVecs = kSliceThreads * kSliceTurns;
+constexpr int kSliceThreads = 256, kSliceTurns = 2, kSliceVecs = kSliceThreads * kSliceTurns;
 template <int N> __device__ __forceinline__ void kept_of(const FilterRow &q, const float (&x)[N], int j0, bool (&in)[N])
 {
     const float than = j0 + N - 1 <= q.last ? q.from : q.above;
