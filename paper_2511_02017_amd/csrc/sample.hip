@@ -64,6 +64,16 @@ __device__ __forceinline__ uint32_t key_of(float x)             // ordered like 
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu)); }
 
+// Keys of a place's values.
+struct Keys { uint32_t lo, hi; };
+__device__ __forceinline__ Keys keys_of(int place)
+{
+    const int entry = entry_at(place), e = entry >> 1;
+    const uint32_t least = (kLow - 1 + (uint32_t)e) << 16, most = e == 0 ? (kLow << 16) - 1 : e > kRegular ? 0x7f7fffffu : least | 0xffffu;
+    if (e == 0) return Keys{~(most | 0x80000000u), most | 0x80000000u};
+    return entry & 1 ? Keys{~(most | 0x80000000u), ~(least | 0x80000000u)} : Keys{least | 0x80000000u, most | 0x80000000u};
+}
+
 // Last element of a run: larger values, and equal ones up to the index, are in it.
 struct Bound {
     float x; int32_t index;
@@ -339,13 +349,21 @@ struct Measure {
     __device__ __forceinline__ uint64_t of(float x, const double *table) const { return weights ? w.of(x, table) : 1; }
 };
 
-// The end of the shortest run of `within` whose measure reaches `target`, which ends in the pair `place` of places, before which the measure is `above`.
+// What top-p asks for of a mass: at least a unit.
+__device__ __forceinline__ uint64_t share_of(uint64_t all, float top_p)
+{
+    const double reached = (double)top_p * (double)all;
+    return reached > 1.0 ? (uint64_t)ceil(reached) : 1;
+}
+
+// The end of the shortest run of `within` whose measure reaches `target`, which ends among the keys of `range`, before which the measure is `above`.
+// top_p: `range` holds all of `within`, at most kList elements, and the target is this share of their weights.
 template <int DT>
-__device__ __forceinline__ Bound end_in(const RowReader<DT> &row, Bound within, uint64_t target, int place, uint64_t above, const Measure &m, Shared &sh)
+__device__ __forceinline__ Bound end_in(const RowReader<DT> &row, Bound within, uint64_t target, Keys range, uint64_t above, const Measure &m, Shared &sh,
+                                        float top_p = -1.f)
 {
     constexpr int n = RowReader<DT>::n;
-    uint32_t lo = 0, hi = 0;
-    bool by_key = false;
+    uint32_t lo = range.lo, hi = range.hi;
     for (;;) {
         __syncthreads();
         if (threadIdx.x == 0) { sh.count = 0; sh.lo = 0xffffffffu; sh.hi = 0; }
@@ -356,10 +374,7 @@ __device__ __forceinline__ Bound end_in(const RowReader<DT> &row, Bound within, 
             unpack<DT>(w, x);
             uint32_t in = 0;
 #pragma unroll
-            for (int e = 0; e < n; ++e) {
-                const uint32_t k = key_of(x[e]);
-                in |= ((by_key ? k >= lo && k <= hi : place_of(x[e]) >> 1 == place) ? 1u : 0u) << e;
-            }
+            for (int e = 0; e < n; ++e) in |= (key_of(x[e]) - lo <= hi - lo ? 1u : 0u) << e;
             if (__any(in != 0))
                 each_chosen<DT>(w, in, row.first(v), [&](float y, int j) {
                     if (!within.holds(y, j)) return;
@@ -378,6 +393,12 @@ __device__ __forceinline__ Bound end_in(const RowReader<DT> &row, Bound within, 
 #pragma unroll 1
             for (int i = threadIdx.x; i < count; i += kThreads) sh.list[kList + i] = m.of(value_of((uint32_t)(sh.list[i] >> 32)), sh.table);
             __syncthreads();
+            if (top_p >= 0.f) {
+                static_assert(kList <= kThreads, "an element a thread");
+                uint64_t all;
+                (void)block_before((int)threadIdx.x < count ? sh.list[kList + threadIdx.x] : 0, all, sh, 0);
+                target = share_of(all, top_p);
+            }
 #pragma unroll 1
             for (int i = threadIdx.x; i < count; i += kThreads) {
                 const uint64_t me = sh.list[i], own = sh.list[kList + i];
@@ -407,7 +428,6 @@ __device__ __forceinline__ Bound end_in(const RowReader<DT> &row, Bound within, 
             if (k >= lo && k <= hi && within.holds(x, j)) atomicAdd((unsigned long long *)&sh.bins[(hi - k) >> shift], (unsigned long long)m.of(x, sh.table));
         });
         const int b = find_place(kBins / kThreads, target, above, [&](int k) { return sh.bins[k]; }, sh);
-        by_key = true;
         const uint32_t top = hi - ((uint32_t)b << shift);
         lo = max(lo, top - min(top, (1u << shift) - 1));
         hi = top;
@@ -609,8 +629,7 @@ __device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, con
     }
     if (!f.greedy && f.top_p < 1.f) {
         before = block_before(own, all, sh, 1);
-        const double reached = (double)f.top_p * (double)all;
-        const uint64_t target = reached > 1.0 ? (uint64_t)ceil(reached) : 1;
+        const uint64_t target = share_of(all, f.top_p);
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             if (before < target && before + mass[k] >= target) {                           // one thread
@@ -665,13 +684,20 @@ __device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, con
 template <int DT>
 __device__ __forceinline__ void by_places(const RowReader<DT> &row, const Filters &f, int shift, float &peak, Weight &w, Bound &end, Shared &sh)
 {
+    const bool by_rank = !f.greedy && f.top_k > 0 && f.top_k < row.V;
     __syncthreads();
     if (threadIdx.x == 0) sh.bad = 0;
+    if (by_rank) {
+#pragma unroll 1
+        for (int k = threadIdx.x; k < kPlaces; k += kThreads) sh.counts[k] = 0;
+    }
+    __syncthreads();
     float m = -INFINITY;
     bool nan = false;
     each_element<DT, 4>(row, [&](float x, int) {
         m = fmaxf(m, x);
         nan |= x != x;
+        if (by_rank && x > -INFINITY) atomicAdd(&sh.counts[place_of(x)], 1u);
     });
     m = lanes_max(m, 0, 6);
     if ((threadIdx.x & 63) == 0) sh.waves_f[threadIdx.x >> 6] = m;
@@ -691,31 +717,46 @@ __device__ __forceinline__ void by_places(const RowReader<DT> &row, const Filter
         return;
     }
     w = Weight{(double)m, f.greedy ? 0.0 : 256.0 / ((double)f.T * kLn2), shift};
+    if (f.greedy) {
+        end = Bound{m, nth_equal<DT>(row, m, 1, sh)};
+        return;
+    }
+    const bool by_mass = f.top_p < 1.f;
+    bool few = false;                                          // the run's elements fit the list
 #pragma unroll 1
-    for (int turn = 0; turn < 2; ++turn) {                     // top-k (greedy: the first one), then top-p of what that leaves
-        if (turn == 0 ? !f.greedy && (f.top_k <= 0 || f.top_k >= row.V) : f.greedy || !(f.top_p < 1.f)) continue;
+    for (int turn = 0; turn < 2; ++turn) {                     // top-k, then top-p of what that leaves
+        if (!(turn ? by_mass : by_rank)) continue;
         const Measure measure{turn == 1, w};
         const Bound within = end;
-        __syncthreads();
+        uint64_t target = f.top_k, above = 0;
+        Keys range{key_of(within.x), 0xff7fffffu};
+        if (turn == 0) {
+            const int place = find_place(kPer, target, above, [&](int p) { return p < kPlaces ? (uint64_t)sh.counts[p] : 0; }, sh);
+            if (place < 0) continue;
+            range = keys_of(place);
+            few = f.top_k <= kList;
+        } else if (!few) {
+            __syncthreads();
 #pragma unroll 1
-        for (int k = threadIdx.x; k < kHalfPlaces; k += kThreads) sh.measures[k] = 0;
-        __syncthreads();
-        each_element<DT, 1>(row, [&](float x, int j) {
-            if (within.holds(x, j)) atomicAdd((unsigned long long *)&sh.measures[place_of(x) >> 1], (unsigned long long)measure.of(x, sh.table));
-        });
-        __syncthreads();
-        constexpr int per = (kHalfPlaces + kThreads - 1) / kThreads;
-        auto at = [&](int p) { return p < kHalfPlaces ? sh.measures[p] : 0; };
-        uint64_t target = f.greedy ? 1 : f.top_k, all, above = 0;
-        if (turn == 1) {
+            for (int k = threadIdx.x; k < kHalfPlaces; k += kThreads) sh.measures[k] = 0;
+            __syncthreads();
+            each_element<DT, 1>(row, [&](float x, int j) {
+                if (within.holds(x, j)) atomicAdd((unsigned long long *)&sh.measures[place_of(x) >> 1], (unsigned long long)w.of(x, sh.table));
+            });
+            __syncthreads();
+            constexpr int per = (kHalfPlaces + kThreads - 1) / kThreads;
+            auto at = [&](int p) { return p < kHalfPlaces ? sh.measures[p] : 0; };
+            uint64_t all;
             (void)block_before(sum_places(per, at), all, sh, 1);
-            const double reached = (double)f.top_p * (double)all;
-            target = reached > 1.0 ? (uint64_t)ceil(reached) : 1;
+            target = share_of(all, f.top_p);
+            const int place = find_place(per, target, above, at, sh);
+            if (place < 0) continue;
+            range = Keys{keys_of(2 * place + 1).lo, keys_of(2 * place).hi};
         }
-        const int place = find_place(per, target, above, at, sh);
-        if (place >= 0) end = end_in<DT>(row, within, target, place, above, measure, sh);
+        end = end_in<DT>(row, within, target, Keys{(uint32_t)uniform((int)range.lo), (uint32_t)uniform((int)range.hi)}, above, measure, sh,
+                         turn && few ? fmaxf(f.top_p, 0.f) : -1.f);
     }
-    if (!f.greedy && f.min_p > 0.f) end = shorter(end, Bound{least_value(m, f.T, f.min_p), kAll});
+    if (f.min_p > 0.f) end = shorter(end, Bound{least_value(m, f.T, f.min_p), kAll});
 }
 
 // What by_places decides about a bfloat16 row, out of the way of those that are decided by their counts.
