@@ -275,7 +275,7 @@ TAPOUT_API tapout_status tapout_draft_stats(tapout_ctx *ctx, const tapout_logits
  * token    [B,K] i32, with u;  logq [B,K] f32 or NULL
  * n_kept   [B,K] i32 or NULL: tokens that are kept
  * kept     [B,K,V] logits, binary32 or bfloat16 at any element-aligned address and
- *          strides, or NULL
+ *          strides, in memory of their own (not that of logits), or NULL
  * flags    [B] u32 or NULL (overwritten): BAD_ROW, a row that holds a NaN or has no
  *          finite maximum, or whose temperature is NaN: token -1, logq NaN, nothing
  *          kept
@@ -798,7 +798,9 @@ TAPOUT_API tapout_status tapout_fp8_dequantize(const uint8_t *codes, const float
  * Draft logits under a head held in 8 bits:
  *   out[b,k,v] = sum over blocks of 128 d: sa[b,k,block] sw[v / 128,block]
  *                sum_d qa[b,k,d] qw[v,d]
- * summed in binary32 and rounded once.  For heads of either type.
+ * summed in binary32 and rounded once.  For heads of either type.  out binary32:
+ * every product of codes is exact.  out bfloat16: within a block of 128, products
+ * may be off by 2^-16 of the largest one.
  *   hidden   [B,K,dim], quantised here with a scale for 128 elements of a row; or
  *            NULL with act_codes [B*K, P], act_scales [B*K, P / 128] as
  *            tapout_head_norm writes them

@@ -526,6 +526,7 @@ tapout_status tapout_sample(tapout_ctx *ctx, const tapout_logits *logits, int32_
     if (!u && (token || logq)) return fail(ctx, TAPOUT_EINVAL, "token and logq need u");
     if (!u && !kept && !n_kept) return fail(ctx, TAPOUT_EINVAL, "nothing to be written: neither u nor kept nor n_kept is given");
     if (kept && rows_overlap(kept, B, K, V)) return fail(ctx, TAPOUT_EINVAL, "kept: rows overlap");
+    if (kept && kept->ptr == logits->ptr) return fail(ctx, TAPOUT_EINVAL, "kept is the memory of logits, which are read again");
     DeviceGuard guard(ctx->cfg.device);
     FilterArgs a{};
     a.base = logits->ptr; a.stride_b = logits->stride_b; a.stride_k = logits->stride_k;
@@ -533,7 +534,9 @@ tapout_status tapout_sample(tapout_ctx *ctx, const tapout_logits *logits, int32_
     a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u;
     a.token = token; a.n_kept = n_kept; a.logq = logq; a.flags = flags; a.exp_table = ctx->exp_table;
     a.rows = ctx->filter_rows; a.slices = ctx->filter_slices; a.counts = ctx->filter_counts;
-    if ((int64_t)B * K * filter_slices(V, logits->dtype) > INT32_MAX) return fail(ctx, TAPOUT_EUNSUPPORTED, "B * K * V beyond 2^31 slices");
+    // a launch has less than 2^32 threads: 256 a slice, 1024 a row
+    if ((int64_t)B * K * filter_slices(V, logits->dtype) >= 1 << 24 || (int64_t)B * K >= 1 << 22)
+        return fail(ctx, TAPOUT_EUNSUPPORTED, "B * K = %lld rows beyond 2^22 or 2^24 slices", (long long)B * K);
     if (kept) { a.kept = (void *)kept->ptr; a.kept_dtype = kept->dtype; a.kept_stride_b = kept->stride_b; a.kept_stride_k = kept->stride_k; }
     const hipError_t e = launch_filtered_sample(a, logits->dtype, (hipStream_t)stream);
     return e == hipSuccess ? TAPOUT_OK : hip_fail(ctx, e, "sample");

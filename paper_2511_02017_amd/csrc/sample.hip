@@ -694,7 +694,7 @@ __device__ __forceinline__ void by_places(const RowReader<DT> &row, const Filter
     __syncthreads();
     float m = -INFINITY;
     bool nan = false;
-    each_element<DT, 4>(row, [&](float x, int) {
+    each_element<DT, DT == TAPOUT_F32 ? 4 : 2>(row, [&](float x, int) {
         m = fmaxf(m, x);
         nan |= x != x;
         if (by_rank && x > -INFINITY) atomicAdd(&sh.counts[place_of(x)], 1u);
@@ -759,15 +759,6 @@ __device__ __forceinline__ void by_places(const RowReader<DT> &row, const Filter
     if (f.min_p > 0.f) end = shorter(end, Bound{least_value(m, f.T, f.min_p), kAll});
 }
 
-// What by_places decides about a bfloat16 row, out of the way of those that are decided by their counts.
-struct Decision { float peak; Weight w; Bound end; };
-__device__ __attribute__((noinline)) Decision any_bf16_row(const void *p, int V, Filters f, int shift, Shared *sh)
-{
-    Decision d{0.f, {0.0, 0.0, shift}, {INFINITY, kNone}};
-    by_places<TAPOUT_BF16>(RowReader<TAPOUT_BF16>(p, V), f, shift, d.peak, d.w, d.end, *sh);
-    return d;
-}
-
 // ---- kernels -----------------------------------------------------------------------------------------------------
 }  // namespace
 
@@ -800,7 +791,9 @@ __global__ __launch_bounds__(kThreads, 8) void filter_counts_kernel(FilterArgs a
     if (threadIdx.x == 0) { to.bad = sh.bad; to.irregular = sh.irregular; to.tinies = min(sh.tinies, 64); }
 }
 
-// What every row keeps: a workgroup a row.
+// What every row keeps: a workgroup a row.  Bound by latency where rows are few (a pass over a row by one unit, and the barriers between what follows it:
+// one row of 32000 binary32 15.5 us, two passes; 120 rows of 50257 47.5 us, up to three passes and a double exponential for each element where top-p
+// alone is asked for), and by the LDS and the vector unit where they are many (576 rows of 128256 bfloat16 86 us, 1.7 TB/s: 2.25 rows a unit, paid as three).
 template <int DT>
 __global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a, int parts)
 {
@@ -822,12 +815,7 @@ __global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a, int
         if constexpr (DT == TAPOUT_BF16) done = by_counts(row, f, a.shift, a.counts + (int64_t)r * parts, parts, max, w, end, kept, sh);
         if (!done && !uniform(sh.bad)) {
             kept = -1;
-            if constexpr (DT == TAPOUT_BF16) {
-                const Decision d = any_bf16_row(row.base + row.before * Elem<DT>::size, a.V, f, a.shift, &sh);
-                max = d.peak; w = d.w; end = d.end;
-            } else {
-                by_places<DT>(row, f, a.shift, max, w, end, sh);
-            }
+            by_places<DT>(row, f, a.shift, max, w, end, sh);
         }
     }
     __syncthreads();
@@ -859,7 +847,8 @@ __device__ __forceinline__ FilterRow row_record(const FilterArgs &a, int r)
     q.last = uniform(q.last); q.kept = uniform(q.kept); q.bad = uniform(q.bad); q.c = uniform(q.c);
     return q;
 }
-// Units of a vector's kept elements: all of its elements in turn where most lanes keep some, else those that are kept.
+// Units of a vector's kept elements: all of its elements in turn where most lanes keep some, else those that are kept (64 rows of 128256 with different
+// filters, slices and tokens, us always all / always those kept / by more than 40 lanes: 14.0 + 9.4 / 14.4 + 10.8 / 13.3 + 9.3).
 template <int DT> __device__ __forceinline__ uint64_t kept_units(const Weight &w, const u32x4 &words, uint32_t keeps, int j0, const double *table)
 {
     uint64_t sum = 0;
@@ -878,7 +867,9 @@ template <int DT> __device__ __forceinline__ uint64_t kept_units(const Weight &w
     return sum;
 }
 
-// The filtered logits, and a slice's kept elements and weights: a workgroup a slice, all of its loads requested first.
+// The filtered logits, and a slice's kept elements and weights: a workgroup a slice, all of its loads requested first.  Bound by memory where rows are
+// many: 576 rows of 128256 bfloat16, read and written, 46 us, 6.4 TB/s.  Slices of 256 vectors a turn, us with 1 / 2 / 4 / 8 turns: 66.9 / 46.1 /
+// 49.0 / 50.0, 64 such rows with tokens (both kernels) 20.7 / 19.7 / 22.6 / 29.5, one row of 32000 binary32 9.2 / 9.7 / 12.0 / 15.5.
 template <int DT>
 __global__ __launch_bounds__(kSliceThreads) void filter_slices_kernel(FilterArgs a, int slices)
 {
@@ -949,7 +940,8 @@ __global__ __launch_bounds__(kSliceThreads) void filter_slices_kernel(FilterArgs
     if (threadIdx.x == 0) a.slices[blockIdx.x] = FilterSlice{sums[0] + sums[1] + sums[2] + sums[3], counts[0] + counts[1] + counts[2] + counts[3], 0};
 }
 
-// How many a row keeps, the flags of its sequence, and its token: the slice that holds it, then the vector, then the element.  A workgroup a row.
+// How many a row keeps, the flags of its sequence, and its token: the slice that holds it, then the vector, then the element.  A workgroup a row;
+// bound by latency, three dependent reads (5 to 8 us).
 template <int DT>
 __global__ __launch_bounds__(kSliceThreads) void filter_tokens_kernel(FilterArgs a, int slices)
 {

@@ -307,3 +307,14 @@ def test_few_rows_with_what_matters_far_apart(V, before):
     tp = binding.Tapout(8, 1, V)
     got = run(tp, wide.to(DEV)[:, :, before:before + V], T, k, p, m, u, bf16)
     check(x, got, bf16, T, k, p, m, u)
+
+
+def test_kept_logits_are_not_written_over_the_logits():
+    x = torch.zeros(2, 1, 64, device=DEV)
+    with pytest.raises(binding.TapoutError, match="memory of logits"):
+        binding.Tapout(2, 1, 64).sample(x, out=dict(kept=x))
+    both = torch.randn(2, 1, 2, 64, device=DEV)                       # side by side they may lie
+    r = binding.Tapout(2, 1, 64).sample(both[:, :, 0], out=dict(kept=both[:, :, 1], n_kept=torch.empty(2, 1, dtype=i32, device=DEV)))
+    torch.cuda.synchronize()
+    z = both[:, :, 0] - both[:, :, 0].amax(-1, keepdim=True)
+    assert torch.equal(r["kept"], z) and bool((r["n_kept"] == 64).all())
