@@ -792,8 +792,9 @@ __global__ __launch_bounds__(kThreads, 8) void filter_counts_kernel(FilterArgs a
 }
 
 // What every row keeps: a workgroup a row.  Bound by latency where rows are few (a pass over a row by one unit, and the barriers between what follows it:
-// one row of 32000 binary32 15.5 us, two passes; 120 rows of 50257 47.5 us, up to three passes and a double exponential for each element where top-p
-// alone is asked for), and by the LDS and the vector unit where they are many (576 rows of 128256 bfloat16 86 us, 1.7 TB/s: 2.25 rows a unit, paid as three).
+// one row of 32000 binary32 15.0 us, two passes; 120 rows of 50257 47.5 us, up to three passes and a double exponential for each element where top-p
+// alone is asked for), and where they are many by what one workgroup of 128 registers a unit has under way (576 rows of 128256 bfloat16 86 us,
+// 1.7 TB/s: 2.25 rows a unit, paid as three, LDS 21 % busy; held to 64 registers, two workgroups a unit: 85.5, with spills).
 template <int DT>
 __global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a, int parts)
 {
