@@ -39,8 +39,7 @@ struct LossArgs {
     const float *logits, *teacher_lse;          // the teacher's: [N, T]; [N] or NULL
     float *top;                  // [N, T]
 };
-hipError_t launch_listed_logits(const LossArgs &a, int dtype, hipStream_t st);      // top
-hipError_t launch_listed_join(const LossArgs &a, int blocks, hipStream_t st);       // the rest of it
+hipError_t launch_listed_join(const LossArgs &a, int blocks, int dtype, hipStream_t st);       // top, and from it and `part` the rest
 hipError_t launch_head_loss(const LossArgs &a, int dtype, hipStream_t st);
 
 // One piece of the vocabulary, rows [v0, v0 + n): its gradient by the logits, both ways round.

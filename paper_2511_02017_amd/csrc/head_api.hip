@@ -135,10 +135,6 @@ tapout_status run_loss(tapout_head *h, const tapout_logits *hidden, const tapout
     a.weight = Operand{weight->ptr, weight->stride * esz, V, h->cfg.dim * esz, nullptr, 0};
     a.N = B * K; a.V = V; a.D = h->cfg.dim; a.rows_per_seq = K; a.B = B;
     a.part = h->part; a.part_cap = (int64_t)h->part_cap; a.target_logit = h->target_logit;
-    if (a.ids) {
-        e = launch_listed_logits(a, h->cfg.dtype, st);
-        if (e != hipSuccess) return hip_fail(h, e, "lists");
-    }
     e = launch_head_loss(a, h->cfg.dtype, st);
     return e == hipSuccess ? TAPOUT_OK : hip_fail(h, e, what);
 }

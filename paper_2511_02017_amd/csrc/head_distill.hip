@@ -30,13 +30,11 @@ template <class E> __device__ __forceinline__ float dot16(u32x4 a, u32x4 b, floa
     return s;
 }
 
-// A workgroup a row, a wavefront eight listed tokens at a time, whose weights it reads side by side.  Bound by what the caches deliver: 8192 rows of 64
-// tokens, dim = 2048, bfloat16, 265 us, 8.1 TB/s, a twelfth of the loss's product.
-template <class E>
-__global__ __launch_bounds__(256) void listed_logits_kernel(LossArgs a)
+// By a workgroup, a wavefront eight listed tokens at a time, whose weights it reads side by side.
+template <class E> __device__ __forceinline__ void listed_logits(const LossArgs &a, int row)
 {
     constexpr int U = 8, n = 16 / (int)sizeof(E);
-    const int row = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const E *h = (const E *)((const char *)a.hidden.p + (int64_t)row * a.hidden.stride);
     const int32_t *ids = a.ids + (int64_t)row * a.T;
     for (int k0 = wave * U; k0 < a.T; k0 += 4 * U) {
@@ -105,12 +103,16 @@ struct Teacher {
     __device__ __forceinline__ bool counts() const { return listed > 0 && !bad_token && mass < (double)INFINITY; }
 };
 
-// A workgroup a row: lse from the blocks of the vocabulary, then its first wavefront the list (8192 rows of 2004 blocks and 64 tokens 31 us).
+// A workgroup a row: the listed logits, lse from the blocks of the vocabulary, then its first wavefront the list.  Bound by what the caches deliver of the
+// listed tokens' weights: 8192 rows of 64, dim = 2048, bfloat16, 260 us, 8.3 TB/s, a twelfth of the loss's product (with a launch of their own for the
+// logits 293; 40 rows of 16, dim = 1024, binary32 10.1 us, with two launches 12.4 and the gap between them).
+template <class E>
 __global__ __launch_bounds__(256) void listed_join_kernel(LossArgs a, int blocks)
 {
     __shared__ float maxima[4];
     __shared__ double sums[4];
     const int n = blockIdx.x;
+    listed_logits<E>(a, n);                                    // in memory for the first wavefront behind the barriers of the sums
     const double lse = join_lse(a.part + (int64_t)n * blocks, blocks, maxima, sums);
     if (threadIdx.x >= 64) return;
     const int32_t *ids = a.ids + (int64_t)n * a.T;
@@ -189,16 +191,10 @@ __global__ __launch_bounds__(64) void listed_grad_kernel(ListedArgs a, GradArgs 
 
 }  // namespace
 
-hipError_t launch_listed_logits(const LossArgs &a, int dtype, hipStream_t st)
+hipError_t launch_listed_join(const LossArgs &a, int blocks, int dtype, hipStream_t st)
 {
-    if (dtype == TAPOUT_F32) listed_logits_kernel<float><<<a.N, 256, 0, st>>>(a);
-    else listed_logits_kernel<__bf16><<<a.N, 256, 0, st>>>(a);
-    return hipGetLastError();
-}
-
-hipError_t launch_listed_join(const LossArgs &a, int blocks, hipStream_t st)
-{
-    listed_join_kernel<<<a.N, 256, 0, st>>>(a, blocks);
+    if (dtype == TAPOUT_F32) listed_join_kernel<float><<<a.N, 256, 0, st>>>(a, blocks);
+    else listed_join_kernel<__bf16><<<a.N, 256, 0, st>>>(a, blocks);
     return hipGetLastError();
 }
 

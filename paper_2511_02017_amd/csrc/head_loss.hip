@@ -283,7 +283,7 @@ template <class T> hipError_t loss_with(const LossArgs &a, hipStream_t st)
         head_loss_kernel<T><<<grid_of<T>((int64_t)ni * nj), T::threads, T::ring_bytes, st>>>(a, ni, nj, stages);
     });
     if (e != hipSuccess) return e;
-    if (a.ids) return launch_listed_join(a, ni * T::WI, st);
+    if (a.ids) return launch_listed_join(a, ni * T::WI, T::esz == 4 ? TAPOUT_F32 : TAPOUT_BF16, st);
     head_loss_join_kernel<<<a.N, 256, 0, st>>>(a, ni * T::WI);
     return hipGetLastError();
 }
