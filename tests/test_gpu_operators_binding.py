@@ -1,0 +1,59 @@
+"""The norm, 8-bit, sampling and distillation calls with tensors taken apart in Python give what the native part of the binding gives, and refuse the same."""
+import pytest
+import torch
+
+from paper_2511_02017_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+f32, bf16, i32 = torch.float32, torch.bfloat16, torch.int32
+
+
+def rand(*shape, seed, dtype=f32):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(dtype).to(DEV)
+
+
+def every_call(dtype, stream=None):
+    B, K, V, D, T = 3, 2, 515, 96, 7
+    kw = dict(stream=stream)
+    head, tp = binding.DraftHead(B * K, D, V, dtype=dtype, training=True), binding.Tapout(B, K, V)
+    x, res, g, w, m = (rand(*s, seed=i, dtype=dtype) for i, s in enumerate([(B, K, D), (B, K, D), (B, K, D), (D,), (V, D)]))
+    out = {}
+    c, s = binding.fp8_quantize(m, 128, **kw)
+    out.update(c=c, s=s, values=binding.fp8_dequantize(c, s, D, 128, dtype, **kw))
+    f = head.norm(x, w, residual=res, **kw)
+    q = head.norm(x, w, residual=res, fp8=True, **kw)
+    out.update(sum=f["sum"], y=f["out"], rstd=f["rstd"], codes=q["codes"], scales=q["scales"], back=binding.fp8_dequantize(q["codes"], q["scales"], D, 1, dtype, **kw))
+    out.update({"n" + k: v for k, v in head.norm_grad(g, f["sum"], w, f["rstd"], grad_sum=x, **kw).items()})
+    z = head.logits_fp8(x, c, s, dtype=f32, **kw)
+    out.update(z=z, zq=head.logits_fp8(q["codes"], c, s, act_scales=q["scales"], **kw))
+    u = torch.rand(B, K, generator=torch.Generator().manual_seed(9)).to(DEV)
+    T_, k, p, least = torch.full((B,), 0.9, device=DEV), torch.full((B,), 50, dtype=i32, device=DEV), torch.full((B,), 0.8, device=DEV), torch.full((B,), 0.01, device=DEV)
+    out.update(tp.sample(z, u, temperature=T_, top_k=k, top_p=p, min_p=least, k_len=torch.full((B,), K, dtype=i32, device=DEV), kept=bf16, **kw))
+    ids = torch.arange(B * K * T, device=DEV, dtype=i32).view(B, K, T)
+    d = head.distill(x, m, ids, rand(B, K, T, seed=11), **kw)
+    out.update({"d" + k: v for k, v in d.items()})
+    out.update(head.distill_grad(x, m, ids, rand(B, K, T, seed=11), d["lse"], d["top"], row_weight=torch.ones(B, K, device=DEV),
+                                 scale=torch.ones(1, device=DEV), **kw))
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("dtype", [f32, bf16])
+def test_without_the_native_part(dtype, monkeypatch):
+    binding.load_library()
+    want = every_call(dtype)
+    monkeypatch.setattr(binding, "_fast", binding._PythonOnly())
+    for stream in (None, torch.cuda.Stream()):
+        got = every_call(dtype, stream)
+        assert got.keys() == want.keys()
+        for k in want:
+            assert torch.equal(got[k].contiguous().view(torch.uint8), want[k].contiguous().view(torch.uint8)), (k, stream)
+    x = rand(2, 1, 64, seed=1)
+    tp = binding.Tapout(2, 1, 64)
+    with pytest.raises(binding.TapoutError, match="memory of logits"):
+        tp.sample(x, out=dict(kept=x))
+    with pytest.raises(ValueError):
+        tp.sample(x, temperature=torch.ones(3, device=DEV))
+    with pytest.raises(ValueError):
+        binding.DraftHead(2, 64, 8, dtype=f32).norm(x, torch.ones(32, device=DEV))
