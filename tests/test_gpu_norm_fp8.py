@@ -435,3 +435,24 @@ def test_refusals():
         head.norm(x, w)
     with pytest.raises(binding.TapoutError, match="NULL"):
         head.logits_fp8(x, c, s)
+
+
+def test_norm_rows_beyond_32_bits_of_offsets():
+    """The rows that lie behind 2^31 and 2^32 elements, and the first, forth and back."""
+    N, D = 2 ** 19 + 3, 8192
+    head = binding.DraftHead(N, D, 1, training=True)
+    x = torch.randn(N, 1, D, device=DEV, dtype=bf16)
+    w = rand(D, seed=1, dtype=bf16).to(DEV)
+    f = head.norm(x, w)
+    q = head.norm(x, w, fp8=True)
+    small = binding.DraftHead(8, D, 1, training=True)
+    at = torch.tensor([0, 2 ** 18 - 1, 2 ** 18, 2 ** 18 + 1, 2 ** 19 - 1, 2 ** 19, N - 1], device=DEV)
+    some = x[at].contiguous()
+    want, wq = small.norm(some, w), small.norm(some, w, fp8=True)
+    assert torch.equal(f["out"][at], want["out"]) and torch.equal(f["rstd"][at], want["rstd"])
+    assert torch.equal(q["codes"][at], wq["codes"]) and torch.equal(q["scales"][at], wq["scales"])
+    del q
+    g = head.norm_grad(f["out"], x, w, f["rstd"], out=dict(grad_x=f["out"], grad_weight=torch.empty(D, dtype=bf16, device=DEV)))
+    back = small.norm_grad(want["out"], some, w, want["rstd"])
+    torch.cuda.synchronize()
+    assert torch.equal(g["grad_x"][at], back["grad_x"])

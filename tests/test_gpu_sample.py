@@ -318,3 +318,26 @@ def test_kept_logits_are_not_written_over_the_logits():
     torch.cuda.synchronize()
     z = both[:, :, 0] - both[:, :, 0].amax(-1, keepdim=True)
     assert torch.equal(r["kept"], z) and bool((r["n_kept"] == 64).all())
+
+
+@pytest.mark.parametrize("dtype", [f32, bf16])
+def test_rows_beyond_32_bits_of_offsets(dtype):
+    """300 rows of which the last begin more than 2^32 elements behind the first."""
+    B, V, apart = 300, 9001, 2 ** 24
+    flat = torch.empty((B - 1) * apart + V, dtype=dtype, device=DEV)
+    x = flat.as_strided((B, 1, V), (apart, V, 1))
+    data = rows(B, 1, V, dtype, seed=2)
+    for b in range(B):
+        x[b].copy_(data[b])
+    kept = torch.empty((B - 1) * apart + V, dtype=bf16, device=DEV).as_strided((B, 1, V), (apart, V, 1))
+    T, k, p, m = (t.repeat(B // len(FILTERS) + 1)[:B] for t in columns(FILTERS))
+    u = torch.rand(B, 1, generator=torch.Generator().manual_seed(3))
+    tp = binding.Tapout(B, 1, V)
+    out = dict(token=torch.empty(B, 1, dtype=i32, device=DEV), logq=torch.empty(B, 1, device=DEV), n_kept=torch.empty(B, 1, dtype=i32, device=DEV),
+               flags=torch.empty(B, dtype=i32, device=DEV), kept=kept)
+    d = lambda t: t.to(DEV)                                                               # noqa: E731
+    tp.sample(x, d(u), temperature=d(T), top_k=d(k), top_p=d(p), min_p=d(m), out=out)
+    torch.cuda.synchronize()
+    got = {n: t.cpu() for n, t in out.items() if n != "kept"}
+    got["kept"] = torch.stack([kept[b].cpu() for b in range(B)])
+    check(data, got, bf16, T, k, p, m, u)
