@@ -64,12 +64,13 @@ __device__ __forceinline__ uint32_t key_of(float x)             // ordered like 
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu)); }
 
-// Keys of a place's values.
+// Keys of a place's values.  The place behind kTinyPlace, to which the smallest values' other sign would belong, has none: an empty range behind them.
 struct Keys { uint32_t lo, hi; };
 __device__ __forceinline__ Keys keys_of(int place)
 {
     const int entry = entry_at(place), e = entry >> 1;
     const uint32_t least = (kLow - 1 + (uint32_t)e) << 16, most = e == 0 ? (kLow << 16) - 1 : e > kRegular ? 0x7f7fffffu : least | 0xffffu;
+    if (place == kTinyPlace + 1) return Keys{~(most | 0x80000000u), ~(most | 0x80000000u) - 1};
     if (e == 0) return Keys{~(most | 0x80000000u), most | 0x80000000u};
     return entry & 1 ? Keys{~(most | 0x80000000u), ~(least | 0x80000000u)} : Keys{least | 0x80000000u, most | 0x80000000u};
 }
