@@ -561,7 +561,7 @@ __device__ __forceinline__ void load_counts(const CountSlice *parts, int n_parts
 }
 
 // A bfloat16 row from its counts: its maximum, where its run ends and how many that keeps.  false: it was not decided here (not regular, without a
-// finite value (sh.bad), or its run ends among the small values).
+// finite value (sh.bad), or a run ends among the small values).
 __device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, const Filters &f, int shift, const CountSlice *parts, int n_parts, float &peak,
                                           Weight &w, Bound &end, int &kept, Shared &sh)
 {
@@ -599,6 +599,7 @@ __device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, con
     int place = uniform(sh.found), n = uniform(sh.count);      // the run: all places before `place`, n elements of it
     first = uniform((int)sh.hi);
     if (first == kTinyPlace && tinies) return false;
+    if (place == kTinyPlace && tinies && !f.greedy && f.top_p < 1.f) return false;         // top-p's share is that of the largest of them, which the place does not tell
     peak = value_at(first);
     w = Weight{(double)peak, f.greedy ? 0.0 : 256.0 / ((double)f.T * kLn2), shift};
     // weights by value, masses of what top-k leaves, the first place whose elements are too light; small values one by one

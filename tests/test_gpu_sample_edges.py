@@ -41,3 +41,35 @@ def test_ten_zeros_and_ten_values_beside_the_smallest():
     T, k, p, m = columns([(1.0, 0, 0.75, 0.0)])
     r = run(binding.Tapout(1, 1, 20), x, T, k, p, m, None, f32)
     assert int(r["n_kept"]) == 15 and (r["kept"].cpu().view(-1)[:15] > -INF).all() and (r["kept"].cpu().view(-1)[15:] == -INF).all()
+
+
+@pytest.mark.parametrize("V", [60, 5003, 20011, 140009])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_top_k_ends_among_small_values_and_top_p_before(V, zeros):
+    """bfloat16 rows with up to 64 small values that top-k divides: top-p's share is that of those it leaves, at temperatures at which their weights differ."""
+    g = torch.Generator().manual_seed(V)
+    n = 10
+    for seed in range(4):
+        small = torch.full((20,), 1.4e-5) if seed == 0 else (torch.rand(20, generator=g) * 2 - 1) * 1.5e-5
+        x = torch.full((V,), -3.0)
+        at = torch.randperm(V, generator=g)
+        x[at[:n]] = TINY
+        x[at[n:n + 20]] = small
+        if zeros:
+            x[at[n + 20:n + 26]] = torch.tensor([0.0, -0.0] * 3)
+        x = x.to(bf16)
+        T, k, p, m = columns([(T, k, p, m) for T in (1e-6, 1e-5, 3e-6) for k in (14, 20, 25, 30) for p, m in ((0.9, 0.0), (0.35, 0.0), (0.97, 0.2))])
+        B = len(T)
+        many = x.expand(B, 1, V).contiguous()
+        u = torch.rand(B, 1, generator=g)
+        check(many, run(binding.Tapout(B, 1, V), many, T, k, p, m, u, bf16), bf16, T, k, p, m, u)
+
+
+@pytest.mark.parametrize("V", [40, 30011])
+def test_ten_largest_small_values_and_twenty_behind(V):
+    x = torch.full((1, 1, V), -1.0)
+    x[..., 3:13] = TINY
+    x[..., 14:34] = 1.4e-5
+    T, k, p, m = columns([(1e-6, 20, 0.9, 0.0)])
+    r = run(binding.Tapout(1, 1, V), x.to(bf16), T, k, p, m, None, bf16)
+    assert int(r["n_kept"]) == 16 and (r["kept"].cpu()[0, 0, 14:20] > -INF).all() and (r["kept"].cpu()[0, 0, 20:] == -INF).all()
