@@ -783,13 +783,16 @@ def fp8_quantize(x, block_rows: int = 1, out=None, stream=None):
 
 def fp8_dequantize(codes, scales, cols: int, block_rows: int = 1, dtype=torch.bfloat16, out=None, stream=None):
     """tapout_fp8_dequantize: the values [rows, cols] that codes and scales stand for; of codes [..., P] with scales [..., P / 128], as norm
-    writes them, [..., cols]."""
+    writes them, contiguous, [..., cols]."""
     lib = _lib or load_library()
     lead = codes.shape[:-1]
     if out is None:
         out = _empty((*lead, cols), dtype, codes.device, stream)
     st = _fast.fp8_dequantize(codes, scales, cols, int(block_rows), out, _handle(stream))
     if st is None and codes.dim() > 2 and block_rows == 1 and scales.shape[:-1] == lead and out.shape[:-1] == lead and out.is_contiguous():
+        for t, n in ((codes, "codes"), (scales, "scales")):    # flatten would copy them, on another stream than the call's
+            if not t.is_contiguous():
+                raise ValueError(f"{n} must be contiguous")
         fp8_dequantize(codes.flatten(0, -2), scales.flatten(0, -2), cols, 1, dtype, out.flatten(0, -2), stream)
         return out
     if st is None:

@@ -88,3 +88,12 @@ def test_plain_form_of_the_distillation():
         got = ou.distillation(h.detach(), w.detach(), ids, logits, given, torch.ones(N), 1.0, torch.float32)
         assert torch.allclose(got[0], loss) and torch.allclose(got[3], dh) and torch.allclose(got[4], dw)
         assert got[2].tolist() == [True, True, False, True, True]
+
+
+def test_8_bit_codes_that_are_not_contiguous_are_refused_not_copied():
+    """A copy would be made on the current stream, which nothing orders before the stream of the call."""
+    codes, scales, out = torch.zeros(2, 4, 128, dtype=torch.uint8), torch.ones(2, 4, 1), torch.zeros(2, 2, 96)
+    for c, s, word in ((codes[:, :2], scales[:, :2].contiguous(), "codes"), (codes[:, :2].contiguous(), scales[:, :2], "scales"),
+                       (codes.transpose(0, 1)[:2], scales[:, :2].contiguous(), "codes")):
+        with pytest.raises(ValueError, match=f"{word} must be contiguous"):
+            binding.fp8_dequantize(c, s, 96, out=out)
