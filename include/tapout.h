@@ -275,7 +275,8 @@ TAPOUT_API tapout_status tapout_draft_stats(tapout_ctx *ctx, const tapout_logits
  * token    [B,K] i32, with u;  logq [B,K] f32 or NULL
  * n_kept   [B,K] i32 or NULL: tokens that are kept
  * kept     [B,K,V] logits, binary32 or bfloat16 at any element-aligned address and
- *          strides, in memory of their own (not that of logits), or NULL
+ *          strides, in memory of their own, or NULL: rows that share memory with
+ *          each other or with those of logits are refused
  * flags    [B] u32 or NULL (overwritten): BAD_ROW, a row that holds a NaN or has no
  *          finite maximum, or whose temperature is NaN: token -1, logq NaN, nothing
  *          kept

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "common.h"
+#include "rows_meet.h"
 
 using namespace tapout;
 
@@ -526,7 +527,7 @@ tapout_status tapout_sample(tapout_ctx *ctx, const tapout_logits *logits, int32_
     if (!u && (token || logq)) return fail(ctx, TAPOUT_EINVAL, "token and logq need u");
     if (!u && !kept && !n_kept) return fail(ctx, TAPOUT_EINVAL, "nothing to be written: neither u nor kept nor n_kept is given");
     if (kept && rows_overlap(kept, B, K, V)) return fail(ctx, TAPOUT_EINVAL, "kept: rows overlap");
-    if (kept && kept->ptr == logits->ptr) return fail(ctx, TAPOUT_EINVAL, "kept is the memory of logits, which are read again");
+    if (kept && rows_meet(*logits, *kept, B, K, V)) return fail(ctx, TAPOUT_EINVAL, "kept shares memory of logits, which are read again");
     DeviceGuard guard(ctx->cfg.device);
     FilterArgs a{};
     a.base = logits->ptr; a.stride_b = logits->stride_b; a.stride_k = logits->stride_k;

@@ -73,3 +73,19 @@ def test_ten_largest_small_values_and_twenty_behind(V):
     T, k, p, m = columns([(1e-6, 20, 0.9, 0.0)])
     r = run(binding.Tapout(1, 1, V), x.to(bf16), T, k, p, m, None, bf16)
     assert int(r["n_kept"]) == 16 and (r["kept"].cpu()[0, 0, 14:20] > -INF).all() and (r["kept"].cpu()[0, 0, 20:] == -INF).all()
+
+
+def test_kept_rows_that_reach_into_the_logits_are_refused():
+    V = 96
+    flat = torch.randn(8 * V, device="cuda:0")
+    x = flat[:4 * V].view(2, 2, V)
+    tp = binding.Tapout(2, 1, V)
+    rows = lambda at, b, k, dtype=f32: flat.view(dtype).as_strided((2, 2, V), (b, k, 1), at)          # noqa: E731
+    for y in (x, rows(V, 2 * V, V), rows(4 * V - 1, 2 * V, V), rows(3 * V - 1, 3 * V, V), rows(8 * V - 2, 2 * V, V, bf16), rows(0, V, 3 * V)):
+        with pytest.raises(binding.TapoutError, match="memory of logits"):
+            tp.sample(x, out=dict(kept=y))
+    want = tp.sample(x, kept=f32)
+    for y in (rows(4 * V, 2 * V, V), rows(8 * V, 2 * V, V, bf16)):                                    # behind them
+        got = tp.sample(x, out=dict(kept=y, n_kept=torch.empty(2, 2, dtype=torch.int32, device="cuda:0")))
+        torch.cuda.synchronize()
+        assert torch.equal(got["kept"], want["kept"].to(y.dtype)) and torch.equal(got["n_kept"], want["n_kept"])
