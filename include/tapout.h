@@ -259,7 +259,8 @@ TAPOUT_API tapout_status tapout_draft_stats(tapout_ctx *ctx, const tapout_logits
  *     top_p[b] < 1: the shortest run from its start whose mass is at least top_p of
  *       the mass that top_k left (its first always); else no limit
  *     min_p[b] > 0: those with w_j >= min_p (the largest always); else no limit
- *     kept = d_j where all three keep j, else -infinity
+ *     kept = d_j where all three keep j (binary64, rounded to binary32 and from there
+ *       to bfloat16), else -infinity
  *     token = smallest j whose inclusive sum of the kept w exceeds u * Z, Z their
  *       sum;  logq = d_token - ln Z
  *   T below 2^-126, 0 and negative ones among them: greedy, the argmax (smallest

@@ -466,7 +466,7 @@ template <class E, int N> __device__ __forceinline__ void store_any(E *to, const
     }
 }
 
-// What a row asks for.  Temperatures below the smallest normal number, whose inverse binary32 does not hold, are as good as 0.
+// What a row asks for.  Temperatures below the smallest normal number are taken as 0.
 constexpr float kLeastT = 0x1p-126f;
 struct Filters {
     float T, top_p, min_p; int top_k; bool greedy;
@@ -767,10 +767,13 @@ __device__ __forceinline__ void by_places(const RowReader<DT> &row, const Filter
 // What every row keeps.  Elements are kept that are larger than one of two values: up to the index `last` than `from`, behind it than `above`, which
 // differ where equal elements are kept in part.
 struct FilterRow {
-    float max, inv, above, from;
+    float max, above, from;
     int32_t last, kept;                        // kept: -1 where it was not counted
-    int32_t bad, pad;
-    double c;                                  // see Weight
+    int32_t bad;
+    double inv, c;                             // 1 / T, 0 of a greedy row;  see Weight
+    // In binary64 and rounded once: in binary32 the difference, the inverse and the product are a rounding each, and a difference beyond it is infinite
+    // whatever T is.
+    __device__ __forceinline__ float logit(float x) const { return (float)(((double)x - (double)max) * inv); }
 };
 static_assert(sizeof(FilterRow) == kFilterRowBytes, "the context makes room for it");
 
@@ -824,8 +827,8 @@ __global__ __launch_bounds__(kThreads) void filter_rows_kernel(FilterArgs a, int
     __syncthreads();
     if (threadIdx.x) return;
     const bool bad = sh.bad;
-    FilterRow q{max, f.greedy ? 0.f : 1.f / f.T, end.x, end.x, kNone, kept, bad, 0, w.c};
-    if (bad) q = FilterRow{0.f, 0.f, INFINITY, INFINITY, kNone, 0, 1, 0, 0.0};
+    FilterRow q{max, end.x, end.x, kNone, kept, bad, f.greedy ? 0.0 : 1.0 / (double)f.T, w.c};
+    if (bad) q = FilterRow{0.f, INFINITY, INFINITY, kNone, 0, 1, 0.0, 0.0};
     else if (end.index == kAll) q.above = q.from = below(end.x);
     else if (end.index != kNone) { q.from = below(end.x); q.last = end.index; }
     a.rows[r] = q;
@@ -918,7 +921,7 @@ __global__ __launch_bounds__(kSliceThreads) void filter_slices_kernel(FilterArgs
         if (draw) mine += kept_units<DT>(w, words[t], keeps, j0, table);
         if (!out) continue;
 #pragma unroll
-        for (int e = 0; e < n; ++e) y[e] = in[e] ? (x[e] - q.max) * q.inv : -INFINITY;
+        for (int e = 0; e < n; ++e) y[e] = in[e] ? q.logit(x[e]) : -INFINITY;
         if (!row.whole(v)) continue;
         if (a.kept_dtype == TAPOUT_F32) store_any<float, n>((float *)out + j0, y);
         else store_any<__bf16, n>((__bf16 *)out + j0, y);
@@ -930,7 +933,7 @@ __global__ __launch_bounds__(kSliceThreads) void filter_slices_kernel(FilterArgs
             if (row.whole(v) || (v - v0) % kSliceThreads != (int)threadIdx.x || v < v0 || v >= v0 + kSliceVecs || (e && v == 0)) continue;
             each_chosen<DT>(row.load(v), (1u << n) - 1, row.first(v), [&](float x, int j) {
                 if (j < 0 || j >= a.V) return;
-                const float z = x > (j <= q.last ? q.from : q.above) ? (x - q.max) * q.inv : -INFINITY;
+                const float z = x > (j <= q.last ? q.from : q.above) ? q.logit(x) : -INFINITY;
                 if (a.kept_dtype == TAPOUT_F32) ((float *)out)[j] = z;
                 else ((__bf16 *)out)[j] = (__bf16)z;
             });
@@ -1010,7 +1013,7 @@ __global__ __launch_bounds__(kSliceThreads) void filter_tokens_kernel(FilterArgs
 #pragma unroll
             for (int e = n - 1; e >= 0; --e) {
                 const int j = row.first(v) + e;
-                if (x[e] > (j <= q.last ? q.from : q.above) && (double)(x[e] - q.max) * (double)q.inv > -745.13) first = min(first, j);
+                if (x[e] > (j <= q.last ? q.from : q.above) && ((double)x[e] - (double)q.max) * q.inv > -745.13) first = min(first, j);
             }
             if (first < 0x7fffffff) break;
         }

@@ -89,3 +89,39 @@ def test_kept_rows_that_reach_into_the_logits_are_refused():
         got = tp.sample(x, out=dict(kept=y, n_kept=torch.empty(2, 2, dtype=torch.int32, device="cuda:0")))
         torch.cuda.synchronize()
         assert torch.equal(got["kept"], want["kept"].to(y.dtype)) and torch.equal(got["n_kept"], want["n_kept"])
+
+
+@pytest.mark.parametrize("dtype", [f32, bf16])
+@pytest.mark.parametrize("kept", [f32, bf16])
+@pytest.mark.parametrize("V", [7, 1003, 9001])
+def test_kept_logits_are_rounded_once(V, dtype, kept):
+    """(x - max) / T in binary64, where the difference, the inverse and their product are off by 2^-53 each, to binary32 and, of bfloat16, from
+    there: half a step of each type, and of binary32's smallest numbers."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.stack([torch.randn(V, generator=g) * s for s in (1.0, 3.0, 30.0, 1e-3, 1e6)]
+                    + [30 - 40 * torch.rand(V, generator=g), 1e-30 * torch.randn(V, generator=g), 1e30 * torch.randn(V, generator=g)]).to(dtype)
+    temperatures = (0.7, 1.3, 0.3333, 1.0, 7e-6, 3e38, 2e-38, INF)          # from 2^-126 on, about 1.2e-38, no greedy ones
+    B, K = len(x), len(temperatures)
+    T = torch.tensor(temperatures)
+    many = x.expand(K, B, V).transpose(0, 1).reshape(B * K, 1, V).contiguous()
+    r = run(binding.Tapout(B * K, 1, V), many, T.repeat(B), None, None, None, None, kept)
+    d = (many.double() - many.double().amax(-1, keepdim=True)) / T.repeat(B).double()[:, None, None]
+    inside = d.abs() < 3.3e38
+    got = r["kept"].cpu().double()
+    assert not torch.isnan(got).any() and (r["n_kept"].cpu() == V).all()
+    half = 2.0 ** -24 + 2.0 ** -50
+    bound = (half if kept == f32 else 2.0 ** -8 * (1 + half) + half) * d.abs() + (2.0 ** -150 if kept == f32 else 2.0 ** -133)
+    assert ((got - d).abs()[inside] <= bound[inside]).all()
+    assert (got[~inside] <= -3.3e38 * (1 - 2.0 ** -8)).all()
+
+
+@pytest.mark.parametrize("dtype", [f32, bf16])
+def test_the_whole_range_under_an_infinite_temperature(dtype):
+    """All weights are 1 and all kept logits 0, also of values whose difference is beyond binary32."""
+    x = torch.tensor([3e38, -3e38, 0.0, -1.0, -INF, 3e38, -2e38, 1e30]).to(dtype).view(1, 1, 8)
+    T = torch.tensor([INF])
+    for u, token in ((0.0, 0), (0.2, 1), (0.5, 3), (0.6, 5), (0.99, 7)):
+        r = run(binding.Tapout(1, 1, 8), x, T, None, None, None, torch.tensor([[u]]), dtype)
+        kept = r["kept"].cpu().view(-1).tolist()
+        assert [v == 0 for v in kept] == [True] * 4 + [False] + [True] * 3 and kept[4] == -INF
+        assert int(r["token"]) == token and int(r["n_kept"]) == 7 and abs(float(r["logq"]) + math.log(7)) < 1e-6
