@@ -159,7 +159,10 @@ typedef struct {
 TAPOUT_API void tapout_default_config(tapout_config *cfg, int32_t max_batch, int32_t max_k, int32_t vocab);
 
 /* Create a context on cfg->device: validates cfg (host), allocates scratch
- * and bandit state (all plays zero).  *out is NULL on failure.               */
+ * and bandit state (all plays zero).  *out is NULL on failure.  Part of the
+ * scratch is that of tapout_sample, whether it is called or not: for a row of
+ * max_batch * (max_k + 1) 40 bytes and 16 for 2048 elements (no more than the
+ * largest call needs: 436 MB), and 96 KB for each of the first 256 rows.      */
 TAPOUT_API tapout_status tapout_create(tapout_ctx **out, const tapout_config *cfg);
 TAPOUT_API tapout_status tapout_destroy(tapout_ctx *ctx);
 /* Text of the last error on ctx (valid until the next call on ctx); with
@@ -269,7 +272,9 @@ TAPOUT_API tapout_status tapout_draft_stats(tapout_ctx *ctx, const tapout_logits
  *   Weights are computed in double and summed as whole multiples of 2^-s of the
  *   largest, s = min(50, 62 - ceil(log2 V)): results do not depend on how the work
  *   is divided.
- * logits   [B,K,V], K up to max_k + 1 (target rows);  V at most 2^24
+ * logits   [B,K,V], K up to max_k + 1 (target rows);  V at most 2^24, and B * K
+ *          less than 2^22 and than 2^24 slices, of which a row has one for 2048
+ *          (bfloat16: 4096) elements or a part of them and its first vector's
  * k_len    [B] i32 or NULL: rows k >= k_len[b] are not read, their outputs untouched
  * temperature, top_p, min_p [B] f32, top_k [B] i32, each or NULL (1, 1, 0, 0)
  * u        [B,K] f32 in [0,1), or NULL: no tokens are drawn

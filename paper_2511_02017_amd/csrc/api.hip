@@ -247,7 +247,9 @@ const char *check_logits(const tapout_logits *l, const char *name, int V, int ro
     return nullptr;
 }
 
+// Of one call of tapout_sample: a launch has less than 2^32 threads, 256 a slice, 1024 a row.  A context has room for no more.
 constexpr int kMaxFilterVocab = 1 << 24;
+constexpr int64_t kMaxFilterSlices = 1 << 24, kMaxFilterRows = 1 << 22;
 
 // Whether two of the B x K rows of `len` elements share memory.
 bool rows_overlap(const tapout_logits *x, int B, int K, int len)
@@ -405,8 +407,8 @@ tapout_status tapout_create(tapout_ctx **out, const tapout_config *cfg)
         table[256 + 2 * idx] = pos;
         table[256 + 2 * idx + 1] = neg;
     }
-    const size_t filter_n = (size_t)cfg->max_batch * (cfg->max_k + 1);
-    const size_t count_n = std::min(filter_n, (size_t)kCountRows) * kCountParts;
+    const size_t filter_n = std::min(rows, (size_t)kMaxFilterRows), count_n = std::min(rows, (size_t)kCountRows) * kCountParts;
+    const size_t slice_n = std::min(filter_n * filter_slices(std::min(cfg->vocab, kMaxFilterVocab), TAPOUT_F32), (size_t)kMaxFilterSlices);
     bool ok = hipMalloc(&c->part, c->part_cap * sizeof(Partial)) == hipSuccess
            && hipMalloc(&c->part_t, c->part_cap * sizeof(Partial)) == hipSuccess
            && hipMalloc(&c->part1, nsums * sizeof(double)) == hipSuccess
@@ -418,7 +420,7 @@ tapout_status tapout_create(tapout_ctx **out, const tapout_config *cfg)
            && hipMalloc(&c->flags_ws, (size_t)cfg->max_batch * sizeof(uint32_t)) == hipSuccess
            && hipMalloc(&c->filter_rows, filter_n * kFilterRowBytes) == hipSuccess
            && hipMalloc(&c->filter_counts, count_n * kCountSliceBytes) == hipSuccess
-           && hipMalloc(&c->filter_slices, filter_n * filter_slices(cfg->vocab, TAPOUT_F32) * sizeof(FilterSlice)) == hipSuccess
+           && hipMalloc(&c->filter_slices, slice_n * sizeof(FilterSlice)) == hipSuccess
            && hipMalloc(&c->arm_played, (size_t)cfg->max_batch * sizeof(int32_t)) == hipSuccess
            && hipMalloc(&c->sum_r, nstate * sizeof(double)) == hipSuccess
            && hipMalloc(&c->sum_r2, nstate * sizeof(double)) == hipSuccess
@@ -535,8 +537,7 @@ tapout_status tapout_sample(tapout_ctx *ctx, const tapout_logits *logits, int32_
     a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u;
     a.token = token; a.n_kept = n_kept; a.logq = logq; a.flags = flags; a.exp_table = ctx->exp_table;
     a.rows = ctx->filter_rows; a.slices = ctx->filter_slices; a.counts = ctx->filter_counts;
-    // a launch has less than 2^32 threads: 256 a slice, 1024 a row
-    if ((int64_t)B * K * filter_slices(V, logits->dtype) >= 1 << 24 || (int64_t)B * K >= 1 << 22)
+    if ((int64_t)B * K * filter_slices(V, logits->dtype) >= kMaxFilterSlices || (int64_t)B * K >= kMaxFilterRows)
         return fail(ctx, TAPOUT_EUNSUPPORTED, "B * K = %lld rows beyond 2^22 or 2^24 slices", (long long)B * K);
     if (kept) { a.kept = (void *)kept->ptr; a.kept_dtype = kept->dtype; a.kept_stride_b = kept->stride_b; a.kept_stride_k = kept->stride_k; }
     const hipError_t e = launch_filtered_sample(a, logits->dtype, (hipStream_t)stream);

@@ -125,3 +125,43 @@ def test_the_whole_range_under_an_infinite_temperature(dtype):
         kept = r["kept"].cpu().view(-1).tolist()
         assert [v == 0 for v in kept] == [True] * 4 + [False] + [True] * 3 and kept[4] == -INF
         assert int(r["token"]) == token and int(r["n_kept"]) == 7 and abs(float(r["logq"]) + math.log(7)) < 1e-6
+
+
+def test_a_context_has_room_for_the_calls_it_takes():
+    """Rows of more than 2^24 elements are not sampled: a context for them has no room for their slices (1.1 GB here), nor has it for more rows or slices
+    than a call may have."""
+    held = []
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    held.append(binding.Tapout(8, 16, 2 ** 30))
+    assert free - torch.cuda.mem_get_info()[0] < 400e6
+    with pytest.raises(binding.TapoutError, match="2\\^24"):
+        held[0].sample(torch.zeros(1, device="cuda:0").expand(1, 1, 2 ** 24 + 1).contiguous(), kept=bf16)
+
+
+@pytest.mark.parametrize("dtype", [f32, bf16])
+def test_as_many_rows_as_a_call_may_have(dtype):
+    B, K, V = 65535, 64, 6
+    row = torch.tensor([0.5, -1.0, 2.0, -INF, 1.0, 2.0]).to(dtype).to("cuda:0")
+    tp = binding.Tapout(B, K, V)
+    u = torch.full((B, K), 0.6, device="cuda:0")
+    u[B // 2:] = 0.3
+    r = tp.sample(row.expand(B, K, V), u, top_k=torch.full((B,), 2, dtype=torch.int32, device="cuda:0"))
+    torch.cuda.synchronize()
+    assert bool((r["n_kept"] == 2).all()) and bool((r["flags"] == 0).all())
+    assert bool((r["token"][:B // 2] == 5).all()) and bool((r["token"][B // 2:] == 2).all())
+    with pytest.raises(binding.TapoutError, match="rows beyond"):
+        tp.sample(row.expand(B, K + 1, V), kept=dtype)
+
+
+def test_as_many_slices_as_a_call_may_have():
+    B, K, V = 23, 89, 2 ** 24                      # 2047 rows of 8193 slices
+    row = torch.full((V,), -3.0, device="cuda:0")
+    row[V - 1], row[5] = 4.0, 3.0
+    tp = binding.Tapout(B, K, V)
+    u = torch.rand(B, K, device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(1))
+    u[0, 0], u[0, 1], u[B - 1, K - 1], u[B - 1, K - 2] = 0.0, 0.999, 0.999, 0.0
+    r = tp.sample(row.expand(B, K, V), u, min_p=torch.full((B,), 0.1, device="cuda:0"))
+    torch.cuda.synchronize()
+    first = math.exp(-1) / (1 + math.exp(-1))
+    assert bool((r["n_kept"] == 2).all()) and torch.equal(r["token"], torch.where(u.double() < first, 5, V - 1).int())
