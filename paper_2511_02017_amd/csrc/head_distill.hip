@@ -153,6 +153,8 @@ __global__ __launch_bounds__(256) void listed_rows_kernel(ListedArgs a)
 // bfloat16: the element is made from the listed logit, since what is in the piece is rounded already.  binary32: the teacher's share is taken from the
 // element that is there.  Its logit is summed like those in lse, so an error that a large one has is in both and mostly leaves the quotient: from the
 // listed logit, which is nearer to the exact one, dW was off by 3.3e-6 of its norm (40 rows, V = 32000, dim = 1024), three times as far.
+// Every entry is compared with all of its row's, and the list is gone through for each piece of the vocabulary: 8192 rows, V = 128256 in four pieces, 25 us a
+// piece for 64 listed tokens, 1.44 ms for 1024 (with 3.9 ms for their logits in the loss 42 % of the 23.0 ms of loss and gradients, 256 listed: 14.6).
 constexpr int kListCap = 1024;
 template <class E>
 __global__ __launch_bounds__(64) void listed_grad_kernel(ListedArgs a, GradArgs piece)

@@ -660,8 +660,10 @@ template <int KIND, int TI_, int TJ_, int WI_, int WJ_, bool TURNED = false> str
             };
             // 8-bit products: a stage has one scale, so every block's products of a stage leave the matrix unit by themselves and are added with their
             // factor by the vector unit, while the next ones are under way.  The barrier that hands both places on comes where the last of a stage's
-            // blocks have been read.  4096 rows, V = 151936, dim = 2048: 1.30 ms, 1.96 PFLOP/s (a library product of such codes without scales 1.11): a
-            // stage of the 256 x 256 tile moves 256 KB through LDS, 2048 cycles of it, as many as its products take.
+            // blocks have been read.  4096 rows, V = 151936, dim = 2048: 1.30 ms, 1.96 PFLOP/s (a library product of such codes without scales
+            // 1.11).  Of some 4200 cycles of a stage of the 256 x 256 tile the matrix unit is busy for 48 %, the vector unit for 46 (128 scaled additions and 18
+            // other instructions to a wavefront's 32 products), LDS for 20: none is the bound by itself, but the first two fill the time between them, as if a
+            // SIMD's two wavefronts took turns.  Why they do not overlap more is not known.
             auto f8_stage = [&](int s) {
                 if constexpr (f8) {
                     constexpr bool wide = KIND == kTileF8x;

@@ -682,7 +682,9 @@ __device__ __forceinline__ bool by_counts(const RowReader<TAPOUT_BF16> &row, con
     return true;
 }
 
-// Any row.
+// Any row.  A bfloat16 row with a finite value of 128 or more, of either sign, comes here behind its counting, so that rows masked by finite values take
+// longer than rows masked by -infinity: 64 rows of 128256 under mixed filters, with their tokens, 119 us for 45, 576 target rows under top-p 333 for 134,
+// whether the masked logits are -1e4, -1e9 or the type's lowest value.
 template <int DT>
 __device__ __forceinline__ void by_places(const RowReader<DT> &row, const Filters &f, int shift, float &peak, Weight &w, Bound &end, Shared &sh)
 {
@@ -873,9 +875,10 @@ template <int DT> __device__ __forceinline__ uint64_t kept_units(const Weight &w
     return sum;
 }
 
-// The filtered logits, and a slice's kept elements and weights: a workgroup a slice, all of its loads requested first.  Bound by memory where rows are
-// many: 576 rows of 128256 bfloat16, read and written, 46 us, 6.4 TB/s.  Slices of 256 vectors a turn, us with 1 / 2 / 4 / 8 turns: 66.9 / 46.1 /
-// 49.0 / 50.0, 64 such rows with tokens (both kernels) 20.7 / 19.7 / 22.6 / 29.5, one row of 32000 binary32 9.2 / 9.7 / 12.0 / 15.5.
+// The filtered logits, and a slice's kept elements and weights: a workgroup a slice, all of its loads requested first.  Where rows are many bound by
+// memory and by the vector unit, which binary64 keeps 79 % busy: 576 rows of 128256 bfloat16, read and written, 49 us, 6.0 TB/s (46 with kept logits in
+// binary32, three roundings each).  Measured with those, slices of 256 vectors a turn, us with 1 / 2 / 4 / 8 turns: 66.9 / 46.1 / 49.0 / 50.0, 64 such
+// rows with tokens (both kernels) 20.7 / 19.7 / 22.6 / 29.5, one row of 32000 binary32 9.2 / 9.7 / 12.0 / 15.5.
 template <int DT>
 __global__ __launch_bounds__(kSliceThreads) void filter_slices_kernel(FilterArgs a, int slices)
 {
