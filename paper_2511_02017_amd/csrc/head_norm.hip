@@ -53,9 +53,9 @@ template <int TPR> __device__ __forceinline__ double row_sum(double v, double *s
     return v;
 }
 
-// A row for TPR threads, VPT 16-byte vectors a thread, all of them (of long rows, those of x) requested before the first is used.  A thread reads each of its places of
-// a row before it writes there, and no other thread does either, so that the sum may take the place of x or of the residual.  Bound by memory: 8192 rows of 2048 bfloat16 with a residual 23.7 us, 5.7 TB/s; to
-// 8 bits, 64 rows: 3.9 us, the launch.
+// A row for TPR threads, VPT 16-byte vectors a thread, all of them (of long rows, those of x) requested before the first is used.  A thread reads each of
+// its places of a row before it writes there, and no other thread does either, so that the sum may take the place of x or of the residual.  Bound by
+// memory: 8192 rows of 2048 bfloat16 with a residual 23.7 us, 5.7 TB/s; to 8 bits, 64 rows: 3.9 us, the launch.
 template <class E, int TPR, int VPT>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void head_norm_kernel(NormArgs a)
 {
